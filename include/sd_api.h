@@ -134,6 +134,137 @@ size_t sd_kv_page_bytes(const sd_model_cfg* cfg, int32_t page_size);
 sd_status sd_bind_kv_paged(sd_engine e, void* k_pages, void* v_pages, int32_t n_pages, int32_t page_size,
                            const int32_t* block_table, int32_t pages_per_seq, int32_t* kv_len);
 
+/* ------------------------------------------- rotary tables, 4-bit KV cache */
+
+/* Rotary position tables.  Pair i of rot_dim/2 turns by the angle p * f_i at
+ * position p, f_i = theta^(-2i/rot_dim), scaled for contexts longer than the
+ * model was trained on (orig_ctx positions) by
+ *   SD_ROPE_NONE    nothing;
+ *   SD_ROPE_LINEAR  f_i / factor;
+ *   SD_ROPE_LLAMA3  by wavelength: t = (orig_ctx f_i / 2pi - low)/(high - low)
+ *                   clamped to [0, 1], f_i (t + (1 - t)/factor);
+ *   SD_ROPE_YARN    by index: f_i ((1 - t) + t/factor) with t = (i - a)/max(b - a,
+ *                   0.001) clamped to [0, 1], a = max(floor(c(high)), 0), b =
+ *                   min(ceil(c(low)), rot_dim - 1), c(turns) = rot_dim *
+ *                   ln(orig_ctx/(2pi turns)) / (2 ln theta); every entry is
+ *                   multiplied by attn_factor, or 0.1 ln(factor) + 1 where
+ *                   attn_factor is 0.
+ * attn_factor is 0 or 1 in the other kinds. */
+typedef enum { SD_ROPE_NONE = 0, SD_ROPE_LINEAR = 1, SD_ROPE_LLAMA3 = 2, SD_ROPE_YARN = 3 } sd_rope_scaling;
+
+typedef struct {
+    double theta;               /* base, > 1 */
+    double factor;              /* >= 1 (not read by SD_ROPE_NONE) */
+    double low, high;           /* LLAMA3: frequency factors, YARN: turns; 0 < low < high (read by these two) */
+    double attn_factor;         /* YARN's multiplier, 0 = by its formula */
+    int32_t rot_dim;            /* rotated dims of a head: even, 2..256 */
+    int32_t scaling;            /* sd_rope_scaling */
+    int32_t orig_ctx;           /* >= 1 (LLAMA3, YARN) */
+    int32_t reserved;           /* 0 */
+} sd_rope_cfg;
+
+/* table[p][i] = (cos, sin) of p * f_i for p in [0, n_pos), fp32[n_pos][rot_dim/2][2]
+ * (8-byte aligned), computed in fp64 and rounded once.  Errors: SD_E_INVAL. */
+sd_status sd_rope_table(const sd_rope_cfg* cfg, int32_t n_pos, float* table, void* stream);
+
+/* Replaces the engine's own table (theta of its configuration, unscaled), for
+ * every later call whatever cache is bound: rot_dim must be head_dim (the
+ * engine turns whole heads, rotate-half).  Enqueued on `stream`; steps that run
+ * on another stream must be ordered after it by the caller, and keys cached
+ * under another table stay as they were. */
+sd_status sd_set_rope(sd_engine e, const sd_rope_cfg* cfg, void* stream);
+
+/* A paged KV cache held in 4 bits.  Every K and V row of a KV head (K after the
+ * rotation) is one affine group of head_dim values: with y the row in fp32,
+ *   s = bf16((max y - min y)/15),  z = bf16(min y + 8 s),
+ *   c = clamp(rint((y - z)/s) + 8, 0, 15)   (c = 8 where s = 0),
+ * the quotient exact and rounded half to even; the row stands for z + s (c - 8).
+ * A row with a value that is not finite is stored as s = z = NaN and reads as
+ * NaN.  A page holds page_size positions of every layer and KV head,
+ * [n_layers][n_kv][page_size/32] tiles of 32 positions, D = head_dim:
+ *   K codes  [32 positions][D/8] words, word w of a position holding its dims
+ *            8w + e;
+ *   V codes  [4 groups][D] words, word d of group j holding dim d of positions
+ *            8j + e;
+ *   K params [32] words, V params [32] words: s in the low half, z in the high;
+ * element e = 0..7 of a code word in the nibble at bit 4*(e/2) + 16*(e%2).
+ * The tensors are the caller's, as those of sd_bind_kv_paged; flags (may be
+ * NULL) collects what a call without an engine finds on the device: words that
+ * are set to 1 and never cleared by the library, [0] slot outside [0,
+ * max_slots), [2] position outside [0, max_ctx) or past the rotary table, [3]
+ * block-table entry outside [0, n_pages), [4] row count outside [0, n] (it is
+ * clamped).  What they concern is skipped: nothing of the cache is read or
+ * written for it, its rows of q_out, k_out, v_out and out are zeros, and the
+ * positions of a missing page are as if masked. */
+typedef struct {
+    void* pages;                /* 16-byte aligned, n_pages * sd_kv4_page_bytes(...) */
+    const int32_t* block_table; /* int32[max_slots][pages_per_seq] */
+    int32_t* kv_len;            /* int32[max_slots] */
+    uint32_t* flags;            /* uint32[5] or NULL */
+    int32_t n_pages, page_size, pages_per_seq;  /* page_size: a multiple of 32, pages_per_seq * page_size >= max_ctx */
+    int32_t n_layers, n_kv, head_dim;           /* head_dim 64 or 128 */
+    int32_t max_slots, max_ctx;
+} sd_kv4_cache;
+
+/* Bytes of a page: n_layers * n_kv * page_size * (head_dim + 8); 0 for
+ * arguments outside what sd_kv4_cache allows. */
+size_t sd_kv4_page_bytes(int32_t n_layers, int32_t n_kv, int32_t head_dim, int32_t page_size);
+
+/* The three calls below need no engine and allocate nothing.  Row i of B
+ * sequences x n rows is position kv_len[slots[b]] + i of slot slots[b] (the
+ * lengths are not changed); with lens (device int32[B], may be NULL) only rows
+ * i < lens[b] exist, and nothing of the others is read or written.  A slot is
+ * named once in a call.  Rows are addressed as base + (b*n + i)*ld + head *
+ * head_dim + d, ld in elements, with base 16-byte aligned and ld a multiple of
+ * 8 (bf16) or 4 (fp32), at least heads*head_dim.  The structs are read before
+ * the call returns.  Errors: SD_E_INVAL. */
+
+/* How sd_kv4_append rotates q and k: by a table of `len` positions
+ * (sd_rope_table), pairs (i, i + rot_dim/2) or, interleaved, (2i, 2i + 1) of the
+ * first rot_dim dims of a head; rot_dim a multiple of 16 up to head_dim, or 0
+ * (no rotation, no table). */
+typedef struct {
+    const float* table;         /* 16-byte aligned */
+    int32_t len, rot_dim, interleaved;
+} sd_rope_args;
+
+/* Stores the rows of k and v (sd_dtype `dtype`) in layer `layer` of the cache:
+ * k rotated (products and sum exact, rounded once to fp32), both quantized.
+ * q (same dtype, may be NULL) is rotated into q_out (bf16, contiguous
+ * [B*n][n_q][head_dim]).  Positions around the new rows keep their contents. */
+sd_status sd_kv4_append(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                        const int32_t* lens, int32_t dtype, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                        const void* q, int64_t q_ld, int32_t n_q, void* q_out, const sd_rope_args* rope, void* stream);
+
+/* The stored values of positions start[b] + i, i < n (start: device int32[B];
+ * any cached positions, lens as above), rounded to bf16: k_out and v_out bf16
+ * [B*n][n_kv][head_dim], contiguous, 16-byte aligned. */
+sd_status sd_kv4_read(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                      const int32_t* start, const int32_t* lens, void* k_out, void* v_out, void* stream);
+
+/* Bytes of the workspace of sd_kv4_attention (0 for arguments it refuses). */
+size_t sd_kv4_workspace_bytes(const sd_kv4_cache* c, int32_t B, int32_t n, int32_t n_q);
+
+/* Attention of the rows' queries over layer `layer` of the cache: row (b, i)
+ * sees the positions up to its own, which the caller has appended,
+ *   out = sum_p softmax_p(scale q.k_p) v_p,
+ * query head h reading KV head h/(n_q/n_kv).  q (bf16, rotated, row stride
+ * q_ld) and out (bf16, row stride out_ld).  workspace: 256-byte aligned,
+ * sd_kv4_workspace_bytes; its contents need no preparation, and calls whose
+ * work may overlap need one each.  A row that sees no position gives zeros. */
+sd_status sd_kv4_attention(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                           const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld, float scale, void* out,
+                           int64_t out_ld, void* workspace, size_t bytes, void* stream);
+
+/* Binds a 4-bit cache to the engine: prefill, draft, verify, AR step and
+ * rollback then run on it as on the caches above (both forwards attend what is
+ * cached, the new rows included, in 4 bits).  Replaces any earlier binding.
+ * c's n_layers, n_kv and head_dim must be the model's, max_slots and max_ctx at
+ * least the engine's; flags is not used (sd_sync reports).  Allocates a buffer for
+ * the rotated queries on first use.  Errors: SD_E_INVAL, SD_E_UNSUPPORTED (an
+ * fp32 model), SD_E_NOMEM. */
+sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c);
+
 /* Drafter weight formats (RTN, groups of 128 weights along K, one fp16 scale
  * per (output column, group)): int4 symmetric (Sec. 4.1, the default), int4
  * asymmetric with a zero point per (column, group) (App. B.2), and int8

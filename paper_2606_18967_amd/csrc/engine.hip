@@ -56,7 +56,7 @@ struct workspace {
     float* h = nullptr;
     void* a = nullptr;
     float* qkv = nullptr;
-    float* qrot = nullptr;       // rotated queries (fp32 cache)
+    void* qrot = nullptr;        // rotated queries (fp32: fp32 cache, bf16: 4-bit cache)
     void* att = nullptr;
     float* gu = nullptr;
     void* act = nullptr;
@@ -80,6 +80,8 @@ struct sd_engine_s {
     void* v = nullptr;
     int32_t* kv_len = nullptr;
     kv_geom geo = {};                  // dense or paged layout of k / v
+    bool kv4 = false;                  // the cache is the 4-bit one of geo4 instead
+    kv4_geom geo4 = {};
     std::vector<const uint32_t*> qw;   // [L*4] packed codes
     std::vector<const uint16_t*> qs;   // [L*4] scales
     std::vector<const uint8_t*> qz;    // [L*4] zero points (asymmetric format), else NULL
@@ -256,7 +258,8 @@ struct ws_blocks_t {
 
 // A prefill's buffers hold the target's activations only (bf16 ones in two
 // bytes), and no gate/up: its SwiGLU is fused or reads the split partials.
-static ws_blocks_t ws_blocks(const sd_model_cfg& c, int max_slots, bool prefill, workspace& w)
+// kv4: with the queries that the 4-bit cache's append rotates (bf16).
+static ws_blocks_t ws_blocks(const sd_model_cfg& c, int max_slots, bool prefill, workspace& w, bool kv4 = false)
 {
     const size_t R = (size_t)w.rows, qkvN = (size_t)(c.n_q + 2 * c.n_kv) * c.head_dim, qd = (size_t)c.n_q * c.head_dim;
     const bool f32 = c.dtype == SD_DTYPE_F32;
@@ -271,7 +274,7 @@ static ws_blocks_t ws_blocks(const sd_model_cfg& c, int max_slots, bool prefill,
     l.add(&w.act, R * c.ffn * el);
     l.add(&w.att_part, attention_part_floats(w.rows, c.n_q, c.n_kv, c.head_dim, f32) * 4);
     l.add(&w.gpart, gp);
-    if (f32) l.add(&w.qrot, R * qd * 4);
+    if (f32 || kv4) l.add(&w.qrot, R * qd * (f32 ? 4 : 2));
     if (!prefill || f32) l.add(&w.gu, R * 2 * (size_t)c.ffn * 4);
     return l;
 }
@@ -332,7 +335,7 @@ static workspace& prefill_ws(sd_engine e, long long rows, hipStream_t s)
     }
     workspace w;
     w.rows = PREFILL_ROWS;
-    const ws_blocks_t blocks = ws_blocks(e->c, e->max_slots, true, w);
+    const ws_blocks_t blocks = ws_blocks(e->c, e->max_slots, true, w, e->kv4);
     size_t need = 0, avail = 0, total = 0;
     for (int i = 0; i < blocks.n; ++i) need += blocks.b[i].bytes;
     if (hipMemGetInfo(&avail, &total) != hipSuccess) (void)hipGetLastError();
@@ -424,6 +427,7 @@ extern "C" sd_status sd_bind_kv(sd_engine e, void* k, void* v, int32_t* kv_len)
     e->v = v;
     e->kv_len = kv_len;
     const long long D = e->c.head_dim, H = e->c.n_kv, C = e->max_ctx;
+    e->kv4 = false;
     e->geo = kv_geom{e->max_ctx, H * C * D, (long long)e->max_slots * H * C * D, C * D, nullptr, 1, e->max_slots};
     return SD_OK;
 }
@@ -451,7 +455,221 @@ extern "C" sd_status sd_bind_kv_paged(sd_engine e, void* k_pages, void* v_pages,
     e->v = v_pages;
     e->kv_len = kv_len;
     const long long D = e->c.head_dim, H = e->c.n_kv, L = e->c.n_layers, P = page_size;
+    e->kv4 = false;
     e->geo = kv_geom{page_size, L * H * P * D, H * P * D, P * D, block_table, pages_per_seq, n_pages};
+    return SD_OK;
+}
+
+// ------------------------------------------------------------------ rotary tables, 4-bit cache
+static sd_status check_rope(const sd_rope_cfg* c)
+{
+    if (!c) return fail(SD_E_INVAL, "rope cfg is NULL");
+    if (c->rot_dim < 2 || c->rot_dim > 256 || c->rot_dim % 2)
+        return fail(SD_E_INVAL, "rot_dim=%d must be even and in [2, 256]", c->rot_dim);
+    if (!(c->theta > 1.0) || !isfinite(c->theta)) return fail(SD_E_INVAL, "theta must be finite and > 1");
+    if (c->scaling < SD_ROPE_NONE || c->scaling > SD_ROPE_YARN) return fail(SD_E_INVAL, "unknown rope scaling %d", c->scaling);
+    if (c->reserved) return fail(SD_E_INVAL, "reserved must be 0");
+    if (c->scaling != SD_ROPE_NONE && (!(c->factor >= 1.0) || !isfinite(c->factor)))
+        return fail(SD_E_INVAL, "factor must be finite and >= 1");
+    if (c->scaling == SD_ROPE_LLAMA3 || c->scaling == SD_ROPE_YARN) {
+        if (!(c->low > 0.0) || !(c->high > c->low) || !isfinite(c->high)) return fail(SD_E_INVAL, "need 0 < low < high, finite");
+        if (c->orig_ctx < 1) return fail(SD_E_INVAL, "orig_ctx must be >= 1");
+    }
+    const bool mul = c->scaling == SD_ROPE_YARN;
+    if (!(c->attn_factor >= 0.0) || !isfinite(c->attn_factor) || (!mul && c->attn_factor != 0.0 && c->attn_factor != 1.0))
+        return fail(SD_E_INVAL, "attn_factor must be finite and >= 0 (YARN), 0 or 1 (others)");
+    return SD_OK;
+}
+
+constexpr int KV4_MAX_CTX = 1 << 30;
+
+extern "C" sd_status sd_rope_table(const sd_rope_cfg* cfg, int32_t n_pos, float* table, void* stream)
+{
+    sd_status st = check_rope(cfg);
+    if (st != SD_OK) return st;
+    if (!table || ((uintptr_t)table & 7)) return fail(SD_E_INVAL, "table is NULL or not 8-byte aligned");
+    if (n_pos < 1 || n_pos > KV4_MAX_CTX) return fail(SD_E_INVAL, "n_pos=%d outside [1, %d]", n_pos, KV4_MAX_CTX);
+    launch_rope_table(*cfg, n_pos, table, (hipStream_t)stream);
+    return launched("sd_rope_table");
+}
+
+extern "C" sd_status sd_set_rope(sd_engine e, const sd_rope_cfg* cfg, void* stream)
+{
+    if (!e) return fail(SD_E_INVAL, "engine is NULL");
+    sd_status st = check_rope(cfg);
+    if (st != SD_OK) return st;
+    if (cfg->rot_dim != e->c.head_dim) return fail(SD_E_INVAL, "rot_dim=%d must be head_dim=%d", cfg->rot_dim, e->c.head_dim);
+    launch_rope_table(*cfg, e->max_ctx, (float*)e->rope, (hipStream_t)stream);
+    return launched("sd_set_rope");
+}
+
+extern "C" size_t sd_kv4_page_bytes(int32_t n_layers, int32_t n_kv, int32_t head_dim, int32_t page_size)
+{
+    if (n_layers < 1 || n_kv < 1 || (head_dim != 64 && head_dim != 128) || page_size < 32 || page_size % 32) return 0;
+    return (size_t)n_layers * n_kv * page_size * (head_dim + 8);
+}
+
+static sd_status check_kv4(const sd_kv4_cache* c)
+{
+    if (!c) return fail(SD_E_INVAL, "cache is NULL");
+    if (!c->pages || !c->block_table || !c->kv_len) return fail(SD_E_INVAL, "pages, block_table or kv_len is NULL");
+    if ((uintptr_t)c->pages & 15) return fail(SD_E_INVAL, "pages must be 16-byte aligned");
+    if (!sd_kv4_page_bytes(c->n_layers, c->n_kv, c->head_dim, c->page_size))
+        return fail(SD_E_INVAL, "need n_layers, n_kv >= 1, head_dim 64 or 128 and page_size a positive multiple of 32 (got %d, %d, %d, %d)",
+                    c->n_layers, c->n_kv, c->head_dim, c->page_size);
+    if (c->n_pages < 1 || c->max_slots < 1) return fail(SD_E_INVAL, "need n_pages and max_slots >= 1");
+    if (c->max_ctx < 1 || c->max_ctx > KV4_MAX_CTX) return fail(SD_E_INVAL, "max_ctx=%d outside [1, %d]", c->max_ctx, KV4_MAX_CTX);
+    if (c->pages_per_seq < 1 || (long long)c->pages_per_seq * c->page_size < c->max_ctx)
+        return fail(SD_E_INVAL, "pages_per_seq * page_size = %lld must cover max_ctx = %d",
+                    (long long)c->pages_per_seq * c->page_size, c->max_ctx);
+    return SD_OK;
+}
+
+static sd_status check_kv4_call(const sd_kv4_cache* c, int layer, int B, int n, const void* slots)
+{
+    sd_status st = check_kv4(c);
+    if (st != SD_OK) return st;
+    if (!slots) return fail(SD_E_INVAL, "slots is NULL");
+    if (layer < 0 || layer >= c->n_layers) return fail(SD_E_INVAL, "layer=%d outside [0, %d)", layer, c->n_layers);
+    if (B < 1 || B > c->max_slots) return fail(SD_E_INVAL, "B=%d outside [1, %d]", B, c->max_slots);
+    if (n < 1 || n > c->max_ctx) return fail(SD_E_INVAL, "n=%d outside [1, max_ctx=%d]", n, c->max_ctx);
+    return SD_OK;
+}
+
+// rows at x of `heads` heads in elements of `el` bytes
+static bool rows_ok(const void* x, int64_t ld, int64_t heads, int D, int el)
+{
+    return x && !((uintptr_t)x & 15) && ld >= heads * D && ld % (16 / el) == 0 && ld <= INT_MAX;
+}
+
+static rows_t kv4_rows(const sd_kv4_cache& c, int B, int n, const int32_t* slots, const int32_t* lens)
+{
+    rows_t r = {B, n, 0, slots, c.kv_len, c.max_slots, c.max_ctx, c.flags};
+    r.lim = lens;
+    return r;
+}
+
+extern "C" sd_status sd_kv4_append(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                                   const int32_t* lens, int32_t dtype, const void* k, int64_t k_ld, const void* v,
+                                   int64_t v_ld, const void* q, int64_t q_ld, int32_t n_q, void* q_out,
+                                   const sd_rope_args* rope, void* stream)
+{
+    sd_status st = check_kv4_call(c, layer, B, n, slots);
+    if (st != SD_OK) return st;
+    if (dtype != SD_DTYPE_F32 && dtype != SD_DTYPE_BF16) return fail(SD_E_INVAL, "dtype must be F32 or BF16");
+    const int el = dtype == SD_DTYPE_F32 ? 4 : 2, D = c->head_dim;
+    if (!rows_ok(k, k_ld, c->n_kv, D, el) || !rows_ok(v, v_ld, c->n_kv, D, el))
+        return fail(SD_E_INVAL, "k and v must be 16-byte aligned, with row strides of whole 16 bytes >= n_kv*head_dim");
+    if (!q != !q_out) return fail(SD_E_INVAL, "q and q_out go together");
+    if (q && (n_q < 1 || !rows_ok(q, q_ld, n_q, D, el) || ((uintptr_t)q_out & 15)))
+        return fail(SD_E_INVAL, "n_q >= 1, q and q_out 16-byte aligned, q's row stride whole 16 bytes >= n_q*head_dim");
+    kv4_rope ro = {nullptr, 0, 0, 0};
+    if (rope && rope->rot_dim) {
+        if (rope->rot_dim < 0 || rope->rot_dim > D || rope->rot_dim % 16)
+            return fail(SD_E_INVAL, "rot_dim=%d must be a multiple of 16 in [0, head_dim]", rope->rot_dim);
+        if (!rope->table || ((uintptr_t)rope->table & 15) || rope->len < 1)
+            return fail(SD_E_INVAL, "the rotary table must be 16-byte aligned and hold at least one position");
+        ro = kv4_rope{(const float2*)rope->table, rope->len, rope->rot_dim, rope->interleaved != 0};
+    }
+    // work-groups of the launch, and the 32-bit wave numbers they are made of
+    const double waves = (double)B * (n / 8 + 2) * 2 * c->n_kv + (q ? (double)B * n * n_q / 4 + 1 : 0.0);
+    if (waves > 1e9) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
+    const rows_t r = kv4_rows(*c, B, n, slots, lens);
+    const kv4_geom g = kv4_layer(kv4_geom_of(*c), layer);
+    const hipStream_t s = (hipStream_t)stream;
+    if (dtype == SD_DTYPE_F32) {
+        const kv4_src<float> xk = {(const float*)k, (size_t)k_ld}, xv = {(const float*)v, (size_t)v_ld}, xq = {(const float*)q, (size_t)q_ld};
+        launch_kv4_append(r, g, n_q, c->n_kv, D, xk, xv, xq, (uint16_t*)q_out, ro, s);
+    } else {
+        const kv4_src<uint16_t> xk = {(const uint16_t*)k, (size_t)k_ld}, xv = {(const uint16_t*)v, (size_t)v_ld},
+                                xq = {(const uint16_t*)q, (size_t)q_ld};
+        launch_kv4_append(r, g, n_q, c->n_kv, D, xk, xv, xq, (uint16_t*)q_out, ro, s);
+    }
+    return launched("sd_kv4_append");
+}
+
+extern "C" sd_status sd_kv4_read(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                                 const int32_t* start, const int32_t* lens, void* k_out, void* v_out, void* stream)
+{
+    sd_status st = check_kv4_call(c, layer, B, n, slots);
+    if (st != SD_OK) return st;
+    if (!start || !k_out || !v_out) return fail(SD_E_INVAL, "NULL start, k_out or v_out");
+    if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return fail(SD_E_INVAL, "k_out and v_out must be 16-byte aligned");
+    if ((double)B * (n / 8 + 2) * 2 * c->n_kv > 1e9) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
+    launch_kv4_read(kv4_rows(*c, B, n, slots, lens), kv4_layer(kv4_geom_of(*c), layer), c->n_kv, c->head_dim, start,
+                    (uint16_t*)k_out, (uint16_t*)v_out, (hipStream_t)stream);
+    return launched("sd_kv4_read");
+}
+
+// The workspace of an attention call without an engine: the plan, then the partial results.
+static sd_status kv4_att_plan(const sd_kv4_cache* c, int B, int n, int n_q, att_plan* p, size_t* plan_bytes, size_t* bytes)
+{
+    if (n_q < 1 || n_q % c->n_kv) return fail(SD_E_INVAL, "n_q=%d must be a positive multiple of n_kv=%d", n_q, c->n_kv);
+    if ((double)B * n * n_q > 1e9 || (double)(n_q / c->n_kv) * n > 4e6 || B > 65535)
+        return fail(SD_E_UNSUPPORTED, "B=%d, n=%d, n_q=%d are too many for one call", B, n, n_q);
+    *p = attention_plan(B, n, n_q, c->n_kv, c->max_ctx, 0);
+    *plan_bytes = align256(attention_plan_bytes(B, c->n_kv));
+    *bytes = *plan_bytes + (p->whole ? 0 : (size_t)p->max_items * n * n_q * (c->head_dim + 4) * 4);
+    return SD_OK;
+}
+
+extern "C" size_t sd_kv4_workspace_bytes(const sd_kv4_cache* c, int32_t B, int32_t n, int32_t n_q)
+{
+    att_plan p;
+    size_t pb, bytes;
+    if (check_kv4_call(c, 0, B, n, c) != SD_OK || kv4_att_plan(c, B, n, n_q, &p, &pb, &bytes) != SD_OK) return 0;
+    return bytes;
+}
+
+extern "C" sd_status sd_kv4_attention(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                                      const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld, float scale, void* out,
+                                      int64_t out_ld, void* workspace, size_t bytes, void* stream)
+{
+    sd_status st = check_kv4_call(c, layer, B, n, slots);
+    if (st != SD_OK) return st;
+    att_plan p;
+    size_t pb, need;
+    if ((st = kv4_att_plan(c, B, n, n_q, &p, &pb, &need)) != SD_OK) return st;
+    if (!rows_ok(q, q_ld, n_q, c->head_dim, 2) || !rows_ok(out, out_ld, n_q, c->head_dim, 2))
+        return fail(SD_E_INVAL, "q and out must be 16-byte aligned, with row strides of whole 16 bytes >= n_q*head_dim");
+    if (!isfinite(scale)) return fail(SD_E_INVAL, "scale must be finite");
+    if (!workspace || ((uintptr_t)workspace & 255)) return fail(SD_E_INVAL, "workspace is NULL or not 256-byte aligned");
+    if (bytes < need) return fail(SD_E_INVAL, "workspace holds %zu bytes, need %zu", bytes, need);
+    const rows_t r = kv4_rows(*c, B, n, slots, lens);
+    const kv4_geom g = kv4_layer(kv4_geom_of(*c), layer);
+    const hipStream_t s = (hipStream_t)stream;
+    float* part = (float*)((char*)workspace + pb);
+    attention_plan_bind(p, workspace, B);
+    launch_attention_plan(r, p, s);
+    launch_kv4_attention(r, p, g, n_q, c->n_kv, c->head_dim, (const uint16_t*)q, q_ld, scale, part, out, ACT_BF16, out_ld, s);
+    if (!p.whole) launch_kv4_combine(r, p, n_q, c->n_kv, c->head_dim, part, out, ACT_BF16, out_ld, s);
+    return launched("sd_kv4_attention");
+}
+
+extern "C" sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c)
+{
+    if (!e) return fail(SD_E_INVAL, "engine is NULL");
+    sd_status st = check_kv4(c);
+    if (st != SD_OK) return st;
+    if (e->f32) return fail(SD_E_UNSUPPORTED, "the 4-bit cache needs a bf16 model");
+    const sd_model_cfg& m = e->c;
+    if (c->n_layers != m.n_layers || c->n_kv != m.n_kv || c->head_dim != m.head_dim)
+        return fail(SD_E_INVAL, "the cache's layers, KV heads and head_dim (%d, %d, %d) must be the model's (%d, %d, %d)",
+                    c->n_layers, c->n_kv, c->head_dim, m.n_layers, m.n_kv, m.head_dim);
+    if (c->max_slots < e->max_slots || c->max_ctx < e->max_ctx)
+        return fail(SD_E_INVAL, "the cache's max_slots and max_ctx (%d, %d) must cover the engine's (%d, %d)", c->max_slots,
+                    c->max_ctx, e->max_slots, e->max_ctx);
+    for (workspace* w : {&e->ws, &e->pf}) {
+        if (!w->rows || w->qrot) continue;
+        const size_t need = (size_t)w->rows * m.n_q * m.head_dim * 2;
+        if (hipMalloc(&w->qrot, need) == hipSuccess) continue;
+        (void)hipGetLastError();
+        w->qrot = nullptr;
+        return fail(SD_E_NOMEM, "workspace allocation of %zu bytes failed", need);
+    }
+    e->geo4 = kv4_geom_of(*c);
+    e->kv_len = c->kv_len;
+    e->kv4 = true;
     return SD_OK;
 }
 
@@ -550,6 +768,30 @@ static bool proj_swiglu(sd_engine e, const workspace& ws, bool draft, int layer,
                                    ws.gpart_cap, s, !e->no_dma, live) != 0;
 }
 
+// Layer l's attention over the 4-bit cache: the new rows are rotated, quantized
+// and stored first (S: the QKV projection's splits), then attended with the rest.
+// kv_only: the cache's new rows alone.
+static void attend_kv4(sd_engine e, const workspace& ws, const rows_t& r, const att_plan& plan, int l, int S, bool kv_only,
+                       act_t at, hipStream_t s)
+{
+    const sd_model_cfg& c = e->c;
+    const int D = c.head_dim, qd = c.n_q * D, kd = c.n_kv * D, ld = qd + 2 * kd;
+    auto src = [&](int col) { return kv4_src<float>{ws.qkv + col, (size_t)ld, ws.gpart + col, S, (size_t)r.B * r.n * ld}; };
+    const kv4_geom g = kv4_layer(e->geo4, l);
+    uint16_t* q = (uint16_t*)ws.qrot;
+    { tscope t(e, T_MISC, s);
+      launch_kv4_append(r, g, c.n_q, c.n_kv, D, src(qd), src(qd + kd), src(0), kv_only ? nullptr : q,
+                        kv4_rope{e->rope, e->max_ctx, D, 0}, s); }
+    if (kv_only) return;
+    { kscope t(e, r.n == 1 ? T_ATTN_D : T_ATTN_V);
+      launch_kv4_attention(r, plan, g, c.n_q, c.n_kv, D, q, qd, 1.f / sqrtf((float)D), ws.att_part, ws.att, at, qd, s, t.start,
+                           t.stop); }
+    if (!plan.whole) {
+        tscope t(e, T_MISC, s);
+        launch_kv4_combine(r, plan, c.n_q, c.n_kv, D, ws.att_part, ws.att, at, qd, s);
+    }
+}
+
 // One forward pass over B sequences x n tokens (row r = b*n + i at position
 // kv_len + off + i).  Token of row (b, i): i == 0 ? tokA[b*sA] :
 // tokB[b*sB + i - 1].  If logits != NULL, row r's logits go to logits + r*ldl;
@@ -579,18 +821,23 @@ static void forward(sd_engine e, const workspace& ws, bool draft, int B, const i
       launch_embed_rmsnorm(r, tokA, sA, tokB, sB, e->w[0], e->f32, c.hidden, c.vocab, ws.h, W(e, 0, 0), c.rms_eps, ws.a, at, plan, s); }
     for (int l = 0; l < c.n_layers; ++l) {
         { tscope t(e, pcls, s); S = proj(e, ws, draft, l, PRJ_QKV, ws.a, ws.qkv, R, qkvN, GEMM_STORE, s, r.live); }
-        if (!logits && l == c.n_layers - 1) {
-            // the rest of the last layer only feeds the logits: the new K/V rows alone
+        // (with no logits wanted, the last layer's new K/V rows alone: the rest of it only feeds the logits)
+        const bool kv_only = !logits && l == c.n_layers - 1;
+        if (e->kv4) {
+            attend_kv4(e, ws, r, plan, l, S, kv_only, at, s);
+            if (kv_only) break;
+        } else if (kv_only) {
             tscope t(e, T_MISC, s);
             launch_rope_kv(r, ws.qkv, ws.gpart, S, e->rope, c.n_q, kv, l, nullptr, s);
             break;
-        }
-        { kscope t(e, n == 1 ? T_ATTN_D : T_ATTN_V);      // RoPE and the new K/V rows are part of the attention
-          launch_attention(r, plan, qkv_src{ws.qkv, ws.gpart, S, e->rope}, ws.qrot, c.n_q, kv, l, ws.att_part, ws.att, at,
-                           s, t.start, t.stop); }
-        if (!plan.whole) {
-            tscope t(e, T_MISC, s);
-            launch_attention_combine(r, plan, c.n_q, c.n_kv, c.head_dim, ws.att_part, ws.att, at, s);
+        } else {
+            { kscope t(e, n == 1 ? T_ATTN_D : T_ATTN_V);  // RoPE and the new K/V rows are part of the attention
+              launch_attention(r, plan, qkv_src{ws.qkv, ws.gpart, S, e->rope}, (float*)ws.qrot, c.n_q, kv, l, ws.att_part,
+                               ws.att, at, s, t.start, t.stop); }
+            if (!plan.whole) {
+                tscope t(e, T_MISC, s);
+                launch_attention_combine(r, plan, c.n_q, c.n_kv, c.head_dim, ws.att_part, ws.att, at, s);
+            }
         }
         { tscope t(e, pcls, s); S = proj(e, ws, draft, l, PRJ_O, ws.att, ws.h, R, c.hidden, GEMM_ADD, s, r.live); }
         { tscope t(e, T_MISC, s); launch_add_rmsnorm(ws.h, ws.gpart, S, R, c.hidden, W(e, l, 3), e->f32, c.rms_eps, ws.a, at, r.live, s); }
@@ -796,7 +1043,10 @@ extern "C" sd_status kv_rollback(sd_engine e, int32_t B, const int32_t* slots, c
     hipStream_t s = (hipStream_t)stream;
     tscope t(e, T_MISC, s);
     launch_kv_advance(B, slots, n_emit, 0, e->kv_len, e->max_slots, e->err, s);
-    if (e->poison) {
+    if (e->poison && e->kv4) {
+        launch_kv4_poison(B, slots, e->kv_len, e->max_gamma + 1, e->geo4, e->c.n_layers, e->c.n_kv, e->c.head_dim, e->max_slots,
+                          e->max_ctx, s);
+    } else if (e->poison) {
         cache_t kv = {e->k, e->v, e->f32 ? 1 : 0, e->c.n_kv, e->c.head_dim, e->geo};
         launch_kv_poison(B, slots, e->kv_len, e->max_gamma + 1, kv, e->c.n_layers, e->max_slots, e->max_ctx, s);
     }

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/sd_api.h"
+
 // Activation element types fed to the GEMMs.
 enum act_t : int { ACT_F32 = 0, ACT_BF16 = 1, ACT_F16 = 2 };
 
@@ -69,6 +71,10 @@ struct att_plan {
 att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32);
 size_t attention_plan_bytes(int max_slots, int n_kv);
 void attention_plan_bind(att_plan& p, void* buf, int max_slots);
+
+// the plan by a kernel of its own, for attention without a forward; lengths
+// outside [0, n] raise ERR_LEN (r.err may be NULL)
+void launch_attention_plan(const rows_t& r, const att_plan& plan, hipStream_t s);
 
 // ---- model kernels (kernels_model.hip)
 // A kernel input produced by a split-K projection is given as partials P with
@@ -170,6 +176,56 @@ void launch_gemm_q4_f32(const float* A, const uint32_t* Wq, const uint16_t* Sc, 
 // packed layout of format fmt, scales Sc and (QF_W4A) zero points Z
 void launch_quant(int fmt, const void* W, int w_f32, int N, int K, uint32_t* Wq, uint16_t* Sc, uint8_t* Z,
                   hipStream_t s);
+
+// ---- 4-bit paged KV cache and rotary tables (kernels_kv4.hip); the formats are
+// those of include/sd_api.h.  In these rows_t::err may be NULL.
+struct kv4_geom {
+    uint8_t* pages;
+    int P;                     // positions per page
+    long long PS, LS, HS;      // bytes of a page, a layer's and a KV head's part of it
+    const int32_t* bt;         // device int32 [max_slots][mpp]
+    int mpp, n_pages;
+};
+inline kv4_geom kv4_geom_of(const sd_kv4_cache& c)
+{
+    const long long hs = (long long)c.page_size * (c.head_dim + 8), ls = hs * c.n_kv;
+    return kv4_geom{(uint8_t*)c.pages, c.page_size, ls * c.n_layers, ls, hs, c.block_table, c.pages_per_seq, c.n_pages};
+}
+// the geometry whose pages start at a layer
+inline kv4_geom kv4_layer(kv4_geom g, int layer)
+{
+    g.pages += layer * g.LS;
+    return g;
+}
+// rows of row stride ld (elements); floats may be S > 1 split-K partials P of
+// stride st
+template <typename T>
+struct kv4_src {
+    const T* x;
+    size_t ld;
+    const T* P = nullptr;
+    int S = 1;
+    size_t st = 0;
+};
+struct kv4_rope {
+    const float2* table;
+    int len, rot, interleaved;
+};
+void launch_rope_table(const sd_rope_cfg& c, int n_pos, float* table, hipStream_t s);
+// T: float or uint16_t (bf16 bits).  q_out NULL: K and V alone
+template <typename T>
+void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, int D, kv4_src<T> k, kv4_src<T> v, kv4_src<T> q,
+                       uint16_t* q_out, const kv4_rope& ro, hipStream_t s);
+void launch_kv4_read(const rows_t& r, const kv4_geom& g, int n_kv, int D, const int32_t* start, uint16_t* k_out,
+                     uint16_t* v_out, hipStream_t s);
+// part: attention_part_floats() floats; then the combine, unless plan.whole
+void launch_kv4_attention(const rows_t& r, const att_plan& plan, const kv4_geom& g, int n_q, int n_kv, int D, const uint16_t* q,
+                          long long q_ld, float scale, float* part, void* out, act_t out_t, long long out_ld, hipStream_t s,
+                          hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
+void launch_kv4_combine(const rows_t& r, const att_plan& plan, int n_q, int n_kv, int D, const float* part, void* out,
+                        act_t out_t, long long out_ld, hipStream_t s);
+void launch_kv4_poison(int B, const int32_t* slots, const int32_t* kv_len, int span, const kv4_geom& g, int n_layers, int n_kv,
+                       int D, int max_slots, int max_ctx, hipStream_t s);
 
 // ---- sampling and acceptance (kernels_sample.hip)
 struct rng_t { uint64_t seed, step; };

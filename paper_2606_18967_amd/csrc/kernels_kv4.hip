@@ -1,0 +1,770 @@
+// kernels_kv4.hip -- the paged KV cache in 4 bits: rotary tables, the append
+// that rotates, quantizes and stores new rows, the read-back, and the attention
+// over it.  Layout and format: sd_kv4_cache in include/sd_api.h.
+#include <hip/hip_ext.h>
+#include <math.h>
+#include "common.h"
+#include "kernels.h"
+
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// bit of element e in a code word: the elements 2i and 2i + 1 of a word w are the
+// low halves' nibbles of w >> 4i, so one AND-OR makes a pair of bf16 of them
+__device__ __forceinline__ constexpr int nib(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
+
+// tile of 32 positions of one KV head (bytes)
+constexpr int tile_bytes(int D) { return 32 * D + 256; }
+
+// first tile of (page of a slot's position pos, layer, KV head), NULL where the
+// block table has no valid page
+__device__ __forceinline__ int kv4_page(const kv4_geom& g, int slot, int lp)
+{
+    if (lp < 0 || lp >= g.mpp) return -1;
+    const int pg = g.bt[(size_t)slot * g.mpp + lp];
+    return pg >= 0 && pg < g.n_pages ? pg : -1;
+}
+
+__device__ __forceinline__ void raise(uint32_t* err, int kind)
+{
+    if (err) flag_error(err, kind);
+}
+
+// ------------------------------------------------------------------ rotary table
+// table[p][i] = mul (cos p f_i, sin p f_i) in fp64, rounded once.  A work-group
+// makes ROPE_PB positions of every pair from the sines and cosines of 8 coarse
+// and 8 fine angles a pair, cos(a + b) = cos a cos b - sin a sin b: a quarter of
+// the transcendental work, which bounds the kernel, for one more rounding in fp64.
+constexpr int ROPE_FINE = 8, ROPE_PB = ROPE_FINE * 8;
+
+__global__ void __launch_bounds__(256) k_rope_table(sd_rope_cfg c, double lo, double hi, double mul, int n_pos,
+                                                    float2* table)
+{
+    __shared__ double s_f[128];
+    __shared__ double2 s_a[8][128], s_b[ROPE_FINE][128];
+    const int np = c.rot_dim / 2, p0 = blockIdx.x * ROPE_PB;
+    for (int i = threadIdx.x; i < np; i += 256) {
+        double f = pow(c.theta, -2.0 * i / c.rot_dim);
+        if (c.scaling == SD_ROPE_LINEAR) {
+            f = f / c.factor;
+        } else if (c.scaling == SD_ROPE_LLAMA3) {
+            const double t = fmin(fmax((c.orig_ctx * f / 6.283185307179586 - c.low) / (c.high - c.low), 0.0), 1.0);
+            f = f * (t + (1.0 - t) / c.factor);
+        } else if (c.scaling == SD_ROPE_YARN) {
+            const double t = fmin(fmax((i - lo) / fmax(hi - lo, 0.001), 0.0), 1.0);
+            f = f * ((1.0 - t) + t / c.factor);
+        }
+        s_f[i] = f;
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < 16 * np; t += 256) {
+        const int k = t / np, i = t - k * np;
+        double sn, cs;
+        sincos((k < 8 ? (double)(p0 + k * ROPE_FINE) : (double)(k - 8)) * s_f[i], &sn, &cs);
+        if (k < 8) s_a[k][i] = make_double2(cs * mul, sn * mul);
+        else s_b[k - 8][i] = make_double2(cs, sn);
+    }
+    __syncthreads();
+    const int live = min(ROPE_PB, n_pos - p0);
+    for (int t = threadIdx.x; t < live * np; t += 256) {
+        const int p = t / np, i = t - p * np;
+        const double2 a = s_a[p / ROPE_FINE][i], b = s_b[p % ROPE_FINE][i];
+        table[(size_t)p0 * np + t] = make_float2((float)(a.x * b.x - a.y * b.y), (float)(a.y * b.x + a.x * b.y));
+    }
+}
+
+// ------------------------------------------------------------------ append
+// eight consecutive inputs as floats; the projection's split-K partials (S > 1)
+// are summed on read
+__device__ __forceinline__ void load8(const kv4_src<float>& x, size_t i, float (&y)[8])
+{
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (x.S > 1) {
+        add_splits2(a, b, x.P, x.S, x.st, i, i + 4);
+    } else {
+        a = *(const float4*)(x.x + i);
+        b = *(const float4*)(x.x + i + 4);
+    }
+    y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
+    y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+}
+__device__ __forceinline__ void load8(const kv4_src<uint16_t>& x, size_t i, float (&y)[8])
+{
+    const u32x4 v = *(const u32x4*)(x.x + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        y[2 * e] = __uint_as_float(v[e] << 16);
+        y[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+    }
+}
+
+// dims d0 .. d0 + 7 of the row at x, rotated by the table row rp; the products
+// and their sum in type A, rounded to fp32
+template <typename A, typename T>
+__device__ __forceinline__ void rotated8(const kv4_src<T>& x, size_t row, int d0, const float2* rp, const kv4_rope& ro,
+                                         float (&y)[8])
+{
+    load8(x, row + d0, y);
+    if (d0 >= ro.rot) return;
+    if (ro.interleaved) {
+        const float4 t0 = *(const float4*)(rp + d0 / 2), t1 = *(const float4*)(rp + d0 / 2 + 2);
+        const float2 t[4] = {{t0.x, t0.y}, {t0.z, t0.w}, {t1.x, t1.y}, {t1.z, t1.w}};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const A a = y[2 * j], b = y[2 * j + 1], c = t[j].x, s = t[j].y;
+            y[2 * j] = (float)(a * c - b * s);
+            y[2 * j + 1] = (float)(a * s + b * c);
+        }
+        return;
+    }
+    const int h = ro.rot / 2;
+    const bool first = d0 < h;
+    const int i0 = first ? d0 : d0 - h;
+    float o[8];
+    load8(x, row + (first ? d0 + h : i0), o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float4 t = *(const float4*)(rp + i0 + 2 * j);
+        const A sg = first ? (A)-1 : (A)1;
+        y[2 * j] = (float)((A)y[2 * j] * (A)t.x + sg * (A)o[2 * j] * (A)t.y);
+        y[2 * j + 1] = (float)((A)y[2 * j + 1] * (A)t.z + sg * (A)o[2 * j + 1] * (A)t.w);
+    }
+}
+
+// code of y in the group (s, z): clamp(rint((y - z)/s) + 8, 0, 15).  The quotient
+// in fp32 is within 2e-5 of the real one, so it decides unless it is near a half;
+// there (two values in a thousand) fp64 does, whose quotient can meet a half only
+// where the real one does.
+__device__ __forceinline__ uint32_t code_of(float y, float z, float s, float rs)
+{
+    const float t = (y - z) * rs;
+    float q = rintf(t);
+    if (!(fabsf(fabsf(t - q) - 0.5f) >= 1e-3f)) q = (float)rint(((double)y - (double)z) / (double)s);
+    return s > 0.f ? (uint32_t)(int)(fminf(fmaxf(q, -8.f), 7.f) + 8.f) : 8u;
+}
+
+// One wave takes the new rows among 8 consecutive positions of one KV head's K or
+// V (the words of V hold 8 positions, so a word has one writer), D/8 lanes a row;
+// further waves rotate the queries, D/8 lanes a row and head.  K is rotated in
+// fp64 so that its codes are those of the exact rotation (a value next to a border
+// moves by a whole step otherwise); its products are few against the row's bytes.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_q, int n_kv, kv4_src<T> xk, kv4_src<T> xv,
+                                                    kv4_src<T> xq, uint16_t* q_out, kv4_rope ro, int ngr, int kv_waves)
+{
+    constexpr int LPR = D / 8, RPW = WAVE / LPR, NP = 8 / RPW;     // lanes a row, rows a pass, passes of a group
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int lw = lane % LPR, lt = lane / LPR, d0 = 8 * lw;
+    if (wave >= kv_waves) {                                        // queries
+        const long long unit = (long long)(wave - kv_waves) * RPW + lt;
+        if (unit >= (long long)r.B * r.n * n_q) return;
+        const int idx = (int)(unit / n_q), h = (int)(unit - (long long)idx * n_q);
+        const int b = idx / r.n, i = idx - b * r.n;
+        if (r.lim && i >= r.lim[b]) return;
+        const size_t row = r.row0 ? r.row0[b] + i : idx;
+        const int slot = r.slots[b];
+        int pos = -1;
+        if (slot >= 0 && slot < r.max_slots) pos = r.kv_len[slot] + r.off + i;
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (pos >= 0 && pos < r.max_ctx && (ro.rot == 0 || pos < ro.len))
+            rotated8<float>(xq, row * xq.ld + (size_t)h * D, d0, ro.table + (size_t)pos * (ro.rot / 2), ro, y);
+        *(u32x4*)(q_out + (row * n_q + h) * D + d0) = (u32x4){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
+                                                             pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+        return;
+    }
+    // (sequence, group, KV head, K or V), the heads of one group side by side
+    const int u = wave % (2 * n_kv), bg = wave / (2 * n_kv), b = bg / ngr, gr = bg - b * ngr;
+    const bool is_v = u >= n_kv;
+    const int h = is_v ? u - n_kv : u;
+    const int nl = r.lim ? r.lim[b] : r.n, nlive = min(max(nl, 0), r.n);
+    const int slot = r.slots[b];
+    const bool first = gr == 0 && u == 0 && lane == 0;
+    if (first && nl != nlive) raise(r.err, ERR_LEN);
+    if (slot < 0 || slot >= r.max_slots) {
+        if (first && nlive > 0) raise(r.err, ERR_SLOT);
+        return;
+    }
+    const int base = r.kv_len[slot] + r.off;
+    const int stop = ro.rot ? min(r.max_ctx, ro.len) : r.max_ctx;  // first position without a table row or a place
+    if (first && nlive > 0 && (base < 0 || base > stop - nlive)) raise(r.err, ERR_CTX);
+    // the group's positions [pg0, pg0 + 8), the rows' [lo, hi)
+    const int pg0 = ((base < 0 ? 0 : base) & ~7) + 8 * gr, lo = max(max(base, 0), pg0);
+    const int hi = min(pg0 + 8, (int)min((long long)stop, (long long)base + nlive));
+    if (lo >= hi) return;
+    const int page = kv4_page(g, slot, pg0 / g.P);                 // a page holds whole groups
+    if (page < 0) {
+        if (u == 0 && lane == 0) raise(r.err, ERR_PAGE);
+        return;
+    }
+    const int in = pg0 % g.P, r32 = in & 31;
+    uint8_t* tile = g.pages + page * g.PS + h * g.HS + (size_t)(in >> 5) * tile_bytes(D);
+    const size_t row0 = r.row0 ? r.row0[b] : (size_t)b * r.n;
+    uint32_t vw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    uint32_t mask = 0;                                             // the new rows' nibbles of a V word
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+        if (pg0 + t >= lo && pg0 + t < hi) mask |= 0xfu << nib(t);
+#pragma unroll
+    for (int ps = 0; ps < NP; ++ps) {
+        const int t = ps * RPW + lt, pos = pg0 + t;
+        const bool live = pos >= lo && pos < hi;
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (live) {
+            const size_t row = row0 + (pos - base);
+            if (is_v) load8(xv, row * xv.ld + (size_t)h * D + d0, y);
+            else rotated8<double>(xk, row * xk.ld + (size_t)h * D, d0, ro.table + (size_t)pos * (ro.rot / 2), ro, y);
+        }
+        float mn = y[0], mx = y[0];
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            bad |= !(fabsf(y[e]) < INFINITY);
+            mn = fminf(mn, y[e]);
+            mx = fmaxf(mx, y[e]);
+        }
+        mx = bad ? INFINITY : mx;
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) {
+            mn = fminf(mn, __shfl_xor(mn, o, WAVE));
+            mx = fmaxf(mx, __shfl_xor(mx, o, WAVE));
+        }
+        bad = mx == INFINITY;
+        const uint32_t sb = f32_to_bf16((float)(((double)mx - (double)mn) / 15.0));
+        const float s = __uint_as_float(sb << 16);
+        const uint32_t zb = f32_to_bf16((float)((double)mn + 8.0 * (double)s));
+        const float z = __uint_as_float(zb << 16), rs = 1.f / s;
+        const uint32_t par = bad ? 0x7fc07fc0u : sb | zb << 16;
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t c = bad ? 8u : code_of(y[e], z, s, rs);
+            w |= c << nib(e);
+            vw[e] |= live ? c << nib(t) : 0u;
+        }
+        if (live) {
+            if (!is_v) *(uint32_t*)(tile + (r32 + t) * (D / 2) + 4 * lw) = w;
+            if (lw == 0) *(uint32_t*)(tile + 32 * D + (is_v ? 128 : 0) + 4 * (r32 + t)) = par;
+        }
+    }
+    if (!is_v) return;
+    // a word's nibbles lie in the lanes lw of every lt: each halving of the lanes
+    // leaves a lane half of the words, until lane (lt, lw) has its 8 / RPW of them
+    constexpr int WPL = 8 / RPW;
+    int w0 = 0;
+#pragma unroll
+    for (int o = 32, n = 4; n >= WPL; o >>= 1, n >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+            const uint32_t got = __shfl_xor(up ? vw[e] : vw[e + n], o, WAVE);
+            vw[e] = (up ? vw[e + n] : vw[e]) | got;
+        }
+        w0 += up ? n : 0;
+    }
+    uint32_t* dst = (uint32_t*)(tile + 16 * D) + (r32 >> 3) * D + d0 + w0;
+#pragma unroll
+    for (int e = 0; e < WPL; ++e) dst[e] = mask == 0xffffffffu ? vw[e] : (dst[e] & ~mask) | vw[e];
+}
+
+// ------------------------------------------------------------------ read
+// A thread takes 8 dims of K or V of the rows among 8 consecutive positions.
+template <int D>
+__global__ void __launch_bounds__(256) k_kv4_read(rows_t r, kv4_geom g, int n_kv, uint16_t* k_out, uint16_t* v_out,
+                                                  const int32_t* start, int ngr, long long total)
+{
+    constexpr int LPR = D / 8;
+    const long long t0 = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (t0 >= total) return;
+    const int lw = (int)(t0 % LPR);
+    const long long un = t0 / LPR;
+    const int u = (int)(un % (2 * n_kv)), bg = (int)(un / (2 * n_kv)), b = bg / ngr, gr = bg - b * ngr;
+    const bool is_v = u >= n_kv;
+    const int h = is_v ? u - n_kv : u;
+    const int nl = r.lim ? r.lim[b] : r.n, nlive = min(max(nl, 0), r.n);
+    const int slot = r.slots[b], base = start[b];
+    const bool first = gr == 0 && u == 0 && lw == 0;
+    if (first) {
+        if (nl != nlive) raise(r.err, ERR_LEN);
+        if (nlive > 0 && (slot < 0 || slot >= r.max_slots)) raise(r.err, ERR_SLOT);
+        if (nlive > 0 && (base < 0 || base > r.max_ctx - nlive)) raise(r.err, ERR_CTX);
+    }
+    // rows i of the group gr: positions 8 (base / 8 + gr) + t (base rounded down, also below 0)
+    const long long pg0 = (long long)(base & ~7) + 8 * gr;
+    int page = -1;
+    if (slot >= 0 && slot < r.max_slots && pg0 >= 0 && pg0 < r.max_ctx) {
+        page = kv4_page(g, slot, (int)(pg0 / g.P));
+        if (page < 0 && u == 0 && lw == 0 && pg0 < (long long)base + nlive) raise(r.err, ERR_PAGE);
+    }
+    uint32_t w[8], par[8];
+    if (page >= 0) {
+        const int in = (int)(pg0 % g.P), r32 = in & 31;
+        const uint8_t* tile = g.pages + page * g.PS + h * g.HS + (size_t)(in >> 5) * tile_bytes(D);
+        const uint32_t* src = is_v ? (const uint32_t*)(tile + 16 * D) + (r32 >> 3) * D + 8 * lw
+                                   : (const uint32_t*)(tile + r32 * (D / 2)) + lw;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[e] = src[is_v ? e : e * (D / 8)];
+            par[e] = ((const uint32_t*)(tile + 32 * D + (is_v ? 128 : 0)))[r32 + e];
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        const long long i = pg0 + t - base;
+        if (i < 0 || i >= nlive) continue;
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (page >= 0 && pg0 + t < r.max_ctx) {
+            const float s = __uint_as_float(par[t] << 16), z = __uint_as_float(par[t] & 0xffff0000u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t c = (is_v ? w[e] >> nib(t) : w[t] >> nib(e)) & 15u;
+                y[e] = __builtin_fmaf(s, (float)((int)c - 8), z);
+            }
+        }
+        uint16_t* o = (is_v ? v_out : k_out) + (((size_t)b * r.n + (size_t)i) * n_kv + h) * D + 8 * lw;
+        *(u32x4*)o = (u32x4){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]),
+                             pack_bf16x2(y[6], y[7])};
+    }
+}
+
+// ------------------------------------------------------------------ attention
+__device__ __forceinline__ void kv4_store4(void* out, int out_t, size_t i, float4 v)
+{
+    if (out_t == ACT_F16) {
+        const half2v a = {(_Float16)v.x, (_Float16)v.y}, b = {(_Float16)v.z, (_Float16)v.w};
+        *(uint2*)((_Float16*)out + i) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+    } else {
+        *(uint2*)((uint16_t*)out + i) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    }
+}
+
+// partial result (m, l, o[D]) of query row qrow (of QR a KV head) of an item, m
+// in base 2
+__device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, int qrow, int D)
+{
+    return (((size_t)item * n_kv + kvh) * QR + qrow) * (D + 4);
+}
+
+// Work-group (item, KV head, slice of 16 MQ query rows) covers the positions
+// [p0, p1) of its item (att_plan); its four waves take the tiles of 32 positions
+// in turn.  With q the query, c the codes of a position and (s, z) its group,
+//   score = s (q . (c - 8)) + z sum(q),
+// so the products run on the codes: the word's nibbles become the bf16 numbers
+// 128 + c by one AND-OR a pair, S^T = K Q^T with v_mfma_f32_16x16x32_bf16 starts
+// from -136 sum(q), and s and z are applied to the 16 scores of a position.
+// Row j of tile half pt is position 8 (j/4) + 4 pt + j%4, so that a lane's eight
+// scores are the positions 8 (lane/16) + 0..7 of query row lane % 16: the B operand
+// of O^T += V^T P^T, whose A operand is one word of V codes a lane (8 positions of
+// one dim).  P s goes in as bf16; 128 + c sums to P s 128 times the size of the
+// output, so a second product with the constant -136 takes the offset off within
+// the same 32 positions (in fp32 the running sum would lose 7 bits to it), and the
+// z are summed as scalars.  Neither K nor V touches LDS.
+// Online softmax in base 2, the row's reference moved only when a tile's maximum
+// exceeds it by more than 8 (exp2 terms up to 256); statistics and sums in fp32.
+template <int D, int MQ>
+__global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4_geom g, int n_q, int n_kv,
+                                                                   const uint16_t* q, long long q_ld, float cs,
+                                                                   float* part, att_plan plan, void* out, int out_t,
+                                                                   long long out_ld)
+{
+    constexpr int KW = D / 32;       // code words of a lane's part of a K row: k-steps of S
+    constexpr int NBD = D / 16;      // 16-row blocks of O^T, code words of a lane's V
+    constexpr int LDO = D + 4;       // LDS row stride of the merge
+    __shared__ __attribute__((aligned(16))) float s_o[4][16 * LDO];
+    __shared__ float s_ml[4][2][16];
+
+    const int item = blockIdx.y, kvh = blockIdx.x, zsl = blockIdx.z;
+    const att_item it = plan.item[item];
+    if (it.nch == 0) return;
+    const int row0 = __builtin_amdgcn_readfirstlane(it.row0), slot = __builtin_amdgcn_readfirstlane(it.slot);
+    const int basepos = __builtin_amdgcn_readfirstlane(it.basepos);
+    const int p0 = __builtin_amdgcn_readfirstlane(it.p0), p1 = __builtin_amdgcn_readfirstlane(it.p1);
+    const int nlive = __builtin_amdgcn_readfirstlane(it.nlive);
+    const int G = n_q / n_kv, QR = G * r.n, qbase = zsl * 16 * MQ;
+    // a slice of rows of one head that all lie past the sequence's
+    if (nlive == 0 || (qbase % r.n >= nlive && qbase % r.n + 16 * MQ <= r.n)) return;
+    if (p0 == 0 && zsl == 0 && kvh == 0 && threadIdx.x == 0) {
+        if (slot < 0 || slot >= r.max_slots) raise(r.err, ERR_SLOT);
+        else if (basepos < 0 || basepos > r.max_ctx - nlive) raise(r.err, ERR_CTX);
+    }
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int cq = lane >> 4, lr = lane & 15;
+    // the last position that a live row of the slice sees, and up to where all of its rows see everything
+    int pe = p1, all = basepos;
+    {
+        const int last = min(qbase + 16 * MQ, QR) - 1, i = last % r.n;
+        if (last - i <= qbase) {                              // rows of one head
+            pe = min(p1, basepos + min(i + 1, nlive));
+            all = basepos + qbase % r.n;
+        }
+    }
+
+    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7, and the sum of a row's values
+    bf16x8 qf[MQ][KW];
+    float qsum[MQ];
+    int lim[MQ];
+#pragma unroll
+    for (int mt = 0; mt < MQ; ++mt) {
+        const int qrow = qbase + 16 * mt + lr, h = qrow / r.n, i = qrow - h * r.n, pos = basepos + i;
+        const bool live = qrow < QR && i < nlive && pos >= 0 && pos < r.max_ctx;
+        lim[mt] = live ? pos : -1;
+        qsum[mt] = 0.f;
+        const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
+#pragma unroll
+        for (int ks = 0; ks < KW; ++ks) {
+            const u32x4 v = live ? *(const u32x4*)(qp + 8 * ks) : (u32x4){0, 0, 0, 0};
+            qf[mt][ks] = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qsum[mt] += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
+        }
+        qsum[mt] += __shfl_xor(qsum[mt], 16, WAVE);
+        qsum[mt] += __shfl_xor(qsum[mt], 32, WAVE);
+    }
+
+    float m[MQ], lsum[MQ], zsum[MQ];
+    floatx4 o[MQ][NBD];
+#pragma unroll
+    for (int mt = 0; mt < MQ; ++mt) {
+        m[mt] = -INFINITY;
+        lsum[mt] = zsum[mt] = 0.f;
+#pragma unroll
+        for (int nb = 0; nb < NBD; ++nb) o[mt][nb] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    }
+
+    struct regs {
+        alignas(16) uint32_t k[2][KW], v[NBD], kp[8], vp[8];
+        bool there;
+    };
+    const int wq0 = p0 + 32 * w, wstep = 128;
+    const int koff = (8 * (lr >> 2) + (lr & 3)) * (D / 2) + cq * (D / 8);      // + 4 pt (D/2)
+    const int voff = 16 * D + (cq * D + NBD * lr) * 4, poff = 32 * D + 32 * cq;
+    const uint8_t* head = g.pages + kvh * g.HS;
+    // the pages of the wave's tiles wq0 + k wstep, k in [kw, kw + 128), lane l
+    // holding those of kw + l and kw + 64 + l (-1: missing): one table load in 128 tiles
+    int pgw[2] = {-1, -1}, kw = -(1 << 20);
+    auto load = [&](int blk, regs& x) {
+        const int lp = __builtin_amdgcn_readfirstlane(blk / g.P);
+        const int k = __builtin_amdgcn_readfirstlane((blk - wq0) / wstep);
+        if (k < kw || k >= kw + 128) {
+            kw = k;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const int bj = wq0 + (k + 64 * hf + lane) * wstep;
+                pgw[hf] = bj < pe ? kv4_page(g, slot, bj / g.P) : -1;
+                if (pgw[hf] < 0 && bj < pe && r.err) ((volatile __attribute__((address_space(1))) uint32_t*)r.err)[ERR_PAGE] = 1u;
+            }
+        }
+        const int j = k - kw;
+        const int pa = __builtin_amdgcn_readlane(pgw[0], j & 63), pb = __builtin_amdgcn_readlane(pgw[1], j & 63);
+        const int pg = j < 64 ? pa : pb;
+        x.there = pg >= 0;
+        // no page: the first tile of the pool is read and masked, so that the loads need no branch
+        const uint8_t* t = head + (pg < 0 ? 0 : pg) * g.PS + (pg < 0 ? 0 : (blk - lp * g.P) >> 5) * (long long)tile_bytes(D);
+#pragma unroll
+        for (int pt = 0; pt < 2; ++pt) {
+            if constexpr (KW == 4) *(u32x4*)x.k[pt] = __builtin_nontemporal_load((const u32x4*)(t + koff + pt * 2 * D));
+            else *(u32x2*)x.k[pt] = __builtin_nontemporal_load((const u32x2*)(t + koff + pt * 2 * D));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+            *(u32x4*)(x.kp + e) = __builtin_nontemporal_load((const u32x4*)(t + poff + 4 * e));
+            *(u32x4*)(x.vp + e) = __builtin_nontemporal_load((const u32x4*)(t + poff + 128 + 4 * e));
+        }
+#pragma unroll
+        for (int e = 0; e < NBD; e += 4) *(u32x4*)(x.v + e) = __builtin_nontemporal_load((const u32x4*)(t + voff + 4 * e));
+    };
+    // eight codes as the bf16 numbers 128 + c
+    auto codes = [](uint32_t x) {
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = ((x >> (4 * e)) & 0x000f000fu) | 0x43004300u;
+        return __builtin_bit_cast(bf16x8, v);
+    };
+    const uint32_t off2 = 0xc308c308u;                             // (-136, -136)
+    const bf16x8 off = __builtin_bit_cast(bf16x8, (u32x4){off2, off2, off2, off2});
+    auto block = [&](int blk, const regs& x) {
+        const bool masked = !x.there || blk + 32 > pe || blk + 31 > all;
+        float ks[8], vs[8], vz[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            ks[e] = __uint_as_float(x.kp[e] << 16) * cs;
+            vs[e] = __uint_as_float(x.vp[e] << 16);
+            vz[e] = __uint_as_float(x.vp[e] & 0xffff0000u);
+        }
+        floatx4 st[MQ][2];
+#pragma unroll
+        for (int pt = 0; pt < 2; ++pt) {
+#pragma unroll
+            for (int mt = 0; mt < MQ; ++mt) {
+                const float c0 = -136.f * qsum[mt];
+                st[mt][pt] = (floatx4){c0, c0, c0, c0};
+            }
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                const bf16x8 kf = codes(x.k[pt][k]);
+#pragma unroll
+                for (int mt = 0; mt < MQ; ++mt) st[mt][pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][k], st[mt][pt], 0, 0, 0);
+            }
+        }
+        bf16x8 pf[MQ];
+#pragma unroll
+        for (int mt = 0; mt < MQ; ++mt) {
+            float sc[8];
+            const float qz = qsum[mt] * cs;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sc[e] = __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], __uint_as_float(x.kp[e] & 0xffff0000u) * qz);
+                if (masked) {
+                    const int pos = blk + 8 * cq + e;
+                    if (!x.there || pos >= pe || pos > lim[mt]) sc[e] = -INFINITY;
+                }
+            }
+            float bm = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
+            bm = fmaxf(bm, __shfl_xor(bm, 16, WAVE));
+            bm = fmaxf(bm, __shfl_xor(bm, 32, WAVE));
+            const bool need = bm > m[mt] + 8.f;
+            if (__builtin_amdgcn_ballot_w64(need)) {
+                const float mn = need ? bm : m[mt];
+                const float corr = m[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mt] - mn);
+                m[mt] = mn;
+                lsum[mt] *= corr;
+                zsum[mt] *= corr;
+#pragma unroll
+                for (int nb = 0; nb < NBD; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[mt][nb][i] *= corr;
+            }
+            const float mn = m[mt] == -INFINITY ? 0.f : m[mt];
+            float pv[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = __builtin_amdgcn_exp2f(sc[e] - mn);
+                // (a value that this row does not see, but a later one does, may be NaN)
+                const bool seen = !masked || sc[e] != -INFINITY;
+                lsum[mt] += p;
+                zsum[mt] = __builtin_fmaf(p, seen ? vz[e] : 0.f, zsum[mt]);
+                pv[e] = p * (seen ? vs[e] : 0.f);
+            }
+            pf[mt] = __builtin_bit_cast(bf16x8, (u32x4){pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]),
+                                                        pack_bf16x2(pv[4], pv[5]), pack_bf16x2(pv[6], pv[7])});
+        }
+#pragma unroll
+        for (int nb = 0; nb < NBD; ++nb) {
+            const bf16x8 vt = codes(x.v[nb]);
+#pragma unroll
+            for (int mt = 0; mt < MQ; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[mt], o[mt][nb], 0, 0, 0);
+        }
+#pragma unroll
+        for (int nb = 0; nb < NBD; ++nb)
+#pragma unroll
+            for (int mt = 0; mt < MQ; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(off, pf[mt], o[mt][nb], 0, 0, 0);
+    };
+
+    const bool usable = slot >= 0 && slot < r.max_slots;           // else p0 == p1 == 0: no tile
+    if (usable && wq0 < pe) {
+        regs x0, x1;
+        load(wq0, x0);
+        for (int blk = wq0; blk < pe; blk += 2 * wstep) {
+            load(blk + wstep, x1);
+            block(blk, x0);
+            if (blk + wstep >= pe) break;
+            load(blk + 2 * wstep, x0);
+            block(blk + wstep, x1);
+        }
+    }
+
+    // merge the four waves, 16 query rows at a time
+#pragma unroll
+    for (int mt = 0; mt < MQ; ++mt) {
+        lsum[mt] += __shfl_xor(lsum[mt], 16, WAVE);
+        lsum[mt] += __shfl_xor(lsum[mt], 32, WAVE);
+        zsum[mt] += __shfl_xor(zsum[mt], 16, WAVE);
+        zsum[mt] += __shfl_xor(zsum[mt], 32, WAVE);
+        __syncthreads();
+        if (cq == 0) { s_ml[w][0][lr] = m[mt]; s_ml[w][1][lr] = lsum[mt]; }
+        // lane (cq, lr) holds dims NBD (4 cq + i) + nb of row lr
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int nb = 0; nb < NBD; nb += 4)
+                *(float4*)(&s_o[w][lr * LDO + NBD * (4 * cq + i) + nb]) =
+                    make_float4(o[mt][nb][i] + zsum[mt], o[mt][nb + 1][i] + zsum[mt], o[mt][nb + 2][i] + zsum[mt],
+                                o[mt][nb + 3][i] + zsum[mt]);
+        __syncthreads();
+        for (int idx = threadIdx.x; idx < 16 * D / 4; idx += 256) {
+            const int qr = idx / (D / 4), d = 4 * (idx - qr * (D / 4)), qrow = qbase + 16 * mt + qr;
+            if (qrow >= QR) continue;
+            const int h = qrow / r.n, i = qrow - h * r.n;
+            if (i >= nlive) continue;
+            float mm = s_ml[0][0][qr];
+#pragma unroll
+            for (int ww = 1; ww < 4; ++ww) mm = fmaxf(mm, s_ml[ww][0][qr]);
+            float ls = 0.f;
+            float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int ww = 0; ww < 4; ++ww) {
+                const float mw = s_ml[ww][0][qr], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+                const float4 x = *(const float4*)(&s_o[ww][qr * LDO + d]);
+                ls += s_ml[ww][1][qr] * f;
+                os = make_float4(os.x + x.x * f, os.y + x.y * f, os.z + x.z * f, os.w + x.w * f);
+            }
+            if (it.nch > 1) {
+                float* pp = part + part_at(item, n_kv, kvh, QR, qrow, D);
+                if (d == 0) *(float2*)pp = make_float2(mm, ls);
+                *(float4*)(pp + 4 + d) = os;
+                continue;
+            }
+            const bool none = ls == 0.f || basepos + i < 0 || basepos + i >= r.max_ctx;
+            const size_t oi = (size_t)(row0 + i) * out_ld + (size_t)(kvh * G + h) * D + d;
+            const float4 v = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(os.x / ls, os.y / ls, os.z / ls, os.w / ls);
+            kv4_store4(out, out_t, oi, v);
+        }
+    }
+}
+
+// The items of a sequence merged in order; a work-group takes one row, its
+// threads the heads' dims four at a time.
+__global__ void __launch_bounds__(256) k_kv4_combine(rows_t r, att_plan plan, int n_q, int n_kv, int D, const float* part,
+                                                     void* out, int out_t, long long out_ld)
+{
+    const int idx = blockIdx.x, b = idx / r.n, i = idx - b * r.n;
+    if (r.lim && i >= r.lim[b]) return;
+    const size_t row = r.row0 ? r.row0[b] + i : idx;
+    const int2 sq = plan.seq[b];
+    const int nch = sq.y;
+    if (nch <= 1) return;                                         // the attention wrote the output
+    const int G = n_q / n_kv, QR = G * r.n, D4 = D / 4;
+    const int t = blockIdx.y * 256 + threadIdx.x;
+    if (t >= n_q * D4) return;
+    const int hq = t / D4, d = 4 * (t - hq * D4), kvh = hq / G;
+    const float* pp = part + part_at(sq.x, n_kv, kvh, QR, (hq - kvh * G) * r.n + i, D);
+    const size_t st = (size_t)n_kv * QR * (D + 4);                // to the next item
+    constexpr int CB = 8;                                         // items whose loads go out together
+    float mm = -INFINITY, ls = 0.f;
+    float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; c0 < nch; c0 += CB) {
+        float2 ml[CB];
+        float4 x[CB];
+#pragma unroll
+        for (int u = 0; u < CB; ++u) {
+            const float* pc = pp + min(c0 + u, nch - 1) * st;
+            ml[u] = *(const float2*)pc;
+            x[u] = *(const float4*)(pc + 4 + d);
+        }
+        float bm = mm;
+#pragma unroll
+        for (int u = 0; u < CB; ++u) bm = fmaxf(bm, ml[u].x);
+        const float f0 = mm == bm ? 1.f : __builtin_amdgcn_exp2f(mm - bm);
+        ls *= f0;
+        os = make_float4(os.x * f0, os.y * f0, os.z * f0, os.w * f0);
+        mm = bm;
+#pragma unroll
+        for (int u = 0; u < CB; ++u) {
+            if (c0 + u >= nch) break;
+            const float f = ml[u].x == mm ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - mm);
+            ls += ml[u].y * f;
+            os = make_float4(os.x + x[u].x * f, os.y + x[u].y * f, os.z + x[u].z * f, os.w + x[u].w * f);
+        }
+    }
+    const float4 v = ls == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(os.x / ls, os.y / ls, os.z / ls, os.w / ls);
+    kv4_store4(out, out_t, row * out_ld + (size_t)hq * D + d, v);
+}
+
+// NaN groups in the positions [kv_len, kv_len + span) of every layer and KV head
+__global__ void __launch_bounds__(256) k_kv4_poison(const int32_t* slots, const int32_t* kv_len, int span, kv4_geom g,
+                                                    int n_layers, int n_kv, int D, int max_slots, int max_ctx)
+{
+    const int s = slots[blockIdx.x];
+    if (s < 0 || s >= max_slots) return;
+    const int lo = max(kv_len[s], 0), per = max((int)min((long long)lo + span, (long long)max_ctx) - lo, 0);
+    const long long total = (long long)n_layers * n_kv * per;
+    for (long long t = threadIdx.x; t < total; t += 256) {
+        const int lh = (int)(t / per), l = lh / n_kv, h = lh - l * n_kv, p = lo + (int)(t - (long long)lh * per);
+        const int pg = kv4_page(g, s, p / g.P);
+        if (pg < 0) continue;
+        uint8_t* tile = g.pages + pg * g.PS + l * g.LS + h * g.HS + (size_t)((p % g.P) >> 5) * tile_bytes(D);
+        ((uint32_t*)(tile + 32 * D))[p & 31] = 0x7fc07fc0u;
+        ((uint32_t*)(tile + 32 * D + 128))[p & 31] = 0x7fc07fc0u;
+    }
+}
+
+}  // namespace
+
+// ======================================================================= launchers
+void launch_rope_table(const sd_rope_cfg& c, int n_pos, float* table, hipStream_t s)
+{
+    double lo = 0, hi = 0, mul = 1;
+    if (c.scaling == SD_ROPE_YARN) {
+        auto at = [&](double turns) { return c.rot_dim * log(c.orig_ctx / (6.283185307179586 * turns)) / (2 * log(c.theta)); };
+        lo = fmax(floor(at(c.high)), 0.0);
+        hi = fmin(ceil(at(c.low)), c.rot_dim - 1.0);
+        mul = c.attn_factor > 0 ? c.attn_factor : 0.1 * log(c.factor) + 1.0;
+    }
+    k_rope_table<<<(n_pos + ROPE_PB - 1) / ROPE_PB, 256, 0, s>>>(c, lo, hi, mul, n_pos, (float2*)table);
+}
+
+template <typename T>
+void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, int D, kv4_src<T> k, kv4_src<T> v, kv4_src<T> q,
+                       uint16_t* q_out, const kv4_rope& ro, hipStream_t s)
+{
+    const int ngr = (r.n + 14) / 8;                               // groups of 8 that n rows can touch
+    const long long kvw = (long long)r.B * ngr * 2 * n_kv, rpw = 512 / D;
+    const long long qw = q_out ? ((long long)r.B * r.n * n_q + rpw - 1) / rpw : 0;
+    const unsigned blocks = (unsigned)((kvw + qw + 3) / 4);
+    if (D == 128) k_kv4_append<T, 128><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, (int)kvw);
+    else k_kv4_append<T, 64><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, (int)kvw);
+}
+template void launch_kv4_append<float>(const rows_t&, const kv4_geom&, int, int, int, kv4_src<float>, kv4_src<float>,
+                                       kv4_src<float>, uint16_t*, const kv4_rope&, hipStream_t);
+template void launch_kv4_append<uint16_t>(const rows_t&, const kv4_geom&, int, int, int, kv4_src<uint16_t>, kv4_src<uint16_t>,
+                                          kv4_src<uint16_t>, uint16_t*, const kv4_rope&, hipStream_t);
+
+void launch_kv4_read(const rows_t& r, const kv4_geom& g, int n_kv, int D, const int32_t* start, uint16_t* k_out,
+                     uint16_t* v_out, hipStream_t s)
+{
+    const int ngr = (r.n + 14) / 8;
+    const long long total = (long long)r.B * ngr * 2 * n_kv * (D / 8);
+    const unsigned blocks = (unsigned)((total + 255) / 256);
+    if (D == 128) k_kv4_read<128><<<blocks, 256, 0, s>>>(r, g, n_kv, k_out, v_out, start, ngr, total);
+    else k_kv4_read<64><<<blocks, 256, 0, s>>>(r, g, n_kv, k_out, v_out, start, ngr, total);
+}
+
+template <int D>
+static void kv4_attn_d(const rows_t& r, const att_plan& pl, const kv4_geom& g, int n_q, int n_kv, const uint16_t* q,
+                       long long q_ld, float cs, float* part, void* out, act_t out_t, long long out_ld, hipStream_t s,
+                       hipEvent_t ev0, hipEvent_t ev1)
+{
+    auto go = [&](auto kern) {
+        const dim3 grid(n_kv, pl.max_items, pl.zs), block(256);
+        if (ev0) hipExtLaunchKernelGGL(kern, grid, block, 0, s, ev0, ev1, 0, r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
+        else kern<<<grid, block, 0, s>>>(r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
+    };
+    switch (pl.mq) {
+        case 1: go(k_kv4_attn<D, 1>); break;
+        case 2: go(k_kv4_attn<D, 2>); break;
+        case 3: go(k_kv4_attn<D, 3>); break;
+        default: go(k_kv4_attn<D, 4>); break;
+    }
+}
+
+void launch_kv4_attention(const rows_t& r, const att_plan& pl, const kv4_geom& g, int n_q, int n_kv, int D, const uint16_t* q,
+                          long long q_ld, float scale, float* part, void* out, act_t out_t, long long out_ld, hipStream_t s,
+                          hipEvent_t ev0, hipEvent_t ev1)
+{
+    const float cs = (float)(scale * 1.4426950408889634);
+    if (D == 128) kv4_attn_d<128>(r, pl, g, n_q, n_kv, q, q_ld, cs, part, out, out_t, out_ld, s, ev0, ev1);
+    else kv4_attn_d<64>(r, pl, g, n_q, n_kv, q, q_ld, cs, part, out, out_t, out_ld, s, ev0, ev1);
+}
+
+void launch_kv4_combine(const rows_t& r, const att_plan& pl, int n_q, int n_kv, int D, const float* part, void* out,
+                        act_t out_t, long long out_ld, hipStream_t s)
+{
+    k_kv4_combine<<<dim3(r.B * r.n, (n_q * D / 4 + 255) / 256), 256, 0, s>>>(r, pl, n_q, n_kv, D, part, out, (int)out_t, out_ld);
+}
+
+void launch_kv4_poison(int B, const int32_t* slots, const int32_t* kv_len, int span, const kv4_geom& g, int n_layers, int n_kv,
+                       int D, int max_slots, int max_ctx, hipStream_t s)
+{
+    k_kv4_poison<<<B, 256, 0, s>>>(slots, kv_len, span, g, n_layers, n_kv, D, max_slots, max_ctx);
+}

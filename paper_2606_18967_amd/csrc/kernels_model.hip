@@ -205,6 +205,14 @@ __device__ void make_att_plan(const rows_t& r, const att_plan& pl)
     for (int i = s_items + tid; i < pl.max_items; i += nt) pl.item[i] = none;
 }
 
+__global__ void __launch_bounds__(1024) k_attn_plan(rows_t r, att_plan plan)
+{
+    if (r.lim && r.err)
+        for (int b = threadIdx.x; b < r.B; b += blockDim.x)
+            if (r.lim[b] < 0 || r.lim[b] > r.n) flag_error(r.err, ERR_LEN);
+    make_att_plan(r, plan);
+}
+
 // h[row] = E[token(row)];  out[row] = RMSNorm(h[row]) * gain.  One more
 // work-group than rows, the first to start (its serial chain is the longest),
 // makes the forward's attention plan.
@@ -1246,6 +1254,11 @@ att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32
     return p;
 }
 
+void launch_attention_plan(const rows_t& r, const att_plan& plan, hipStream_t s)
+{
+    k_attn_plan<<<1, r.B > 256 ? 1024 : 256, 0, s>>>(r, plan);
+}
+
 // seq [max_slots], item [max(max_slots, ATT_TARGET_WGS / n_kv)]
 static size_t plan_seq_bytes(int max_slots) { return ((size_t)max_slots * sizeof(int2) + 63) & ~(size_t)63; }
 
@@ -1262,12 +1275,13 @@ void attention_plan_bind(att_plan& p, void* buf, int max_slots)
 }
 
 // only items of a sequence cut in several are stored, and then there are at most `target` of them
+// (a row's sums and two statistics, with the 4-bit cache at a stride of head_dim + 4)
 size_t attention_part_floats(int R, int n_q, int n_kv, int head_dim, int kv_f32)
 {
     size_t most = 0;
     for (int n = 1; n <= R; ++n) {
         const att_plan p = attention_plan(1, n, n_q, n_kv, 1 << 30, kv_f32);
-        const size_t f = p.whole ? 0 : (size_t)p.target * n * n_q * (head_dim + 2);
+        const size_t f = p.whole ? 0 : (size_t)p.target * n * n_q * (head_dim + 4);
         most = f > most ? f : most;
     }
     return most > 64 ? most : 64;

@@ -35,6 +35,8 @@ API_SYMBOLS = (
     "sd_accept", "kv_rollback", "sd_ar_step", "sd_sync", "sd_set_debug", "sd_cost_init",
     "sd_cost_times", "sd_toggle", "sd_gamma_init", "sd_gamma_next", "sd_tau_from_alpha",
     "sd_alpha_from_tau", "sd_timing", "sd_timing_read", "sd_dense_gemm_bf16", "sd_accept_noalloc",
+    "sd_rope_table", "sd_set_rope", "sd_kv4_page_bytes", "sd_kv4_append", "sd_kv4_read", "sd_kv4_workspace_bytes",
+    "sd_kv4_attention", "sd_bind_kv4",
 )
 
 # kernel classes of sd_timing_read
@@ -73,8 +75,25 @@ class GammaCtl(C.Structure):
                 ("hist", C.c_double * 64)]
 
 
+class RopeCfg(C.Structure):
+    _fields_ = [("theta", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("attn_factor", C.c_double), ("rot_dim", C.c_int32), ("scaling", C.c_int32), ("orig_ctx", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class RopeArgs(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("len", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class KV4Struct(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("block_table", C.c_void_p), ("kv_len", C.c_void_p), ("flags", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("pages_per_seq", C.c_int32),
+                ("n_layers", C.c_int32), ("n_kv", C.c_int32), ("head_dim", C.c_int32), ("max_slots", C.c_int32),
+                ("max_ctx", C.c_int32)]
+
+
 _lib = None
-_P, _i32, _f, _d, _sz = C.c_void_p, C.c_int32, C.c_float, C.c_double, C.c_size_t
+_P, _i32, _i64, _f, _d, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_double, C.c_size_t
 
 
 def lib():
@@ -116,6 +135,14 @@ def lib():
             "sd_toggle": (_i32, [_P, _i32, _d, _d, _i32, _d, _P]),
             "sd_gamma_init": (_i32, [_P, _P, _i32, _i32, _d, _d]),
             "sd_gamma_next": (_i32, [_P, _d, _P]),
+            "sd_rope_table": (_i32, [_P, _i32, _P, _P]),
+            "sd_set_rope": (_i32, [_P, _P, _P]),
+            "sd_kv4_page_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+            "sd_kv4_append": (_i32, [_P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _P, _i64, _P, _i64, _i32, _P, _P, _P]),
+            "sd_kv4_read": (_i32, [_P, _i32, _i32, _i32, _P, _P, _P, _P, _P, _P]),
+            "sd_kv4_workspace_bytes": (_sz, [_P, _i32, _i32, _i32]),
+            "sd_kv4_attention": (_i32, [_P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _f, _P, _i64, _P, _sz, _P]),
+            "sd_bind_kv4": (_i32, [_P, _P]),
             "sd_tau_from_alpha": (_d, [_d, _i32]),
             "sd_alpha_from_tau": (_d, [_d, _i32]),
         }
@@ -241,6 +268,24 @@ class Engine:
                                       _dev(block_table, "block_table", torch.int32, (self.max_slots, pps), self.device),
                                       pps, _dev(kv_len, "kv_len", torch.int32, (self.max_slots,), self.device)))
         self._keep_kv = (k, v, block_table, kv_len)
+
+    def alloc_kv4(self, n_pages: int, page_size: int, block_table: torch.Tensor) -> "KV4Cache":
+        """A 4-bit cache of n_pages pages for this model (KV4Cache); block_table as bind_kv_paged."""
+        c = self.cfg
+        pages = kv4_pages(n_pages, c["n_layers"], c["n_kv"], c["head_dim"], page_size, self.device)
+        return KV4Cache(pages, block_table, torch.zeros(self.max_slots, dtype=torch.int32, device=self.device),
+                        self.max_ctx)
+
+    def bind_kv4(self, cache: "KV4Cache"):
+        """Prefill, draft, verify, AR step and rollback run on the 4-bit cache from here on."""
+        if cache.device != self.device:
+            raise ValueError(f"cache on {cache.device}, engine is on {self.device}")
+        _check(lib().sd_bind_kv4(self.h, C.byref(cache.c)))
+        self._keep_kv = cache
+
+    def set_rope(self, rope: "RopeConfig"):
+        """Replaces the engine's rotary table (on the current stream) for every later call."""
+        _check(lib().sd_set_rope(self.h, C.byref(rope.c), _stream()))
 
     def drafter_bytes(self, fmt: str = "w4") -> int:
         return int(lib().sd_drafter_bytes_fmt(C.byref(self.c), DRAFT_FORMATS[fmt]))
@@ -430,6 +475,166 @@ def accept_noalloc(slots, kv_len, draft_tok, q_logits, q_stats, p_logits, gamma,
                                    gamma, T, Rng(seed, step),
                                    _dev(out_tok, "out_tok", torch.int32, (B, gamma + 1), dev),
                                    _dev(n_emit, "n_emit", torch.int32, (B,), dev), nt, _stream()))
+
+
+# ------------------------------------------------- rotary tables, 4-bit KV cache
+ROPE_SCALINGS = {"none": 0, "linear": 1, "llama3": 2, "yarn": 3}
+
+
+class RopeConfig:
+    """Rotary positions: base theta, rotated dims of a head, and the scaling for long contexts ("none",
+    "linear", "llama3" with low/high frequency factors, "yarn" with low/high turns; sd_rope_cfg)."""
+
+    def __init__(self, theta: float, rot_dim: int, scaling: str = "none", factor: float = 1.0, low: float = 0.0,
+                 high: float = 0.0, orig_ctx: int = 0, attn_factor: float = 0.0):
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"scaling: expected one of {sorted(ROPE_SCALINGS)}, got {scaling!r}")
+        self.rot_dim = rot_dim
+        self.c = RopeCfg(theta, factor, low, high, attn_factor, rot_dim, ROPE_SCALINGS[scaling], orig_ctx, 0)
+
+
+def rope_table(rope: RopeConfig, n_pos: int, out: torch.Tensor | None = None) -> torch.Tensor:
+    """(cos, sin) of the positions [0, n_pos): fp32 [n_pos][rot_dim / 2][2] on the current device."""
+    if out is None:
+        out = torch.empty((n_pos, rope.rot_dim // 2, 2), dtype=torch.float32, device="cuda")
+    _check(lib().sd_rope_table(C.byref(rope.c), n_pos,
+                               _dev(out, "out", torch.float32, (n_pos, rope.rot_dim // 2, 2), _current()), _stream()))
+    return out
+
+
+def _current():
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def kv4_pages(n_pages: int, n_layers: int, n_kv: int, head_dim: int, page_size: int, device="cuda") -> torch.Tensor:
+    """Zeroed pages of a 4-bit cache: uint8 [n_pages][n_layers][n_kv][page_size / 32][tile bytes]."""
+    if not lib().sd_kv4_page_bytes(n_layers, n_kv, head_dim, page_size):
+        raise ValueError("need n_layers, n_kv >= 1, head_dim 64 or 128 and page_size a positive multiple of 32")
+    return torch.zeros((n_pages, n_layers, n_kv, page_size // 32, 32 * (head_dim + 8)), dtype=torch.uint8, device=device)
+
+
+class KV4Cache:
+    """A paged KV cache in 4 bits (sd_kv4_cache): pages from kv4_pages, an int32 block table
+    [max_slots][pages_per_seq] of page indices and the int32 lengths kv_len [max_slots], all caller-owned.  What
+    calls without an engine find out of range on the device is collected in `flags`; check() reports it."""
+
+    def __init__(self, pages: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, max_ctx: int):
+        if pages.dim() != 5 or block_table.dim() != 2 or kv_len.dim() != 1:
+            raise ValueError("expected pages [n_pages][layers][n_kv][tiles][bytes], block_table [slots][pages], kv_len [slots]")
+        n_pages, n_layers, n_kv, tiles, tile = pages.shape
+        head_dim, slots = tile // 32 - 8, kv_len.shape[0]
+        if tile % 32 or head_dim not in (64, 128):
+            raise ValueError(f"pages: tiles of {tile} bytes, expected 2304 (head_dim 64) or 4352 (128)")
+        self.device = pages.device
+        self.n_layers, self.n_kv, self.head_dim, self.page_size = n_layers, n_kv, head_dim, 32 * tiles
+        self.max_slots, self.max_ctx = slots, max_ctx
+        if block_table.shape[1] * self.page_size < max_ctx:
+            raise ValueError(f"block_table: {block_table.shape[1]} pages of {self.page_size} do not cover max_ctx={max_ctx}")
+        ptrs = (_dev(pages, "pages", torch.uint8), _dev(block_table, "block_table", torch.int32, (slots, block_table.shape[1]), self.device),
+                _dev(kv_len, "kv_len", torch.int32, None, self.device))
+        self.pages, self.block_table, self.kv_len = pages, block_table, kv_len
+        self.flags = torch.zeros(5, dtype=torch.int32, device=self.device)
+        self.c = KV4Struct(*ptrs, C.c_void_p(self.flags.data_ptr()), n_pages, self.page_size, block_table.shape[1],
+                           n_layers, n_kv, head_dim, slots, max_ctx)
+
+    def check(self):
+        """Waits for the current stream and raises what calls found out of range since the last check."""
+        f = self.flags.tolist()
+        if not any(f):
+            return
+        self.flags.zero_()
+        what = ("slot index outside [0, max_slots)", None, "position outside [0, max_ctx) or the rotary table",
+                "block-table entry outside [0, n_pages)", "row count outside [0, n]")
+        raise SDError(SD_E_INVAL, "device: " + "; ".join(w for w, x in zip(what, f) if x and w))
+
+
+def _rows(t: torch.Tensor, name: str, dtype, shape, dev):
+    """Rows [B][n][heads][head_dim] at a common row stride: the pointer and the stride in elements."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != dev:
+        raise ValueError(f"{name}: expected a tensor on {dev}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    B, n, heads, D = shape
+    st = t.stride()
+    ld = st[1] if n > 1 else st[0] if B > 1 else heads * D
+    if st[3] != 1 or (heads > 1 and st[2] != D) or (n > 1 and B > 1 and st[0] != n * ld) or ld < heads * D:
+        raise ValueError(f"{name}: rows must lie at one stride with contiguous heads, got strides {st}")
+    return t.data_ptr(), ld
+
+
+def _kv4_args(cache: KV4Cache, slots, lens):
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"cache on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    B = slots.numel()
+    return B, _dev(slots, "slots", torch.int32, (B,), cache.device), \
+        _dev(lens, "lens", torch.int32, (B,), cache.device) if lens is not None else None
+
+
+def kv4_append(cache: KV4Cache, layer: int, slots, k, v, q=None, q_out=None, rope=None, layout: str = "half", lens=None):
+    """Stores rows k, v [B][n][n_kv][head_dim] (bf16 or fp32, strided rows allowed) of sequences slots[b] at
+    positions kv_len + i of a layer, k rotated by the table `rope` (rope_table; None: not rotated) in pairs of
+    "half" or "interleaved" layout, and rotates q [B][n][n_q][head_dim] into q_out (bf16).  lens [B]: rows of
+    each sequence.  kv_len is not changed."""
+    B, sp, lp = _kv4_args(cache, slots, lens)
+    dev, D, n = cache.device, cache.head_dim, k.shape[1]
+    if k.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"k: expected bfloat16 or float32, got {k.dtype}")
+    if layout not in ("half", "interleaved"):
+        raise ValueError(f"layout: expected 'half' or 'interleaved', got {layout!r}")
+    shape = (B, n, cache.n_kv, D)
+    (kp, k_ld), (vp, v_ld) = _rows(k, "k", k.dtype, shape, dev), _rows(v, "v", k.dtype, shape, dev)
+    qp, q_ld, n_q, op = None, 0, 0, None
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        n_q = q.shape[2]
+        qp, q_ld = _rows(q, "q", k.dtype, (B, n, n_q, D), dev)
+        op = _dev(q_out, "q_out", torch.bfloat16, (B, n, n_q, D), dev)
+    ra = RopeArgs(None, 0, 0, 0)
+    if rope is not None and rope.shape[1]:
+        ra = RopeArgs(_dev(rope, "rope", torch.float32, (rope.shape[0], rope.shape[1], 2), dev), rope.shape[0],
+                      2 * rope.shape[1], layout == "interleaved")
+    _check(lib().sd_kv4_append(C.byref(cache.c), layer, B, n, sp, lp,
+                               SD_DTYPE_BF16 if k.dtype == torch.bfloat16 else SD_DTYPE_F32, kp, k_ld, vp, v_ld, qp, q_ld,
+                               n_q, op, C.byref(ra), _stream()))
+
+
+def kv4_read(cache: KV4Cache, layer: int, slots, start, k_out, v_out, lens=None):
+    """The stored values of positions start[b] + i of a layer into k_out, v_out (bf16 [B][n][n_kv][head_dim])."""
+    B, sp, lp = _kv4_args(cache, slots, lens)
+    n = k_out.shape[1]
+    shape = (B, n, cache.n_kv, cache.head_dim)
+    _check(lib().sd_kv4_read(C.byref(cache.c), layer, B, n, sp, _dev(start, "start", torch.int32, (B,), cache.device), lp,
+                             _dev(k_out, "k_out", torch.bfloat16, shape, cache.device),
+                             _dev(v_out, "v_out", torch.bfloat16, shape, cache.device), _stream()))
+
+
+def kv4_attention(cache: KV4Cache, layer: int, slots, q, out=None, scale: float | None = None, lens=None, workspace=None):
+    """Attention of rows q [B][n][n_q][head_dim] (bf16, rotated) at positions kv_len + i over the positions up to
+    each row's own (append them first) into out (bf16, same shape); scale defaults to 1/sqrt(head_dim).  workspace:
+    a uint8 tensor of kv4_workspace_bytes, for callers that keep one (not for calls that may overlap)."""
+    B, sp, lp = _kv4_args(cache, slots, lens)
+    shape = (B, q.shape[1], q.shape[2], cache.head_dim)
+    qp, q_ld = _rows(q, "q", torch.bfloat16, shape, cache.device)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+    op, o_ld = _rows(out, "out", torch.bfloat16, shape, cache.device)
+    if workspace is None:
+        workspace = torch.empty(kv4_workspace_bytes(cache, B, shape[1], shape[2]), dtype=torch.uint8, device=cache.device)
+    _check(lib().sd_kv4_attention(C.byref(cache.c), layer, B, shape[1], sp, lp, shape[2], qp, q_ld,
+                                  cache.head_dim ** -0.5 if scale is None else scale, op, o_ld,
+                                  _dev(workspace, "workspace", torch.uint8, None, cache.device), workspace.numel(), _stream()))
+    return out
+
+
+def kv4_workspace_bytes(cache: KV4Cache, B: int, n: int, n_q: int) -> int:
+    """Bytes of kv4_attention's workspace."""
+    nb = int(lib().sd_kv4_workspace_bytes(C.byref(cache.c), B, n, n_q))
+    if not nb:
+        raise SDError(SD_E_INVAL, lib().sd_last_error().decode(errors="replace"))
+    return nb
 
 
 def dense_gemm_bf16(A: torch.Tensor, W: torch.Tensor, out: torch.Tensor):
