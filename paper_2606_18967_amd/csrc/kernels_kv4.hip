@@ -3,6 +3,9 @@
 // over it.  Layout and format: sd_kv4_cache in include/sd_api.h.
 #include <hip/hip_ext.h>
 #include <math.h>
+
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -339,8 +342,7 @@ __device__ __forceinline__ void kv4_store4(void* out, int out_t, size_t i, float
     }
 }
 
-// partial result (m, l, o[D]) of query row qrow (of QR a KV head) of an item, m
-// in base 2
+// partial result (ref, l, o[D]) of query row qrow (of QR a KV head) of an item
 __device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, int qrow, int D)
 {
     return (((size_t)item * n_kv + kvh) * QR + qrow) * (D + 4);
@@ -349,20 +351,43 @@ __device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, i
 // Work-group (item, KV head, slice of 16 MQ query rows) covers the positions
 // [p0, p1) of its item (att_plan); its four waves take the tiles of 32 positions
 // in turn.  With q the query, c the codes of a position and (s, z) its group,
-//   score = s (q . (c - 8)) + z sum(q),
-// so the products run on the codes: the word's nibbles become the bf16 numbers
-// 128 + c by one AND-OR a pair, S^T = K Q^T with v_mfma_f32_16x16x32_bf16 starts
-// from -136 sum(q), and s and z are applied to the 16 scores of a position.
-// Row j of tile half pt is position 8 (j/4) + 4 pt + j%4, so that a lane's eight
-// scores are the positions 8 (lane/16) + 0..7 of query row lane % 16: the B operand
-// of O^T += V^T P^T, whose A operand is one word of V codes a lane (8 positions of
-// one dim).  P s goes in as bf16; 128 + c sums to P s 128 times the size of the
-// output, so a second product with the constant -136 takes the offset off within
-// the same 32 positions (in fp32 the running sum would lose 7 bits to it), and the
-// z are summed as scalars.  Neither K nor V touches LDS.
-// Online softmax in base 2, the row's reference moved only when a tile's maximum
-// exceeds it by more than 8 (exp2 terms up to 256); statistics and sums in fp32.
-template <int D, int MQ>
+//   score = s (q . c) + (z - 8 s) sum(q),   out = sum (P s) (c - 8) + sum P z,
+// so the products run on the codes themselves.  A nibble under a mask is an fp16
+// number as it stands: c 2^-24 in bits 0..3 (denormal, which the matrix cores
+// take), c 2^-20 in bits 4..7; a word's eight codes are four ANDs and a shift,
+// and the other operand's elements 2, 3, 6 and 7 carry the factor 1/16.
+//   S^T = K Q^T with v_mfma_f32_16x16x32_f16, the queries scaled by a power of
+// two a row (bf16 values keep all their bits).  Row j of tile half pt is position
+// 8 (j/4) + 4 pt + j%4, so that a lane's eight scores are the positions
+// 8 (lane/16) + 0..7 of query row lane % 16: the B operand of O^T += V^T P^T, whose
+// A operand is one word of V codes a lane (8 positions of one dim).  P s goes in
+// as fp16 (2^-11, an eighth of the output's own rounding), and one more product
+// with codes of 8 sums what the centre takes off again.  Neither K nor V touches
+// LDS.
+// Online softmax in base 2.  A row's reference ref bounds the products' operand:
+// P s = exp2(score - ref) s <= 2^15; it moves, with all sums, only where a tile
+// would exceed that, to where the tile's largest P s is 2^7, so small terms are
+// lost at 2^-24 of a row's largest and not earlier.  (P alone stays below 2^100 for
+// rows of s = 0.)  Sums and statistics in fp32.
+constexpr float KV4_REF0 = -1e30f;     // the reference of a row that has seen no position
+
+// 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
+// `lds` on; non-temporal.  The compiler's wait counts do not see them.
+__device__ __forceinline__ void tile_dma16(const void* base, uint32_t off, uint32_t lds)
+{
+    asm volatile("global_load_lds_dwordx4 %0, %1 nt" : : "v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void tile_dma4(const void* base, uint32_t off, uint32_t lds)
+{
+    asm volatile("global_load_lds_dword %0, %1 nt" : : "v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_tiles()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+template <int D, int MQ, int RING>
 __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4_geom g, int n_q, int n_kv,
                                                                    const uint16_t* q, long long q_ld, float cs,
                                                                    float* part, att_plan plan, void* out, int out_t,
@@ -371,8 +396,12 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     constexpr int KW = D / 32;       // code words of a lane's part of a K row: k-steps of S
     constexpr int NBD = D / 16;      // 16-row blocks of O^T, code words of a lane's V
     constexpr int LDO = D + 4;       // LDS row stride of the merge
-    __shared__ __attribute__((aligned(16))) float s_o[4][16 * LDO];
+    constexpr int TB = tile_bytes(D), PIECES = D / 32 + 1;
+    constexpr int BUF = 4 * RING * TB > 4 * 16 * LDO * 4 ? 4 * RING * TB : 4 * 16 * LDO * 4;
+    static_assert(PIECES * (RING - 1) < 64, "vmcnt range");
+    __shared__ __attribute__((aligned(1024))) uint8_t s_buf[BUF];  // the waves' rings, then the merge
     __shared__ float s_ml[4][2][16];
+    float (*s_o)[16 * LDO] = (float (*)[16 * LDO])s_buf;
 
     const int item = blockIdx.y, kvh = blockIdx.x, zsl = blockIdx.z;
     const att_item it = plan.item[item];
@@ -400,179 +429,238 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         }
     }
 
-    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7, and the sum of a row's values
-    bf16x8 qf[MQ][KW];
-    float qsum[MQ];
+    // tile i of the wave is at positions wq0 + 128 i
+    const int wq0 = p0 + 32 * w;
+    const bool usable = slot >= 0 && slot < r.max_slots;           // else p0 == p1 == 0: no tile
+    const int nt = usable && wq0 < pe ? (pe - wq0 + 127) >> 7 : 0;
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_buf + w * (RING * TB);
+    const uint8_t* head = g.pages + kvh * g.HS;
+    // a lane's pieces of a tile: K row 8 (lr/4) + 4 pt + lr%4, words (D/32) cq + 0..; V group cq, words NBD lr + 0..
+    uint32_t src[PIECES];
+    if constexpr (D == 128) {
+        src[0] = (8 * (lr >> 2) + (lr & 3)) * 64 + cq * 16;
+        src[1] = src[0] + 256;
+        src[2] = 2048 + cq * 512 + lr * 32;
+        src[3] = src[2] + 16;
+    } else {
+        src[0] = 16 * lane;
+        src[1] = 1024 + 16 * lane;
+    }
+    src[PIECES - 1] = 32 * D + 4 * lane;                           // the params: 64 lanes x 4 bytes
+    // the pages of the tiles [kw, kw + 128), lane l holding those of kw + l and
+    // kw + 64 + l (-1: missing): one table load in 128 tiles
+    int pgw[2] = {-1, -1}, kw = -(1 << 20);
+    uint32_t there = 0;                                            // bit i % 32: tile i has a page
+    auto issue = [&](int i, int at) {
+        if (i < kw || i >= kw + 128) {
+            kw = i;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                const int bj = wq0 + (i + 64 * hf + lane) * 128;
+                pgw[hf] = bj < pe ? kv4_page(g, slot, bj / g.P) : -1;
+                if (pgw[hf] < 0 && bj < pe && r.err) ((volatile __attribute__((address_space(1))) uint32_t*)r.err)[ERR_PAGE] = 1u;
+            }
+        }
+        const int j = i - kw, blk = wq0 + 128 * i, in = __builtin_amdgcn_readfirstlane(blk % g.P);
+        const int pa = __builtin_amdgcn_readlane(pgw[0], j & 63), pb = __builtin_amdgcn_readlane(pgw[1], j & 63);
+        const int pg = j < 64 ? pa : pb;
+        there = (there & ~(1u << (i & 31))) | (uint32_t)(pg >= 0) << (i & 31);
+        // no page: the first tile of the pool is fetched and not used, so that every tile counts alike
+        const uint8_t* t = head + (pg < 0 ? 0 : pg * g.PS + (in >> 5) * (long long)TB);
+        const uint32_t to = ring + at * TB;
+#pragma unroll
+        for (int k = 0; k < PIECES - 1; ++k) tile_dma16(t, src[k], to + 1024 * k);
+        tile_dma4(t, src[PIECES - 1], to + 32 * D);
+    };
+#pragma unroll
+    for (int u = 0; u < RING; ++u)
+        if (u < nt) issue(u, u);
+
+    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7 times a power of two that puts
+    // the row's largest below 2^14, elements 2, 3, 6, 7 of them over 16; the row's
+    // sum in the products' unit (2^-24), and the factor back to a score in base 2
+    half8 qf[MQ][KW];
+    float qsum[MQ], rcs[MQ];
     int lim[MQ];
 #pragma unroll
     for (int mt = 0; mt < MQ; ++mt) {
         const int qrow = qbase + 16 * mt + lr, h = qrow / r.n, i = qrow - h * r.n, pos = basepos + i;
         const bool live = qrow < QR && i < nlive && pos >= 0 && pos < r.max_ctx;
         lim[mt] = live ? pos : -1;
-        qsum[mt] = 0.f;
         const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
+        u32x4 v[KW];
+        float top = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KW; ++ks) {
-            const u32x4 v = live ? *(const u32x4*)(qp + 8 * ks) : (u32x4){0, 0, 0, 0};
-            qf[mt][ks] = __builtin_bit_cast(bf16x8, v);
+            v[ks] = live ? *(const u32x4*)(qp + 8 * ks) : (u32x4){0, 0, 0, 0};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) qsum[mt] += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xffff0000u);
+            for (int e = 0; e < 4; ++e)
+                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(v[ks][e] << 16)), fabsf(__uint_as_float(v[ks][e] & 0xffff0000u))));
         }
-        qsum[mt] += __shfl_xor(qsum[mt], 16, WAVE);
-        qsum[mt] += __shfl_xor(qsum[mt], 32, WAVE);
+        top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+        const int ex = min(max(267 - (int)(__float_as_uint(top) >> 23), 1), 253);
+        const float up = __uint_as_float((uint32_t)ex << 23);
+        float sum = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KW; ++ks)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float a = __uint_as_float(v[ks][e] << 16) * up, b = __uint_as_float(v[ks][e] & 0xffff0000u) * up;
+                sum += a + b;
+                const float f = e & 1 ? 0.0625f : 1.f;
+                qf[mt][ks][2 * e] = (_Float16)(a * f);
+                qf[mt][ks][2 * e + 1] = (_Float16)(b * f);
+            }
+        sum += __shfl_xor(sum, 16, WAVE);
+        sum += __shfl_xor(sum, 32, WAVE);
+        qsum[mt] = sum * 5.9604644775390625e-08f;                  // 2^-24
+        rcs[mt] = cs * __uint_as_float((uint32_t)(254 - ex) << 23) * 16777216.f;
     }
 
-    float m[MQ], lsum[MQ], zsum[MQ];
-    floatx4 o[MQ][NBD];
+    float ref[MQ], lsum[MQ], zsum[MQ];
+    floatx4 o[MQ][NBD], oc[MQ];
 #pragma unroll
     for (int mt = 0; mt < MQ; ++mt) {
-        m[mt] = -INFINITY;
+        ref[mt] = KV4_REF0;
         lsum[mt] = zsum[mt] = 0.f;
+        oc[mt] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int nb = 0; nb < NBD; ++nb) o[mt][nb] = (floatx4){0.f, 0.f, 0.f, 0.f};
     }
 
-    struct regs {
-        alignas(16) uint32_t k[2][KW], v[NBD], kp[8], vp[8];
-        bool there;
+    // a word's codes in fp16 (see above)
+    auto codes = [](uint32_t x) {
+        const uint32_t y = x >> 8;
+        return __builtin_bit_cast(half8, (u32x4){x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u});
     };
-    const int wq0 = p0 + 32 * w, wstep = 128;
-    const int koff = (8 * (lr >> 2) + (lr & 3)) * (D / 2) + cq * (D / 8);      // + 4 pt (D/2)
-    const int voff = 16 * D + (cq * D + NBD * lr) * 4, poff = 32 * D + 32 * cq;
-    const uint8_t* head = g.pages + kvh * g.HS;
-    // the pages of the wave's tiles wq0 + k wstep, k in [kw, kw + 128), lane l
-    // holding those of kw + l and kw + 64 + l (-1: missing): one table load in 128 tiles
-    int pgw[2] = {-1, -1}, kw = -(1 << 20);
-    auto load = [&](int blk, regs& x) {
-        const int lp = __builtin_amdgcn_readfirstlane(blk / g.P);
-        const int k = __builtin_amdgcn_readfirstlane((blk - wq0) / wstep);
-        if (k < kw || k >= kw + 128) {
-            kw = k;
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const int bj = wq0 + (k + 64 * hf + lane) * wstep;
-                pgw[hf] = bj < pe ? kv4_page(g, slot, bj / g.P) : -1;
-                if (pgw[hf] < 0 && bj < pe && r.err) ((volatile __attribute__((address_space(1))) uint32_t*)r.err)[ERR_PAGE] = 1u;
-            }
-        }
-        const int j = k - kw;
-        const int pa = __builtin_amdgcn_readlane(pgw[0], j & 63), pb = __builtin_amdgcn_readlane(pgw[1], j & 63);
-        const int pg = j < 64 ? pa : pb;
-        x.there = pg >= 0;
-        // no page: the first tile of the pool is read and masked, so that the loads need no branch
-        const uint8_t* t = head + (pg < 0 ? 0 : pg) * g.PS + (pg < 0 ? 0 : (blk - lp * g.P) >> 5) * (long long)tile_bytes(D);
-#pragma unroll
-        for (int pt = 0; pt < 2; ++pt) {
-            if constexpr (KW == 4) *(u32x4*)x.k[pt] = __builtin_nontemporal_load((const u32x4*)(t + koff + pt * 2 * D));
-            else *(u32x2*)x.k[pt] = __builtin_nontemporal_load((const u32x2*)(t + koff + pt * 2 * D));
+    auto block = [&](int blk, const uint8_t* t, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        alignas(16) uint32_t kc[2][KW], kp[8], vp[8], vc[NBD];
+        if constexpr (D == 128) {
+            *(u32x4*)kc[0] = *(const u32x4*)(t + 16 * lane);
+            *(u32x4*)kc[1] = *(const u32x4*)(t + 1024 + 16 * lane);
+        } else {
+            const uint8_t* kr = t + (8 * (lr >> 2) + (lr & 3)) * 32 + cq * 8;
+            *(u32x2*)kc[0] = *(const u32x2*)kr;
+            *(u32x2*)kc[1] = *(const u32x2*)(kr + 128);
         }
 #pragma unroll
         for (int e = 0; e < 8; e += 4) {
-            *(u32x4*)(x.kp + e) = __builtin_nontemporal_load((const u32x4*)(t + poff + 4 * e));
-            *(u32x4*)(x.vp + e) = __builtin_nontemporal_load((const u32x4*)(t + poff + 128 + 4 * e));
-        }
-#pragma unroll
-        for (int e = 0; e < NBD; e += 4) *(u32x4*)(x.v + e) = __builtin_nontemporal_load((const u32x4*)(t + voff + 4 * e));
-    };
-    // eight codes as the bf16 numbers 128 + c
-    auto codes = [](uint32_t x) {
-        u32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = ((x >> (4 * e)) & 0x000f000fu) | 0x43004300u;
-        return __builtin_bit_cast(bf16x8, v);
-    };
-    const uint32_t off2 = 0xc308c308u;                             // (-136, -136)
-    const bf16x8 off = __builtin_bit_cast(bf16x8, (u32x4){off2, off2, off2, off2});
-    auto block = [&](int blk, const regs& x) {
-        const bool masked = !x.there || blk + 32 > pe || blk + 31 > all;
-        float ks[8], vs[8], vz[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ks[e] = __uint_as_float(x.kp[e] << 16) * cs;
-            vs[e] = __uint_as_float(x.vp[e] << 16);
-            vz[e] = __uint_as_float(x.vp[e] & 0xffff0000u);
+            *(u32x4*)(kp + e) = *(const u32x4*)(t + 32 * D + 32 * cq + 4 * e);
+            *(u32x4*)(vp + e) = *(const u32x4*)(t + 32 * D + 128 + 32 * cq + 4 * e);
         }
         floatx4 st[MQ][2];
 #pragma unroll
-        for (int pt = 0; pt < 2; ++pt) {
-#pragma unroll
-            for (int mt = 0; mt < MQ; ++mt) {
-                const float c0 = -136.f * qsum[mt];
-                st[mt][pt] = (floatx4){c0, c0, c0, c0};
-            }
+        for (int pt = 0; pt < 2; ++pt)
 #pragma unroll
             for (int k = 0; k < KW; ++k) {
-                const bf16x8 kf = codes(x.k[pt][k]);
+                const half8 kf = codes(kc[pt][k]);
 #pragma unroll
-                for (int mt = 0; mt < MQ; ++mt) st[mt][pt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[mt][k], st[mt][pt], 0, 0, 0);
+                for (int mt = 0; mt < MQ; ++mt)
+                    st[mt][pt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[mt][k], k ? st[mt][pt] : (floatx4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
             }
+        float ks[8], kz[8], vs[8], vz[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            ks[e] = __uint_as_float(kp[e] << 16);
+            kz[e] = __builtin_fmaf(-8.f, ks[e], __uint_as_float(kp[e] & 0xffff0000u));
+            vs[e] = __uint_as_float(vp[e] << 16);
+            vz[e] = __uint_as_float(vp[e] & 0xffff0000u);
         }
-        bf16x8 pf[MQ];
+        half8 pf[MQ];
 #pragma unroll
         for (int mt = 0; mt < MQ; ++mt) {
-            float sc[8];
-            const float qz = qsum[mt] * cs;
+            float u[8], p[8], pv[8];
+            bool seen[8];
+            const int last = min(pe - 1, lim[mt]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sc[e] = __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], __uint_as_float(x.kp[e] & 0xffff0000u) * qz);
-                if (masked) {
-                    const int pos = blk + 8 * cq + e;
-                    if (!x.there || pos >= pe || pos > lim[mt]) sc[e] = -INFINITY;
-                }
+                u[e] = __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], kz[e] * qsum[mt]);
+                seen[e] = !MASKED || blk + 8 * cq + e <= last;     // what a row does not see may hold anything
             }
-            float bm = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
-            bm = fmaxf(bm, __shfl_xor(bm, 16, WAVE));
-            bm = fmaxf(bm, __shfl_xor(bm, 32, WAVE));
-            const bool need = bm > m[mt] + 8.f;
-            if (__builtin_amdgcn_ballot_w64(need)) {
-                const float mn = need ? bm : m[mt];
-                const float corr = m[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mt] - mn);
-                m[mt] = mn;
+            auto weights = [&] {
+                float top = 0.f, most = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float a = __builtin_fmaf(rcs[mt], u[e], -ref[mt]);
+                    p[e] = __builtin_amdgcn_exp2f(seen[e] ? a : -INFINITY);
+                    pv[e] = p[e] * (seen[e] ? vs[e] : 0.f);
+                    top = fmaxf(top, pv[e]);
+                    most = fmaxf(most, p[e]);
+                }
+                return fmaxf(top, most * 0x1p-85f);
+            };
+            float top = weights();
+            // (infinite references, of infinite scores, stay)
+            if (__builtin_amdgcn_ballot_w64(top > 32768.f && ref[mt] < INFINITY)) {
+                float bm = KV4_REF0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float a = rcs[mt] * u[e];
+                    if (seen[e]) bm = fmaxf(bm, fmaxf(a + __builtin_amdgcn_logf(vs[e]), a - 85.f));
+                }
+                bm = fmaxf(bm, __shfl_xor(bm, 16, WAVE));
+                bm = fmaxf(bm, __shfl_xor(bm, 32, WAVE));
+                top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+                top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+                const float to = top > 32768.f ? fmaxf(bm - 7.f, ref[mt]) : ref[mt];
+                const float corr = to == ref[mt] ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - to);
+                ref[mt] = to;
                 lsum[mt] *= corr;
                 zsum[mt] *= corr;
 #pragma unroll
-                for (int nb = 0; nb < NBD; ++nb)
+                for (int i = 0; i < 4; ++i) {
+                    oc[mt][i] *= corr;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[mt][nb][i] *= corr;
+                    for (int nb = 0; nb < NBD; ++nb) o[mt][nb][i] *= corr;
+                }
+                weights();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) pv[e] = fminf(pv[e], 32768.f);   // (scores past 2^23, where a unit in the last place is large)
             }
-            const float mn = m[mt] == -INFINITY ? 0.f : m[mt];
-            float pv[8];
+            float2v pr[4];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float p = __builtin_amdgcn_exp2f(sc[e] - mn);
-                // (a value that this row does not see, but a later one does, may be NaN)
-                const bool seen = !masked || sc[e] != -INFINITY;
-                lsum[mt] += p;
-                zsum[mt] = __builtin_fmaf(p, seen ? vz[e] : 0.f, zsum[mt]);
-                pv[e] = p * (seen ? vs[e] : 0.f);
+                lsum[mt] += p[e];
+                zsum[mt] = __builtin_fmaf(p[e], seen[e] ? vz[e] : 0.f, zsum[mt]);
+                pr[e >> 1][e & 1] = e & 2 ? pv[e] * 0.0625f : pv[e];
             }
-            pf[mt] = __builtin_bit_cast(bf16x8, (u32x4){pack_bf16x2(pv[0], pv[1]), pack_bf16x2(pv[2], pv[3]),
-                                                        pack_bf16x2(pv[4], pv[5]), pack_bf16x2(pv[6], pv[7])});
+            u32x4 pk;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pk[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr[e], half2v));
+            pf[mt] = __builtin_bit_cast(half8, pk);
         }
+#pragma unroll
+        for (int e = 0; e < NBD; e += 4) *(u32x4*)(vc + e) = *(const u32x4*)(t + 16 * D + 256 * e + 16 * lane);
 #pragma unroll
         for (int nb = 0; nb < NBD; ++nb) {
-            const bf16x8 vt = codes(x.v[nb]);
+            const half8 vt = codes(vc[nb]);
 #pragma unroll
-            for (int mt = 0; mt < MQ; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[mt], o[mt][nb], 0, 0, 0);
+            for (int mt = 0; mt < MQ; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, pf[mt], o[mt][nb], 0, 0, 0);
         }
+        const half8 mid = codes(0x88888888u);
 #pragma unroll
-        for (int nb = 0; nb < NBD; ++nb)
-#pragma unroll
-            for (int mt = 0; mt < MQ; ++mt) o[mt][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(off, pf[mt], o[mt][nb], 0, 0, 0);
+        for (int mt = 0; mt < MQ; ++mt) oc[mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(mid, pf[mt], oc[mt], 0, 0, 0);
     };
-
-    const bool usable = slot >= 0 && slot < r.max_slots;           // else p0 == p1 == 0: no tile
-    if (usable && wq0 < pe) {
-        regs x0, x1;
-        load(wq0, x0);
-        for (int blk = wq0; blk < pe; blk += 2 * wstep) {
-            load(blk + wstep, x1);
-            block(blk, x0);
-            if (blk + wstep >= pe) break;
-            load(blk + 2 * wstep, x0);
-            block(blk + wstep, x1);
-        }
-    }
+    // a tile waits for its own pieces; once it is used, its place is filled with the tile RING further
+    int at = 0;
+    auto tile = [&](int i, auto masked) {
+        const int later = nt - 1 - i;
+        if (later >= RING - 1) wait_tiles<PIECES * (RING - 1)>();
+        else if (RING > 3 && later == 2) wait_tiles<PIECES * 2>();
+        else if (RING > 2 && later == 1) wait_tiles<PIECES>();
+        else wait_tiles<0>();
+        if (there >> (i & 31) & 1) block(wq0 + 128 * i, s_buf + w * (RING * TB) + at * TB, masked);   // else no page: nothing to see
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // read before the place is filled again
+        if (i + RING < nt) issue(i + RING, at);
+        at = at + 1 == RING ? 0 : at + 1;
+    };
+    // the tiles that every row sees as a whole, then the others
+    const int whole = min(nt, max(0, (min(pe, all + 1) - wq0 + 96) >> 7));
+    int i = 0;
+    for (; i < whole; ++i) tile(i, std::false_type());
+    for (; i < nt; ++i) tile(i, std::true_type());
 
     // merge the four waves, 16 query rows at a time
 #pragma unroll
@@ -582,15 +670,18 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         zsum[mt] += __shfl_xor(zsum[mt], 16, WAVE);
         zsum[mt] += __shfl_xor(zsum[mt], 32, WAVE);
         __syncthreads();
-        if (cq == 0) { s_ml[w][0][lr] = m[mt]; s_ml[w][1][lr] = lsum[mt]; }
+        if (cq == 0) { s_ml[w][0][lr] = ref[mt]; s_ml[w][1][lr] = lsum[mt]; }
         // lane (cq, lr) holds dims NBD (4 cq + i) + nb of row lr
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int nb = 0; nb < NBD; nb += 4)
-                *(float4*)(&s_o[w][lr * LDO + NBD * (4 * cq + i) + nb]) =
-                    make_float4(o[mt][nb][i] + zsum[mt], o[mt][nb + 1][i] + zsum[mt], o[mt][nb + 2][i] + zsum[mt],
-                                o[mt][nb + 3][i] + zsum[mt]);
+            {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(o[mt][nb + e][i] - oc[mt][i], 16777216.f, zsum[mt]);
+                *(float4*)(&s_o[w][lr * LDO + NBD * (4 * cq + i) + nb]) = make_float4(v[0], v[1], v[2], v[3]);
+            }
         __syncthreads();
         for (int idx = threadIdx.x; idx < 16 * D / 4; idx += 256) {
             const int qr = idx / (D / 4), d = 4 * (idx - qr * (D / 4)), qrow = qbase + 16 * mt + qr;
@@ -741,10 +832,10 @@ static void kv4_attn_d(const rows_t& r, const att_plan& pl, const kv4_geom& g, i
         else kern<<<grid, block, 0, s>>>(r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
     };
     switch (pl.mq) {
-        case 1: go(k_kv4_attn<D, 1>); break;
-        case 2: go(k_kv4_attn<D, 2>); break;
-        case 3: go(k_kv4_attn<D, 3>); break;
-        default: go(k_kv4_attn<D, 4>); break;
+        case 1: go(k_kv4_attn<D, 1, 4>); break;
+        case 2: go(k_kv4_attn<D, 2, 4>); break;
+        case 3: go(k_kv4_attn<D, 3, 4>); break;
+        default: go(k_kv4_attn<D, 4, 4>); break;
     }
 }
 
