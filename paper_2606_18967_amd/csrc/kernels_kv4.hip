@@ -78,109 +78,200 @@ __global__ void __launch_bounds__(256) k_rope_table(sd_rope_cfg c, double lo, do
 }
 
 // ------------------------------------------------------------------ append
-// eight consecutive inputs as floats; the projection's split-K partials (S > 1)
-// are summed on read
-__device__ __forceinline__ void load8(const kv4_src<float>& x, size_t i, float (&y)[8])
-{
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-    if (x.S > 1) {
-        add_splits2(a, b, x.P, x.S, x.st, i, i + 4);
-    } else {
-        a = *(const float4*)(x.x + i);
-        b = *(const float4*)(x.x + i + 4);
-    }
-    y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
-    y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
-}
-__device__ __forceinline__ void load8(const kv4_src<uint16_t>& x, size_t i, float (&y)[8])
-{
-    const u32x4 v = *(const u32x4*)(x.x + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        y[2 * e] = __uint_as_float(v[e] << 16);
-        y[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
-    }
-}
-
-// dims d0 .. d0 + 7 of the row at x, rotated by the table row rp; the products
-// and their sum in type A, rounded to fp32
-template <typename A, typename T>
-__device__ __forceinline__ void rotated8(const kv4_src<T>& x, size_t row, int d0, const float2* rp, const kv4_rope& ro,
-                                         float (&y)[8])
-{
-    load8(x, row + d0, y);
-    if (d0 >= ro.rot) return;
-    if (ro.interleaved) {
-        const float4 t0 = *(const float4*)(rp + d0 / 2), t1 = *(const float4*)(rp + d0 / 2 + 2);
-        const float2 t[4] = {{t0.x, t0.y}, {t0.z, t0.w}, {t1.x, t1.y}, {t1.z, t1.w}};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const A a = y[2 * j], b = y[2 * j + 1], c = t[j].x, s = t[j].y;
-            y[2 * j] = (float)(a * c - b * s);
-            y[2 * j + 1] = (float)(a * s + b * c);
+// Eight consecutive inputs as they are loaded, and as floats; the projection's
+// split-K partials (S > 1) are summed on read.
+template <typename T> struct oct;
+template <> struct oct<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const kv4_src<float>& x, size_t i)
+    {
+        if (x.S > 1) {
+            a = b = make_float4(0.f, 0.f, 0.f, 0.f);
+            add_splits2(a, b, x.P, x.S, x.st, i, i + 4);
+        } else {
+            a = *(const float4*)(x.x + i);
+            b = *(const float4*)(x.x + i + 4);
         }
-        return;
     }
-    const int h = ro.rot / 2;
-    const bool first = d0 < h;
-    const int i0 = first ? d0 : d0 - h;
-    float o[8];
-    load8(x, row + (first ? d0 + h : i0), o);
+    __device__ __forceinline__ void get(float (&y)[8]) const
+    {
+        y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
+        y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+    }
+};
+template <> struct oct<uint16_t> {
+    u32x4 v;
+    __device__ __forceinline__ void load(const kv4_src<uint16_t>& x, size_t i) { v = *(const u32x4*)(x.x + i); }
+    __device__ __forceinline__ void get(float (&y)[8]) const
+    {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float4 t = *(const float4*)(rp + i0 + 2 * j);
-        const A sg = first ? (A)-1 : (A)1;
-        y[2 * j] = (float)((A)y[2 * j] * (A)t.x + sg * (A)o[2 * j] * (A)t.y);
-        y[2 * j + 1] = (float)((A)y[2 * j + 1] * (A)t.z + sg * (A)o[2 * j + 1] * (A)t.w);
+        for (int e = 0; e < 4; ++e) {
+            y[2 * e] = __uint_as_float(v[e] << 16);
+            y[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        }
     }
+};
+
+// A lane's eight dims d0 .. d0 + 7 of a head, and with the half layout the eight
+// that they turn with.
+template <typename T>
+struct rows8 {
+    oct<T> own, other;
+    __device__ __forceinline__ void fetch(const kv4_src<T>& x, size_t at, int d0, const kv4_rope& ro)
+    {
+        own.load(x, at + d0);
+        if (d0 < ro.rot && !ro.interleaved) other.load(x, at + (d0 < ro.rot / 2 ? d0 + ro.rot / 2 : d0 - ro.rot / 2));
+    }
+    // rotated, the products and their sum in type A, rounded to fp32; t: the lane's (cos, sin)
+    template <typename A>
+    __device__ __forceinline__ void turn(const float2 (&t)[8], int d0, const kv4_rope& ro, float (&y)[8]) const
+    {
+        own.get(y);
+        if (d0 >= ro.rot) return;
+        if (ro.interleaved) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const A a = y[2 * j], b = y[2 * j + 1], c = t[j].x, s = t[j].y;
+                y[2 * j] = (float)(a * c - b * s);
+                y[2 * j + 1] = (float)(a * s + b * c);
+            }
+        } else {
+            float o[8];
+            other.get(o);
+            const A sg = d0 < ro.rot / 2 ? (A)-1 : (A)1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = (float)((A)y[j] * (A)t[j].x + sg * (A)o[j] * (A)t[j].y);
+        }
+    }
+};
+// the table's entries for a lane's dims at a position
+__device__ __forceinline__ void turns(const kv4_rope& ro, int pos, int d0, float2 (&t)[8])
+{
+    if (d0 >= ro.rot) return;
+    const int h = ro.rot / 2;
+    const float4* rp = (const float4*)(ro.table + (size_t)pos * h + (ro.interleaved ? d0 / 2 : d0 < h ? d0 : d0 - h));
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < 2 || !ro.interleaved) {
+            const float4 v = rp[j];
+            t[2 * j] = make_float2(v.x, v.y);
+            t[2 * j + 1] = make_float2(v.z, v.w);
+        }
 }
 
-// code of y in the group (s, z): clamp(rint((y - z)/s) + 8, 0, 15).  The quotient
-// in fp32 is within 2e-5 of the real one, so it decides unless it is near a half;
-// there (two values in a thousand) fp64 does, whose quotient can meet a half only
-// where the real one does.
-__device__ __forceinline__ uint32_t code_of(float y, float z, float s, float rs)
+// min or max over the D/8 lanes that share a row (neighbours), by lane permutations
+// within 16 lanes: i ^ 1, i ^ 2, 7 - i, 15 - i
+template <int LPR, typename F>
+__device__ __forceinline__ float row_reduce(float v, F f)
 {
-    const float t = (y - z) * rs;
-    float q = rintf(t);
-    if (!(fabsf(fabsf(t - q) - 0.5f) >= 1e-3f)) q = (float)rint(((double)y - (double)z) / (double)s);
-    return s > 0.f ? (uint32_t)(int)(fminf(fmaxf(q, -8.f), 7.f) + 8.f) : 8u;
+    auto swap = [&](auto ctrl) {
+        return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v = f(v, swap(std::integral_constant<int, 0xb1>()));
+    v = f(v, swap(std::integral_constant<int, 0x4e>()));
+    v = f(v, swap(std::integral_constant<int, 0x141>()));
+    if (LPR == 16) v = f(v, swap(std::integral_constant<int, 0x140>()));
+    return v;
+}
+
+// A lane's part of quantizing a row (the group (s, z) of the row's D/8 lanes):
+// CODE0 + code of each value, clamp(rint((y - z)/s) + 8, 0, 15).  A sum with
+// CODE0 + 8 = 1.5 * 2^23 + 8 rounds to the nearest integer, ties to even.  The
+// quotient in fp32 is within 2e-6 of the real one, so it decides unless one is
+// within 1e-4 of a half; there (a value in five thousand) fp64 does, whose
+// quotient can meet a half only where the real one does.
+constexpr uint32_t CODE0 = 0x4b400000u;
+
+template <int LPR>
+__device__ __forceinline__ uint32_t quantize8(const float (&y)[8], bool live, uint32_t (&code)[8])
+{
+    float mn = y[0], mx = y[0], fin = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        mn = fminf(mn, y[e]);
+        mx = fmaxf(mx, y[e]);
+        fin = __builtin_fmaf(y[e], 0.f, fin);                      // NaN once a value is not finite
+    }
+    mx = fin == 0.f ? mx : INFINITY;
+    mn = row_reduce<LPR>(mn, [](float a, float b) { return fminf(a, b); });
+    mx = row_reduce<LPR>(mx, [](float a, float b) { return fmaxf(a, b); });
+    const bool bad = mx == INFINITY;
+    // (mx - mn) / 15, correctly rounded: the reciprocal's product, and its remainder's
+    const double d = (double)mx - (double)mn, r15 = 1.0 / 15.0, q0 = d * r15;
+    const uint32_t sb = f32_to_bf16((float)__builtin_fma(__builtin_fma(-15.0, q0, d), r15, q0));
+    const float s = __uint_as_float(sb << 16);
+    const uint32_t zb = f32_to_bf16((float)__builtin_fma(8.0, (double)s, (double)mn));
+    const float z = __uint_as_float(zb << 16), rs = __builtin_amdgcn_rcpf(s);
+    float far = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = __builtin_amdgcn_fmed3f((y[e] - z) * rs, -8.f, 7.f);
+        const float m = t + __uint_as_float(CODE0 + 8);
+        far = fmaxf(far, fabsf(t - (m - __uint_as_float(CODE0 + 8))));
+        code[e] = __float_as_uint(m);
+    }
+    // (and steps that are 0, not finite, or without a reciprocal)
+    if (__builtin_amdgcn_ballot_w64(live && !(far < 0.4999f && s >= 0x1p-100f && s <= 0x1p100f))) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double q = rint(((double)y[e] - (double)z) / (double)s);
+            code[e] = CODE0 + (s > 0.f && !bad ? (uint32_t)((int)fmin(fmax(q, -8.0), 7.0) + 8) : 8u);
+        }
+    }
+    return bad ? 0x7fc07fc0u : sb | zb << 16;
 }
 
 // One wave takes the new rows among 8 consecutive positions of one KV head's K or
 // V (the words of V hold 8 positions, so a word has one writer), D/8 lanes a row;
-// further waves rotate the queries, D/8 lanes a row and head.  K is rotated in
+// further waves rotate the queries, D/8 lanes a head, QPASS times 512/D heads of a
+// row each.  K is rotated in
 // fp64 so that its codes are those of the exact rotation (a value next to a border
 // moves by a whole step otherwise); its products are few against the row's bytes.
+constexpr int QPASS = 4;
+constexpr int KV4_APPEND_WAVES = 4096;
+
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_q, int n_kv, kv4_src<T> xk, kv4_src<T> xv,
-                                                    kv4_src<T> xq, uint16_t* q_out, kv4_rope ro, int ngr, int kv_waves)
+                                                    kv4_src<T> xq, uint16_t* q_out, kv4_rope ro, int ngr, int hpw, int kv_waves)
 {
     constexpr int LPR = D / 8, RPW = WAVE / LPR, NP = 8 / RPW;     // lanes a row, rows a pass, passes of a group
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     const int lw = lane % LPR, lt = lane / LPR, d0 = 8 * lw;
-    if (wave >= kv_waves) {                                        // queries
-        const long long unit = (long long)(wave - kv_waves) * RPW + lt;
-        if (unit >= (long long)r.B * r.n * n_q) return;
-        const int idx = (int)(unit / n_q), h = (int)(unit - (long long)idx * n_q);
+    if (wave >= kv_waves) {                                        // queries: QH heads of one row
+        if (!q_out) return;                                        // the last work-group's waves past K and V
+        constexpr int QH = QPASS * RPW;
+        const int qw = (n_q + QH - 1) / QH, unit = wave - kv_waves, idx = unit / qw, h0 = (unit - idx * qw) * QH + lt;
         const int b = idx / r.n, i = idx - b * r.n;
-        if (r.lim && i >= r.lim[b]) return;
+        if (b >= r.B || (r.lim && i >= r.lim[b])) return;
         const size_t row = r.row0 ? r.row0[b] + i : idx;
         const int slot = r.slots[b];
         int pos = -1;
         if (slot >= 0 && slot < r.max_slots) pos = r.kv_len[slot] + r.off + i;
-        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (pos >= 0 && pos < r.max_ctx && (ro.rot == 0 || pos < ro.len))
-            rotated8<float>(xq, row * xq.ld + (size_t)h * D, d0, ro.table + (size_t)pos * (ro.rot / 2), ro, y);
-        *(u32x4*)(q_out + (row * n_q + h) * D + d0) = (u32x4){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
-                                                             pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+        const bool ok = pos >= 0 && pos < r.max_ctx && (ro.rot == 0 || pos < ro.len);
+        float2 tr[8] = {};
+        rows8<T> x[QPASS] = {};
+        if (ok) {
+#pragma unroll
+            for (int ps = 0; ps < QPASS; ++ps)                     // past the last head: it again, not stored
+                x[ps].fetch(xq, row * xq.ld + (size_t)min(h0 + ps * RPW, n_q - 1) * D, d0, ro);
+            turns(ro, pos, d0, tr);
+        }
+#pragma unroll
+        for (int ps = 0; ps < QPASS; ++ps) {
+            float y[8];
+            x[ps].template turn<float>(tr, d0, ro, y);
+            if (h0 + ps * RPW < n_q)
+                *(u32x4*)(q_out + (row * n_q + h0 + ps * RPW) * D + d0) =
+                    (u32x4){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+        }
         return;
     }
-    // (sequence, group, KV head, K or V), the heads of one group side by side
-    const int u = wave % (2 * n_kv), bg = wave / (2 * n_kv), b = bg / ngr, gr = bg - b * ngr;
-    const bool is_v = u >= n_kv;
-    const int h = is_v ? u - n_kv : u;
+    // (sequence, group, hpw KV heads, K or V), the heads of one group side by side
+    const int hw = (n_kv + hpw - 1) / hpw;
+    const int u = wave % (2 * hw), bg = wave / (2 * hw), b = bg / ngr, gr = bg - b * ngr;
+    const bool is_v = u >= hw;
+    const int h0 = (is_v ? u - hw : u) * hpw, h1 = min(h0 + hpw, n_kv);
     const int nl = r.lim ? r.lim[b] : r.n, nlive = min(max(nl, 0), r.n);
     const int slot = r.slots[b];
     const bool first = gr == 0 && u == 0 && lane == 0;
@@ -202,73 +293,88 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         return;
     }
     const int in = pg0 % g.P, r32 = in & 31;
-    uint8_t* tile = g.pages + page * g.PS + h * g.HS + (size_t)(in >> 5) * tile_bytes(D);
+    uint8_t* tile = g.pages + page * g.PS + h0 * g.HS + (size_t)(in >> 5) * tile_bytes(D);
     const size_t row0 = r.row0 ? r.row0[b] : (size_t)b * r.n;
-    uint32_t vw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    uint32_t mask = 0;                                             // the new rows' nibbles of a V word
+    auto store = [&](auto vtag) {
+        constexpr bool V = decltype(vtag)::value;
+        const kv4_src<T>& src = V ? xv : xk;
+        const kv4_rope rk = V ? kv4_rope{nullptr, 0, 0, 0} : ro;
+        rows8<T> next[NP] = {};
+        float2 tr[NP][8] = {};
+        auto fetch = [&](int h) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-        if (pg0 + t >= lo && pg0 + t < hi) mask |= 0xfu << nib(t);
+            for (int ps = 0; ps < NP; ++ps) {
+                const int pos = pg0 + ps * RPW + lt;
+                if (pos >= lo && pos < hi) next[ps].fetch(src, (row0 + (pos - base)) * src.ld + (size_t)h * D, d0, rk);
+            }
+        };
+        fetch(h0);
 #pragma unroll
-    for (int ps = 0; ps < NP; ++ps) {
-        const int t = ps * RPW + lt, pos = pg0 + t;
-        const bool live = pos >= lo && pos < hi;
-        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) {
-            const size_t row = row0 + (pos - base);
-            if (is_v) load8(xv, row * xv.ld + (size_t)h * D + d0, y);
-            else rotated8<double>(xk, row * xk.ld + (size_t)h * D, d0, ro.table + (size_t)pos * (ro.rot / 2), ro, y);
+        for (int ps = 0; ps < NP; ++ps) {
+            const int pos = pg0 + ps * RPW + lt;
+            if (pos >= lo && pos < hi) turns(rk, pos, d0, tr[ps]);
         }
-        float mn = y[0], mx = y[0];
-        bool bad = false;
+        uint32_t mask = 0;                                         // the new rows' nibbles of a V word
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            bad |= !(fabsf(y[e]) < INFINITY);
-            mn = fminf(mn, y[e]);
-            mx = fmaxf(mx, y[e]);
+        for (int t = 0; t < 8; ++t)
+            if (pg0 + t >= lo && pg0 + t < hi) mask |= 0xfu << nib(t);
+        for (int h = h0; h < h1; ++h, tile += g.HS) {
+            rows8<T> now[NP];
+#pragma unroll
+            for (int ps = 0; ps < NP; ++ps) now[ps] = next[ps];
+            if (h + 1 < h1) fetch(h + 1);
+            uint32_t vw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int ps = 0; ps < NP; ++ps) {
+                const int t = ps * RPW + lt, pos = pg0 + t;
+                const bool live = pos >= lo && pos < hi;
+                float y[8];
+                uint32_t code[8];
+                now[ps].template turn<double>(tr[ps], d0, rk, y);
+                const uint32_t par = quantize8<LPR>(y, live, code);
+                if (V) {
+                    const int sh = nib(t);
+                    const uint32_t take = live ? 15u : 0u;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) vw[e] |= (code[e] & take) << sh;
+                } else if (live) {
+                    uint32_t w = 0, zero = 0;                      // sum (CODE0 + code) 2^nib, less that of CODE0
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        w += code[e] << nib(e);
+                        zero += CODE0 << nib(e);
+                    }
+                    *(uint32_t*)(tile + (r32 + t) * (D / 2) + 4 * lw) = w - zero;
+                }
+                if (live && lw == 0) *(uint32_t*)(tile + 32 * D + (V ? 128 : 0) + 4 * (r32 + t)) = par;
+            }
+            if (!V) continue;
+            // a word's nibbles lie in the lanes lw of every lt: each exchange leaves a lane
+            // half of the words, until lane (lt, lw) has its 8 / RPW of them
+            constexpr int WPL = 8 / RPW;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const auto x = __builtin_amdgcn_permlane32_swap(vw[e], vw[e + 4], false, false);
+                vw[e] = x[0] | x[1];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const auto x = __builtin_amdgcn_permlane16_swap(vw[e], vw[e + 2], false, false);
+                vw[e] = x[0] | x[1];
+            }
+            int w0 = (lane & 32 ? 4 : 0) + (lane & 16 ? 2 : 0);
+            if (WPL == 1) {
+                const uint32_t got = __builtin_amdgcn_mov_dpp(lane & 8 ? vw[0] : vw[1], 0x128, 0xf, 0xf, true);   // lane ^ 8
+                vw[0] = (lane & 8 ? vw[1] : vw[0]) | got;
+                w0 += lane & 8 ? 1 : 0;
+            }
+            uint32_t* dst = (uint32_t*)(tile + 16 * D) + (r32 >> 3) * D + d0 + w0;
+#pragma unroll
+            for (int e = 0; e < WPL; ++e) dst[e] = mask == 0xffffffffu ? vw[e] : (dst[e] & ~mask) | vw[e];
         }
-        mx = bad ? INFINITY : mx;
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) {
-            mn = fminf(mn, __shfl_xor(mn, o, WAVE));
-            mx = fmaxf(mx, __shfl_xor(mx, o, WAVE));
-        }
-        bad = mx == INFINITY;
-        const uint32_t sb = f32_to_bf16((float)(((double)mx - (double)mn) / 15.0));
-        const float s = __uint_as_float(sb << 16);
-        const uint32_t zb = f32_to_bf16((float)((double)mn + 8.0 * (double)s));
-        const float z = __uint_as_float(zb << 16), rs = 1.f / s;
-        const uint32_t par = bad ? 0x7fc07fc0u : sb | zb << 16;
-        uint32_t w = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t c = bad ? 8u : code_of(y[e], z, s, rs);
-            w |= c << nib(e);
-            vw[e] |= live ? c << nib(t) : 0u;
-        }
-        if (live) {
-            if (!is_v) *(uint32_t*)(tile + (r32 + t) * (D / 2) + 4 * lw) = w;
-            if (lw == 0) *(uint32_t*)(tile + 32 * D + (is_v ? 128 : 0) + 4 * (r32 + t)) = par;
-        }
-    }
-    if (!is_v) return;
-    // a word's nibbles lie in the lanes lw of every lt: each halving of the lanes
-    // leaves a lane half of the words, until lane (lt, lw) has its 8 / RPW of them
-    constexpr int WPL = 8 / RPW;
-    int w0 = 0;
-#pragma unroll
-    for (int o = 32, n = 4; n >= WPL; o >>= 1, n >>= 1) {
-        const bool up = lane & o;
-#pragma unroll
-        for (int e = 0; e < n; ++e) {
-            const uint32_t got = __shfl_xor(up ? vw[e] : vw[e + n], o, WAVE);
-            vw[e] = (up ? vw[e + n] : vw[e]) | got;
-        }
-        w0 += up ? n : 0;
-    }
-    uint32_t* dst = (uint32_t*)(tile + 16 * D) + (r32 >> 3) * D + d0 + w0;
-#pragma unroll
-    for (int e = 0; e < WPL; ++e) dst[e] = mask == 0xffffffffu ? vw[e] : (dst[e] & ~mask) | vw[e];
+    };
+    if (is_v) store(std::true_type());
+    else store(std::false_type());
 }
 
 // ------------------------------------------------------------------ read
@@ -351,7 +457,7 @@ __device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, i
 // Work-group (item, KV head, slice of 16 MQ query rows) covers the positions
 // [p0, p1) of its item (att_plan); its four waves take the tiles of 32 positions
 // in turn.  With q the query, c the codes of a position and (s, z) its group,
-//   score = s (q . c) + (z - 8 s) sum(q),   out = sum (P s) (c - 8) + sum P z,
+//   score = s (q . c - 8 sum(q)) + z sum(q),   out = sum (P s) (c - 8) + sum P z,
 // so the products run on the codes themselves.  A nibble under a mask is an fp16
 // number as it stands: c 2^-24 in bits 0..3 (denormal, which the matrix cores
 // take), c 2^-20 in bits 4..7; a word's eight codes are four ANDs and a shift,
@@ -367,8 +473,8 @@ __device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, i
 // Online softmax in base 2.  A row's reference ref bounds the products' operand:
 // P s = exp2(score - ref) s <= 2^15; it moves, with all sums, only where a tile
 // would exceed that, to where the tile's largest P s is 2^7, so small terms are
-// lost at 2^-24 of a row's largest and not earlier.  (P alone stays below 2^100 for
-// rows of s = 0.)  Sums and statistics in fp32.
+// lost at 2^-24 of a row's largest and not earlier (P itself stays below 2^75 where
+// s is smaller than 2^-60).  Sums and statistics in fp32.
 constexpr float KV4_REF0 = -1e30f;     // the reference of a row that has seen no position
 
 // 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
@@ -400,6 +506,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     constexpr int BUF = 4 * RING * TB > 4 * 16 * LDO * 4 ? 4 * RING * TB : 4 * 16 * LDO * 4;
     static_assert(PIECES * (RING - 1) < 64, "vmcnt range");
     __shared__ __attribute__((aligned(1024))) uint8_t s_buf[BUF];  // the waves' rings, then the merge
+    __shared__ float2 s_par[4 * 64];
     __shared__ float s_ml[4][2][16];
     float (*s_o)[16 * LDO] = (float (*)[16 * LDO])s_buf;
 
@@ -476,47 +583,56 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     for (int u = 0; u < RING; ++u)
         if (u < nt) issue(u, u);
 
-    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7 times a power of two that puts
-    // the row's largest below 2^14, elements 2, 3, 6, 7 of them over 16; the row's
-    // sum in the products' unit (2^-24), and the factor back to a score in base 2
+    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7 times the power of two that
+    // puts the slice's largest below 2^14 (what is lost of small ones is 2^-38 of
+    // it), elements 2, 3, 6, 7 over 16; the row's sum in the products' unit (2^-24);
+    // and the factor from that unit to a score in base 2
     half8 qf[MQ][KW];
-    float qsum[MQ], rcs[MQ];
+    float qsum[MQ], unit;
     int lim[MQ];
-#pragma unroll
-    for (int mt = 0; mt < MQ; ++mt) {
-        const int qrow = qbase + 16 * mt + lr, h = qrow / r.n, i = qrow - h * r.n, pos = basepos + i;
-        const bool live = qrow < QR && i < nlive && pos >= 0 && pos < r.max_ctx;
-        lim[mt] = live ? pos : -1;
-        const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
-        u32x4 v[KW];
+    {
+        u32x4 v[MQ][KW];
         float top = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KW; ++ks) {
-            v[ks] = live ? *(const u32x4*)(qp + 8 * ks) : (u32x4){0, 0, 0, 0};
+        for (int mt = 0; mt < MQ; ++mt) {
+            const int qrow = qbase + 16 * mt + lr, h = qrow / r.n, i = qrow - h * r.n, pos = basepos + i;
+            const bool live = qrow < QR && i < nlive && pos >= 0 && pos < r.max_ctx;
+            lim[mt] = live ? pos : -1;
+            const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(v[ks][e] << 16)), fabsf(__uint_as_float(v[ks][e] & 0xffff0000u))));
+            for (int ks = 0; ks < KW; ++ks) {
+                v[mt][ks] = live ? *(const u32x4*)(qp + 8 * ks) : (u32x4){0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(v[mt][ks][e] << 16)), fabsf(__uint_as_float(v[mt][ks][e] & 0xffff0000u))));
+            }
         }
-        top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-        top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+        top = wave_max(top);
         const int ex = min(max(267 - (int)(__float_as_uint(top) >> 23), 1), 253);
         const float up = __uint_as_float((uint32_t)ex << 23);
-        float sum = 0.f;
+        unit = cs * __uint_as_float((uint32_t)(254 - ex) << 23) * 16777216.f;
 #pragma unroll
-        for (int ks = 0; ks < KW; ++ks)
+        for (int mt = 0; mt < MQ; ++mt) {
+            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = __uint_as_float(v[ks][e] << 16) * up, b = __uint_as_float(v[ks][e] & 0xffff0000u) * up;
-                sum += a + b;
-                const float f = e & 1 ? 0.0625f : 1.f;
-                qf[mt][ks][2 * e] = (_Float16)(a * f);
-                qf[mt][ks][2 * e + 1] = (_Float16)(b * f);
-            }
-        sum += __shfl_xor(sum, 16, WAVE);
-        sum += __shfl_xor(sum, 32, WAVE);
-        qsum[mt] = sum * 5.9604644775390625e-08f;                  // 2^-24
-        rcs[mt] = cs * __uint_as_float((uint32_t)(254 - ex) << 23) * 16777216.f;
+            for (int ks = 0; ks < KW; ++ks)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = __uint_as_float(v[mt][ks][e] << 16) * up, b = __uint_as_float(v[mt][ks][e] & 0xffff0000u) * up;
+                    sum += a + b;
+                    const float f = e & 1 ? 0.0625f : 1.f;
+                    qf[mt][ks][2 * e] = (_Float16)(a * f);
+                    qf[mt][ks][2 * e + 1] = (_Float16)(b * f);
+                }
+            sum += __shfl_xor(sum, 16, WAVE);
+            sum += __shfl_xor(sum, 32, WAVE);
+            qsum[mt] = sum * 5.9604644775390625e-08f;              // 2^-24
+        }
     }
+    // a tile's groups in fp32, a lane a group: (s, z) of a key in score units, (s, z) of a
+    // value with the operand's 1/16
+    float2* par = (float2*)(s_par + 64 * w);
+    const float par_s = lane < 32 ? unit : lane & 2 ? 0.0625f : 1.f, par_z = lane < 32 ? unit : 1.f;
 
     float ref[MQ], lsum[MQ], zsum[MQ];
     floatx4 o[MQ][NBD], oc[MQ];
@@ -529,6 +645,10 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         for (int nb = 0; nb < NBD; ++nb) o[mt][nb] = (floatx4){0.f, 0.f, 0.f, 0.f};
     }
 
+    floatx4 mid8[MQ];                                              // what the centre 8 takes off a score's products
+#pragma unroll
+    for (int mt = 0; mt < MQ; ++mt) mid8[mt] = (floatx4){-8.f * qsum[mt], -8.f * qsum[mt], -8.f * qsum[mt], -8.f * qsum[mt]};
+
     // a word's codes in fp16 (see above)
     auto codes = [](uint32_t x) {
         const uint32_t y = x >> 8;
@@ -536,7 +656,8 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     };
     auto block = [&](int blk, const uint8_t* t, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
-        alignas(16) uint32_t kc[2][KW], kp[8], vp[8], vc[NBD];
+        alignas(16) uint32_t kc[2][KW], vc[NBD];
+        const uint32_t raw = *(const uint32_t*)(t + 32 * D + 4 * lane);
         if constexpr (D == 128) {
             *(u32x4*)kc[0] = *(const u32x4*)(t + 16 * lane);
             *(u32x4*)kc[1] = *(const u32x4*)(t + 1024 + 16 * lane);
@@ -545,11 +666,13 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
             *(u32x2*)kc[0] = *(const u32x2*)kr;
             *(u32x2*)kc[1] = *(const u32x2*)(kr + 128);
         }
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-            *(u32x4*)(kp + e) = *(const u32x4*)(t + 32 * D + 32 * cq + 4 * e);
-            *(u32x4*)(vp + e) = *(const u32x4*)(t + 32 * D + 128 + 32 * cq + 4 * e);
-        }
+        const float step = __uint_as_float(raw << 16);
+        par[lane] = make_float2(step * par_s, __uint_as_float(raw & 0xffff0000u) * par_z);
+        // (values that are all alike have s = 0: P needs a bound of its own)
+        const bool tiny = __builtin_amdgcn_ballot_w64(lane >= 32 && !(step >= 0x1p-60f)) != 0;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         floatx4 st[MQ][2];
 #pragma unroll
         for (int pt = 0; pt < 2; ++pt)
@@ -558,38 +681,37 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
                 const half8 kf = codes(kc[pt][k]);
 #pragma unroll
                 for (int mt = 0; mt < MQ; ++mt)
-                    st[mt][pt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[mt][k], k ? st[mt][pt] : (floatx4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                    st[mt][pt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[mt][k], k ? st[mt][pt] : mid8[mt], 0, 0, 0);
             }
         float ks[8], kz[8], vs[8], vz[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ks[e] = __uint_as_float(kp[e] << 16);
-            kz[e] = __builtin_fmaf(-8.f, ks[e], __uint_as_float(kp[e] & 0xffff0000u));
-            vs[e] = __uint_as_float(vp[e] << 16);
-            vz[e] = __uint_as_float(vp[e] & 0xffff0000u);
+        for (int e = 0; e < 8; e += 2) {
+            const float4 a = *(const float4*)(par + 8 * cq + e), b = *(const float4*)(par + 32 + 8 * cq + e);
+            ks[e] = a.x, kz[e] = a.y, ks[e + 1] = a.z, kz[e + 1] = a.w;
+            vs[e] = b.x, vz[e] = b.y, vs[e + 1] = b.z, vz[e + 1] = b.w;
         }
         half8 pf[MQ];
 #pragma unroll
         for (int mt = 0; mt < MQ; ++mt) {
-            float u[8], p[8], pv[8];
+            float p[8], pv[8];
             bool seen[8];
             const int last = min(pe - 1, lim[mt]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                u[e] = __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], kz[e] * qsum[mt]);
-                seen[e] = !MASKED || blk + 8 * cq + e <= last;     // what a row does not see may hold anything
-            }
+            for (int e = 0; e < 8; ++e) seen[e] = !MASKED || blk + 8 * cq + e <= last;   // what a row does not see may hold anything
+            auto score = [&](int e, float from) { return __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], __builtin_fmaf(kz[e], qsum[mt], from)); };
             auto weights = [&] {
-                float top = 0.f, most = 0.f;
+                float top = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float a = __builtin_fmaf(rcs[mt], u[e], -ref[mt]);
+                    const float a = score(e, -ref[mt]);
                     p[e] = __builtin_amdgcn_exp2f(seen[e] ? a : -INFINITY);
                     pv[e] = p[e] * (seen[e] ? vs[e] : 0.f);
                     top = fmaxf(top, pv[e]);
-                    most = fmaxf(most, p[e]);
                 }
-                return fmaxf(top, most * 0x1p-85f);
+                if (tiny)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, p[e] * 0x1p-60f);
+                return top;
             };
             float top = weights();
             // (infinite references, of infinite scores, stay)
@@ -597,8 +719,9 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
                 float bm = KV4_REF0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float a = rcs[mt] * u[e];
-                    if (seen[e]) bm = fmaxf(bm, fmaxf(a + __builtin_amdgcn_logf(vs[e]), a - 85.f));
+                    float v = vs[e];
+                    asm volatile("" : "+v"(v));                    // keeps the logarithms on this path
+                    if (seen[e]) bm = fmaxf(bm, score(e, fmaxf(__builtin_amdgcn_logf(v), -60.f)));
                 }
                 bm = fmaxf(bm, __shfl_xor(bm, 16, WAVE));
                 bm = fmaxf(bm, __shfl_xor(bm, 32, WAVE));
@@ -624,7 +747,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
             for (int e = 0; e < 8; ++e) {
                 lsum[mt] += p[e];
                 zsum[mt] = __builtin_fmaf(p[e], seen[e] ? vz[e] : 0.f, zsum[mt]);
-                pr[e >> 1][e & 1] = e & 2 ? pv[e] * 0.0625f : pv[e];
+                pr[e >> 1][e & 1] = pv[e];
             }
             u32x4 pk;
 #pragma unroll
@@ -714,52 +837,68 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     }
 }
 
-// The items of a sequence merged in order; a work-group takes one row, its
-// threads the heads' dims four at a time.
-__global__ void __launch_bounds__(256) k_kv4_combine(rows_t r, att_plan plan, int n_q, int n_kv, int D, const float* part,
+// The items of a sequence merged: a work-group takes one row and head, D/4 lanes an
+// item, so 1024/D items at a time; its partial sums are added in a fixed order.
+// One round trip to memory is all it takes up to 8 * 1024/D items (one sequence's
+// 64 items by one thread a dim: 21 us).
+template <int D>
+__global__ void __launch_bounds__(256) k_kv4_combine(rows_t r, att_plan plan, int n_q, int n_kv, const float* part,
                                                      void* out, int out_t, long long out_ld)
 {
-    const int idx = blockIdx.x, b = idx / r.n, i = idx - b * r.n;
+    constexpr int D4 = D / 4, NG = 256 / D4, CB = 8;              // lanes an item, items at a time, loads in flight
+    __shared__ float2 s_ml[NG];
+    __shared__ float4 s_o[NG][D4];
+    const int idx = blockIdx.x / n_q, hq = blockIdx.x - idx * n_q, b = idx / r.n, i = idx - b * r.n;
     if (r.lim && i >= r.lim[b]) return;
     const size_t row = r.row0 ? r.row0[b] + i : idx;
     const int2 sq = plan.seq[b];
     const int nch = sq.y;
     if (nch <= 1) return;                                         // the attention wrote the output
-    const int G = n_q / n_kv, QR = G * r.n, D4 = D / 4;
-    const int t = blockIdx.y * 256 + threadIdx.x;
-    if (t >= n_q * D4) return;
-    const int hq = t / D4, d = 4 * (t - hq * D4), kvh = hq / G;
+    const int G = n_q / n_kv, QR = G * r.n, kvh = hq / G, d4 = threadIdx.x % D4, gp = threadIdx.x / D4;
     const float* pp = part + part_at(sq.x, n_kv, kvh, QR, (hq - kvh * G) * r.n + i, D);
     const size_t st = (size_t)n_kv * QR * (D + 4);                // to the next item
-    constexpr int CB = 8;                                         // items whose loads go out together
-    float mm = -INFINITY, ls = 0.f;
+    float mm = KV4_REF0, ls = 0.f;
     float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < nch; c0 += CB) {
+    auto add = [&](float m, float l, float4 x) {
+        const float f = m == mm ? 1.f : __builtin_amdgcn_exp2f(m - mm);
+        ls += l * f;
+        os = make_float4(os.x + x.x * f, os.y + x.y * f, os.z + x.z * f, os.w + x.w * f);
+    };
+    auto raise_to = [&](float m) {
+        const float f = mm == m ? 1.f : __builtin_amdgcn_exp2f(mm - m);
+        ls *= f;
+        os = make_float4(os.x * f, os.y * f, os.z * f, os.w * f);
+        mm = m;
+    };
+    for (int c0 = gp; c0 < nch; c0 += CB * NG) {
         float2 ml[CB];
         float4 x[CB];
 #pragma unroll
         for (int u = 0; u < CB; ++u) {
-            const float* pc = pp + min(c0 + u, nch - 1) * st;
+            const float* pc = pp + min(c0 + u * NG, nch - 1) * st;
             ml[u] = *(const float2*)pc;
-            x[u] = *(const float4*)(pc + 4 + d);
+            x[u] = *(const float4*)(pc + 4 + 4 * d4);
         }
         float bm = mm;
 #pragma unroll
         for (int u = 0; u < CB; ++u) bm = fmaxf(bm, ml[u].x);
-        const float f0 = mm == bm ? 1.f : __builtin_amdgcn_exp2f(mm - bm);
-        ls *= f0;
-        os = make_float4(os.x * f0, os.y * f0, os.z * f0, os.w * f0);
-        mm = bm;
+        raise_to(bm);
 #pragma unroll
-        for (int u = 0; u < CB; ++u) {
-            if (c0 + u >= nch) break;
-            const float f = ml[u].x == mm ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - mm);
-            ls += ml[u].y * f;
-            os = make_float4(os.x + x[u].x * f, os.y + x[u].y * f, os.z + x[u].z * f, os.w + x[u].w * f);
-        }
+        for (int u = 0; u < CB; ++u)
+            if (c0 + u * NG < nch) add(ml[u].x, ml[u].y, x[u]);
     }
+    if (d4 == 0) s_ml[gp] = make_float2(mm, ls);
+    s_o[gp][d4] = os;
+    __syncthreads();
+    if (gp) return;
+    float bm = mm;
+#pragma unroll
+    for (int u = 1; u < NG; ++u) bm = fmaxf(bm, s_ml[u].x);
+    raise_to(bm);
+#pragma unroll
+    for (int u = 1; u < NG; ++u) add(s_ml[u].x, s_ml[u].y, s_o[u][d4]);
     const float4 v = ls == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(os.x / ls, os.y / ls, os.z / ls, os.w / ls);
-    kv4_store4(out, out_t, row * out_ld + (size_t)hq * D + d, v);
+    kv4_store4(out, out_t, row * out_ld + (size_t)hq * D + 4 * d4, v);
 }
 
 // NaN groups in the positions [kv_len, kv_len + span) of every layer and KV head
@@ -800,11 +939,16 @@ void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, in
                        uint16_t* q_out, const kv4_rope& ro, hipStream_t s)
 {
     const int ngr = (r.n + 14) / 8;                               // groups of 8 that n rows can touch
-    const long long kvw = (long long)r.B * ngr * 2 * n_kv, rpw = 512 / D;
-    const long long qw = q_out ? ((long long)r.B * r.n * n_q + rpw - 1) / rpw : 0;
+    // KV heads a wave: one, or as many as leave KV4_APPEND_WAVES waves
+    const long long one = (long long)r.B * ngr * 2 * n_kv;
+    int hpw = one > KV4_APPEND_WAVES ? (int)min((long long)n_kv, one / KV4_APPEND_WAVES) : 1;
+    const int hw = (n_kv + hpw - 1) / hpw;
+    hpw = (n_kv + hw - 1) / hw;                                   // evenly
+    const long long kvw = (long long)r.B * ngr * 2 * ((n_kv + hpw - 1) / hpw), qh = QPASS * 512 / D;
+    const long long qw = q_out ? (long long)r.B * r.n * ((n_q + qh - 1) / qh) : 0;
     const unsigned blocks = (unsigned)((kvw + qw + 3) / 4);
-    if (D == 128) k_kv4_append<T, 128><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, (int)kvw);
-    else k_kv4_append<T, 64><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, (int)kvw);
+    if (D == 128) k_kv4_append<T, 128><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, hpw, (int)kvw);
+    else k_kv4_append<T, 64><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, hpw, (int)kvw);
 }
 template void launch_kv4_append<float>(const rows_t&, const kv4_geom&, int, int, int, kv4_src<float>, kv4_src<float>,
                                        kv4_src<float>, uint16_t*, const kv4_rope&, hipStream_t);
@@ -851,7 +995,8 @@ void launch_kv4_attention(const rows_t& r, const att_plan& pl, const kv4_geom& g
 void launch_kv4_combine(const rows_t& r, const att_plan& pl, int n_q, int n_kv, int D, const float* part, void* out,
                         act_t out_t, long long out_ld, hipStream_t s)
 {
-    k_kv4_combine<<<dim3(r.B * r.n, (n_q * D / 4 + 255) / 256), 256, 0, s>>>(r, pl, n_q, n_kv, D, part, out, (int)out_t, out_ld);
+    if (D == 128) k_kv4_combine<128><<<r.B * r.n * n_q, 256, 0, s>>>(r, pl, n_q, n_kv, part, out, (int)out_t, out_ld);
+    else k_kv4_combine<64><<<r.B * r.n * n_q, 256, 0, s>>>(r, pl, n_q, n_kv, part, out, (int)out_t, out_ld);
 }
 
 void launch_kv4_poison(int B, const int32_t* slots, const int32_t* kv_len, int span, const kv4_geom& g, int n_layers, int n_kv,
