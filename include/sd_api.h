@@ -203,7 +203,7 @@ typedef struct {
     uint32_t* flags;            /* uint32[5] or NULL */
     int32_t n_pages, page_size, pages_per_seq;  /* page_size: a multiple of 32, pages_per_seq * page_size >= max_ctx */
     int32_t n_layers, n_kv, head_dim;           /* head_dim 64 or 128 */
-    int32_t max_slots, max_ctx;
+    int32_t max_slots, max_ctx;                 /* max_ctx up to 2^24 */
 } sd_kv4_cache;
 
 /* Bytes of a page: n_layers * n_kv * page_size * (head_dim + 8); 0 for

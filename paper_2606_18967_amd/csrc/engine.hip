@@ -481,14 +481,15 @@ static sd_status check_rope(const sd_rope_cfg* c)
     return SD_OK;
 }
 
-constexpr int KV4_MAX_CTX = 1 << 30;
+constexpr int ROPE_MAX_POS = 1 << 30;
+constexpr int KV4_MAX_CTX = 1 << 24;     // the plan's chunk lengths stay below 2^31 in 32-bit arithmetic
 
 extern "C" sd_status sd_rope_table(const sd_rope_cfg* cfg, int32_t n_pos, float* table, void* stream)
 {
     sd_status st = check_rope(cfg);
     if (st != SD_OK) return st;
     if (!table || ((uintptr_t)table & 7)) return fail(SD_E_INVAL, "table is NULL or not 8-byte aligned");
-    if (n_pos < 1 || n_pos > KV4_MAX_CTX) return fail(SD_E_INVAL, "n_pos=%d outside [1, %d]", n_pos, KV4_MAX_CTX);
+    if (n_pos < 1 || n_pos > ROPE_MAX_POS) return fail(SD_E_INVAL, "n_pos=%d outside [1, %d]", n_pos, ROPE_MAX_POS);
     launch_rope_table(*cfg, n_pos, table, (hipStream_t)stream);
     return launched("sd_rope_table");
 }
@@ -608,6 +609,8 @@ static sd_status kv4_att_plan(const sd_kv4_cache* c, int B, int n, int n_q, att_
     if ((double)B * n * n_q > 1e9 || (double)(n_q / c->n_kv) * n > 4e6 || B > 65535)
         return fail(SD_E_UNSUPPORTED, "B=%d, n=%d, n_q=%d are too many for one call", B, n, n_q);
     *p = attention_plan(B, n, n_q, c->n_kv, c->max_ctx, 0);
+    if (!p->whole && (double)B * c->max_ctx >= 2147483648.0)
+        return fail(SD_E_UNSUPPORTED, "B * max_ctx = %.0f positions are too many for one call", (double)B * c->max_ctx);
     *plan_bytes = align256(attention_plan_bytes(B, c->n_kv));
     *bytes = *plan_bytes + (p->whole ? 0 : (size_t)p->max_items * n * n_q * (c->head_dim + 4) * 4);
     return SD_OK;
@@ -640,7 +643,8 @@ extern "C" sd_status sd_kv4_attention(const sd_kv4_cache* c, int32_t layer, int3
     const hipStream_t s = (hipStream_t)stream;
     float* part = (float*)((char*)workspace + pb);
     attention_plan_bind(p, workspace, B);
-    launch_attention_plan(r, p, s);
+    if (kv4_plans_itself(p, B)) p.item = nullptr;
+    else launch_attention_plan(r, p, s);
     launch_kv4_attention(r, p, g, n_q, c->n_kv, c->head_dim, (const uint16_t*)q, q_ld, scale, part, out, ACT_BF16, out_ld, s);
     if (!p.whole) launch_kv4_combine(r, p, n_q, c->n_kv, c->head_dim, part, out, ACT_BF16, out_ld, s);
     return launched("sd_kv4_attention");

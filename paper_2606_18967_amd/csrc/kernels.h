@@ -69,6 +69,27 @@ struct att_plan {
 };
 // the launch geometry of B sequences x n rows (no device pointers)
 att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32);
+constexpr int PLAN_UNIT = 32;       // chunk lengths are multiples of a wave's block
+#ifndef ATT_FULL_CHUNK
+#define ATT_FULL_CHUNK 512
+#endif
+// The candidate chunk lengths of contexts of `sum` positions in all and `top` in the
+// longest: between the even share and the longest context, denser near the share
+// (with little context in all, a quarter of the target's work-groups: shorter chunks
+// would be all prologue).
+struct plan_cut {
+    int base, more;
+    __device__ int at(int k) const { return base + (more * (k * k) + 63 * 63 - 1) / (63 * 63) * PLAN_UNIT; }
+};
+__device__ __forceinline__ plan_cut plan_candidates(int sum, int top, const att_plan& pl)
+{
+    const int few = max(pl.target / 4, 1);
+    const int even = (sum + pl.target - 1) / pl.target, fewer = (sum + few - 1) / few;
+    const int share = max(max(even, min(fewer, ATT_FULL_CHUNK)), pl.min_chunk);
+    const int longest = max((top + PLAN_UNIT - 1) / PLAN_UNIT * PLAN_UNIT, pl.min_chunk);
+    const int base = min((share + PLAN_UNIT - 1) / PLAN_UNIT * PLAN_UNIT, longest);
+    return plan_cut{base, (longest - base) / PLAN_UNIT};
+}
 size_t attention_plan_bytes(int max_slots, int n_kv);
 void attention_plan_bind(att_plan& p, void* buf, int max_slots);
 
@@ -218,10 +239,13 @@ void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, in
                        uint16_t* q_out, const kv4_rope& ro, hipStream_t s);
 void launch_kv4_read(const rows_t& r, const kv4_geom& g, int n_kv, int D, const int32_t* start, uint16_t* k_out,
                      uint16_t* v_out, hipStream_t s);
-// part: attention_part_floats() floats; then the combine, unless plan.whole
+// plan.item NULL: the plan is made by the attention itself, which it can where every
+// sequence is an item in order, or there are up to 64 (kv4_plans_itself); plan.seq is
+// then written for the combine.  part: attention_part_floats() floats; then the combine, unless plan.whole
 void launch_kv4_attention(const rows_t& r, const att_plan& plan, const kv4_geom& g, int n_q, int n_kv, int D, const uint16_t* q,
                           long long q_ld, float scale, float* part, void* out, act_t out_t, long long out_ld, hipStream_t s,
                           hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
+inline bool kv4_plans_itself(const att_plan& p, int B) { return p.whole ? p.in_order : B <= 64; }
 void launch_kv4_combine(const rows_t& r, const att_plan& plan, int n_q, int n_kv, int D, const float* part, void* out,
                         act_t out_t, long long out_ld, hipStream_t s);
 void launch_kv4_poison(int B, const int32_t* slots, const int32_t* kv_len, int span, const kv4_geom& g, int n_layers, int n_kv,

@@ -454,6 +454,71 @@ __device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, i
     return (((size_t)item * n_kv + kvh) * QR + qrow) * (D + 4);
 }
 
+// The item of a work-group without a plan in memory (plan.item NULL), as
+// launch_attention_plan would make it: the sequence itself where every one is an
+// item in order, else, of up to 64 sequences (a lane each), the cut whose chunk
+// length is the shortest of 64 candidates that makes at most `target` items.  A
+// wave needs a microsecond for it, where a launch before the attention and the
+// way through memory take four.  nch also tells the combine (plan.seq).
+__device__ att_item own_item(const rows_t& r, const att_plan& pl, int item)
+{
+    const int lane = threadIdx.x & 63, b = pl.whole ? item : lane;
+    att_item it = {0, -1, 0, 0, 0, 0, 0, 0};
+    if (b < r.B) {
+        it.row0 = b * r.n;
+        it.slot = r.slots[b];
+        const int nl = r.lim ? r.lim[b] : r.n;
+        it.nlive = min(max(nl, 0), r.n);
+        if (nl != it.nlive) raise(r.err, ERR_LEN);
+        it.nch = 1;
+        if (it.slot >= 0 && it.slot < r.max_slots) {
+            it.basepos = r.kv_len[it.slot];
+            it.ctx = (int)max(0ll, min((long long)it.basepos + it.nlive, (long long)r.max_ctx));
+        }
+        it.p1 = it.ctx;
+    }
+    if (pl.whole) return it;
+    int sum = it.ctx, top = it.ctx;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        sum += __shfl_xor(sum, o, WAVE);
+        top = max(top, __shfl_xor(top, o, WAVE));
+    }
+    const plan_cut c = plan_candidates(sum, top, pl);
+    const int ck = c.at(lane);
+    const float rc = 1.f / (float)ck;
+    // chunks of ctx positions, at most some hundred: one correction makes the quotient exact
+    auto chunks = [](int ctx, int ch, float rc) {
+        int q = (int)((float)ctx * rc);
+        q += q * ch < ctx;
+        return max(q, 1);
+    };
+    int cnt = 0;
+    for (int s = 0; s < r.B; ++s) cnt += chunks(__builtin_amdgcn_readlane(it.ctx, s), ck, rc);
+    const uint64_t fits = __builtin_amdgcn_ballot_w64(cnt <= min(pl.target, pl.max_items));
+    const int ch = c.at(fits ? (int)__builtin_ctzll(fits) : 63);
+    const int nch = b < r.B ? chunks(it.ctx, ch, 1.f / (float)ch) : 0;
+    int upto = nch;                                                // inclusive sum over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto, o, WAVE);
+        if (lane >= o) upto += v;
+    }
+    const uint64_t mine = __builtin_amdgcn_ballot_w64(upto > item);
+    att_item none = {0, -1, 0, 0, 0, 0, 0, 0};
+    if (!mine) return none;                                        // past the last item
+    const int s = __builtin_ctzll(mine);
+    it.nch = nch;
+    auto from = [&](int v) { return __builtin_amdgcn_readlane(v, s); };
+    const int first = from(upto) - from(nch);
+    it = att_item{from(it.row0), from(it.slot), from(it.basepos), from(it.ctx), 0, 0, from(it.nch), from(it.nlive)};
+    const int len = ((it.ctx + it.nch - 1) / it.nch + PLAN_UNIT - 1) / PLAN_UNIT * PLAN_UNIT;
+    it.p0 = min((item - first) * len, it.ctx);
+    it.p1 = min(it.p0 + len, it.ctx);
+    if (item == first && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.z == 0) pl.seq[s] = make_int2(first, it.nch);
+    return it;
+}
+
 // Work-group (item, KV head, slice of 16 MQ query rows) covers the positions
 // [p0, p1) of its item (att_plan); its four waves take the tiles of 32 positions
 // in turn.  With q the query, c the codes of a position and (s, z) its group,
@@ -476,6 +541,7 @@ __device__ __forceinline__ size_t part_at(int item, int n_kv, int kvh, int QR, i
 // lost at 2^-24 of a row's largest and not earlier (P itself stays below 2^75 where
 // s is smaller than 2^-60).  Sums and statistics in fp32.
 constexpr float KV4_REF0 = -1e30f;     // the reference of a row that has seen no position
+constexpr int RING = 2;                // tiles a wave has in LDS or on the way (three and four: the same times)
 
 // 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
 // `lds` on; non-temporal.  The compiler's wait counts do not see them.
@@ -493,7 +559,7 @@ __device__ __forceinline__ void wait_tiles()
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-template <int D, int MQ, int RING>
+template <int D, int MQ>
 __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4_geom g, int n_q, int n_kv,
                                                                    const uint16_t* q, long long q_ld, float cs,
                                                                    float* part, att_plan plan, void* out, int out_t,
@@ -504,14 +570,13 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     constexpr int LDO = D + 4;       // LDS row stride of the merge
     constexpr int TB = tile_bytes(D), PIECES = D / 32 + 1;
     constexpr int BUF = 4 * RING * TB > 4 * 16 * LDO * 4 ? 4 * RING * TB : 4 * 16 * LDO * 4;
-    static_assert(PIECES * (RING - 1) < 64, "vmcnt range");
     __shared__ __attribute__((aligned(1024))) uint8_t s_buf[BUF];  // the waves' rings, then the merge
     __shared__ float2 s_par[4 * 64];
     __shared__ float s_ml[4][2][16];
     float (*s_o)[16 * LDO] = (float (*)[16 * LDO])s_buf;
 
     const int item = blockIdx.y, kvh = blockIdx.x, zsl = blockIdx.z;
-    const att_item it = plan.item[item];
+    const att_item it = plan.item ? plan.item[item] : own_item(r, plan, item);
     if (it.nch == 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(it.row0), slot = __builtin_amdgcn_readfirstlane(it.slot);
     const int basepos = __builtin_amdgcn_readfirstlane(it.basepos);
@@ -767,17 +832,13 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         for (int mt = 0; mt < MQ; ++mt) oc[mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(mid, pf[mt], oc[mt], 0, 0, 0);
     };
     // a tile waits for its own pieces; once it is used, its place is filled with the tile RING further
-    int at = 0;
     auto tile = [&](int i, auto masked) {
-        const int later = nt - 1 - i;
-        if (later >= RING - 1) wait_tiles<PIECES * (RING - 1)>();
-        else if (RING > 3 && later == 2) wait_tiles<PIECES * 2>();
-        else if (RING > 2 && later == 1) wait_tiles<PIECES>();
+        const int at = i % RING;
+        if (i + 1 < nt) wait_tiles<PIECES>();                      // all but the next tile's
         else wait_tiles<0>();
         if (there >> (i & 31) & 1) block(wq0 + 128 * i, s_buf + w * (RING * TB) + at * TB, masked);   // else no page: nothing to see
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // read before the place is filled again
         if (i + RING < nt) issue(i + RING, at);
-        at = at + 1 == RING ? 0 : at + 1;
     };
     // the tiles that every row sees as a whole, then the others
     const int whole = min(nt, max(0, (min(pe, all + 1) - wq0 + 96) >> 7));
@@ -976,10 +1037,10 @@ static void kv4_attn_d(const rows_t& r, const att_plan& pl, const kv4_geom& g, i
         else kern<<<grid, block, 0, s>>>(r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
     };
     switch (pl.mq) {
-        case 1: go(k_kv4_attn<D, 1, 4>); break;
-        case 2: go(k_kv4_attn<D, 2, 4>); break;
-        case 3: go(k_kv4_attn<D, 3, 4>); break;
-        default: go(k_kv4_attn<D, 4, 4>); break;
+        case 1: go(k_kv4_attn<D, 1>); break;
+        case 2: go(k_kv4_attn<D, 2>); break;
+        case 3: go(k_kv4_attn<D, 3>); break;
+        default: go(k_kv4_attn<D, 4>); break;
     }
 }
 

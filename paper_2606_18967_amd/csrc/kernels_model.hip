@@ -81,10 +81,6 @@ template <> __device__ __forceinline__ float4 load4<uint16_t>(const uint16_t* p)
 // is resident at once: the kernel takes 5.3, 5.6, 5.0 and 6.1 us with the plans
 // of 16, 28, 64 and 200 sequences (7.5, 8.1, 10.3 and 13.5 otherwise; 5.1 to 5.4
 // without a plan).
-#ifndef ATT_FULL_CHUNK
-#define ATT_FULL_CHUNK 512
-#endif
-constexpr int PLAN_UNIT = 32;       // chunk lengths are multiples of a wave's block
 constexpr int PLAN_SEQS = 512;      // sequences planned in LDS (more are always whole and in order)
 
 __device__ void make_att_plan(const rows_t& r, const att_plan& pl)
@@ -152,22 +148,14 @@ __device__ void make_att_plan(const rows_t& r, const att_plan& pl)
         sum = w ? sum + s_sum[w] : s_sum[0];
         top = w ? max(top, s_top[w]) : s_top[0];
     }
-    // candidate k: between the even share and the longest context, denser near the share
-    // (with little context in all, a quarter of the target's work-groups: shorter chunks would be all prologue)
-    const int few = max(pl.target / 4, 1);
-    const int even = (sum + pl.target - 1) / pl.target, fewer = (sum + few - 1) / few;
-    const int share = max(max(even, min(fewer, ATT_FULL_CHUNK)), pl.min_chunk);
-    const int longest = max((top + PLAN_UNIT - 1) / PLAN_UNIT * PLAN_UNIT, pl.min_chunk);
-    const int base = min((share + PLAN_UNIT - 1) / PLAN_UNIT * PLAN_UNIT, longest);
-    const int more = (longest - base) / PLAN_UNIT;
-    auto cand = [&](int k) { return base + (more * (k * k) + 63 * 63 - 1) / (63 * 63) * PLAN_UNIT; };
-    const int ck = cand(lane);
+    const plan_cut cut = plan_candidates(sum, top, pl);
+    const int ck = cut.at(lane);
     int cnt = 0;
     for (int b = wv; b < r.B; b += nt >> 6) cnt += max(1u, (unsigned)(s_it[b].ctx + ck - 1) / (unsigned)ck);
     if (wv < r.B) atomicAdd(&s_cnt[lane], cnt);
     __syncthreads();
     const uint64_t fits = __builtin_amdgcn_ballot_w64(s_cnt[lane] <= min(pl.target, pl.max_items));
-    const int ch = cand(fits ? (int)__builtin_ctzll(fits) : 63);
+    const int ch = cut.at(fits ? (int)__builtin_ctzll(fits) : 63);
     if (wv == 0) {                                             // items in the sequences' order
         int items = 0;
         for (int b0 = 0; b0 < r.B; b0 += 64) {
