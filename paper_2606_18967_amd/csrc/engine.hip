@@ -608,7 +608,7 @@ static sd_status kv4_att_plan(const sd_kv4_cache* c, int B, int n, int n_q, att_
     if (n_q < 1 || n_q % c->n_kv) return fail(SD_E_INVAL, "n_q=%d must be a positive multiple of n_kv=%d", n_q, c->n_kv);
     if ((double)B * n * n_q > 1e9 || (double)(n_q / c->n_kv) * n > 4e6 || B > 65535)
         return fail(SD_E_UNSUPPORTED, "B=%d, n=%d, n_q=%d are too many for one call", B, n, n_q);
-    *p = attention_plan(B, n, n_q, c->n_kv, c->max_ctx, 0);
+    *p = attention_plan(B, n, n_q, c->n_kv, c->max_ctx, 0, true);
     if (!p->whole && (double)B * c->max_ctx >= 2147483648.0)
         return fail(SD_E_UNSUPPORTED, "B * max_ctx = %.0f positions are too many for one call", (double)B * c->max_ctx);
     *plan_bytes = align256(attention_plan_bytes(B, c->n_kv));
@@ -818,7 +818,7 @@ static void forward(sd_engine e, const workspace& ws, bool draft, int B, const i
     const act_t at = act_of(e, draft);
     const int qkvN = (c.n_q + 2 * c.n_kv) * c.head_dim;
     const int pcls = draft ? T_Q4 : T_PROJ;
-    att_plan plan = attention_plan(B, n, c.n_q, c.n_kv, e->max_ctx, e->f32);
+    att_plan plan = attention_plan(B, n, c.n_q, c.n_kv, e->max_ctx, e->f32, e->kv4);
     attention_plan_bind(plan, e->plan, e->max_slots);
     int S;
     { tscope t(e, T_MISC, s);

@@ -65,10 +65,12 @@ struct att_plan {
     bool whole;            // every sequence is one item: no combine
     bool in_order;         // and the items are in the sequences' order
     bool kv_first;         // the new K/V rows are stored by a launch before the attention (bf16 cache)
-    int mq, zs;            // 16-row query tiles per work-group, query-row slices
+    int mq, zs;            // 16-row query tiles per work-group (by_rows: per wave), query-row slices
+    bool by_rows;          // 4-bit cache: the waves divide the rows instead of the positions
 };
 // the launch geometry of B sequences x n rows (no device pointers)
-att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32);
+// (kv4: of the 4-bit cache's attention; its items are as many)
+att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32, bool kv4 = false);
 constexpr int PLAN_UNIT = 32;       // chunk lengths are multiples of a wave's block
 #ifndef ATT_FULL_CHUNK
 #define ATT_FULL_CHUNK 512

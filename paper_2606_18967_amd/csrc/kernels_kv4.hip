@@ -36,18 +36,21 @@ __device__ __forceinline__ void raise(uint32_t* err, int kind)
 
 // ------------------------------------------------------------------ rotary table
 // table[p][i] = mul (cos p f_i, sin p f_i) in fp64, rounded once.  A work-group
-// makes ROPE_PB positions of every pair from the sines and cosines of 8 coarse
-// and 8 fine angles a pair, cos(a + b) = cos a cos b - sin a sin b: a quarter of
-// the transcendental work, which bounds the kernel, for one more rounding in fp64.
-constexpr int ROPE_FINE = 8, ROPE_PB = ROPE_FINE * 8;
-
-__global__ void __launch_bounds__(256) k_rope_table(sd_rope_cfg c, double lo, double hi, double mul, int n_pos,
+// makes FINE^2 positions of every pair from the sines and cosines of FINE coarse and
+// FINE fine angles a pair, cos(a + b) = cos a cos b - sin a sin b: with FINE 16 an
+// eighth of the transcendental work, which would bound the kernel, for one more
+// rounding in fp64.  What bounds it is a work-group's chain of pow, sincos and two
+// barriers, so a short table takes FINE 8, which makes more and shorter groups
+// (2048 x 32 pairs 4.6 against 6.4 us; 131072 x 64 22.4 against 18.5, the store
+// of 67 MB alone 13).
+template <int FINE>
+__global__ void __launch_bounds__(512) k_rope_table(sd_rope_cfg c, double lo, double hi, double mul, int n_pos,
                                                     float2* table)
 {
     __shared__ double s_f[128];
-    __shared__ double2 s_a[8][128], s_b[ROPE_FINE][128];
-    const int np = c.rot_dim / 2, p0 = blockIdx.x * ROPE_PB;
-    for (int i = threadIdx.x; i < np; i += 256) {
+    __shared__ double2 s_a[FINE * 128], s_b[FINE * 128];
+    const int np = c.rot_dim / 2, p0 = blockIdx.x * FINE * FINE;
+    for (int i = threadIdx.x; i < np; i += 512) {
         double f = pow(c.theta, -2.0 * i / c.rot_dim);
         if (c.scaling == SD_ROPE_LINEAR) {
             f = f / c.factor;
@@ -61,18 +64,19 @@ __global__ void __launch_bounds__(256) k_rope_table(sd_rope_cfg c, double lo, do
         s_f[i] = f;
     }
     __syncthreads();
-    for (int t = threadIdx.x; t < 16 * np; t += 256) {
+    for (int t = threadIdx.x; t < 2 * FINE * np; t += 512) {
         const int k = t / np, i = t - k * np;
+        const bool coarse = k < FINE;
         double sn, cs;
-        sincos((k < 8 ? (double)(p0 + k * ROPE_FINE) : (double)(k - 8)) * s_f[i], &sn, &cs);
-        if (k < 8) s_a[k][i] = make_double2(cs * mul, sn * mul);
-        else s_b[k - 8][i] = make_double2(cs, sn);
+        sincos((coarse ? (double)p0 + k * FINE : (double)(k - FINE)) * s_f[i], &sn, &cs);
+        if (coarse) s_a[t] = make_double2(cs * mul, sn * mul);
+        else s_b[t - FINE * np] = make_double2(cs, sn);
     }
     __syncthreads();
-    const int live = min(ROPE_PB, n_pos - p0);
-    for (int t = threadIdx.x; t < live * np; t += 256) {
+    const int live = min(FINE * FINE, n_pos - p0);
+    for (int t = threadIdx.x; t < live * np; t += 512) {
         const int p = t / np, i = t - p * np;
-        const double2 a = s_a[p / ROPE_FINE][i], b = s_b[p % ROPE_FINE][i];
+        const double2 a = s_a[p / FINE * np + i], b = s_b[p % FINE * np + i];
         table[(size_t)p0 * np + t] = make_float2((float)(a.x * b.x - a.y * b.y), (float)(a.y * b.x + a.x * b.y));
     }
 }
@@ -541,7 +545,6 @@ __device__ att_item own_item(const rows_t& r, const att_plan& pl, int item)
 // lost at 2^-24 of a row's largest and not earlier (P itself stays below 2^75 where
 // s is smaller than 2^-60).  Sums and statistics in fp32.
 constexpr float KV4_REF0 = -1e30f;     // the reference of a row that has seen no position
-constexpr int RING = 2;                // tiles a wave has in LDS or on the way (three and four: the same times)
 
 // 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
 // `lds` on; non-temporal.  The compiler's wait counts do not see them.
@@ -559,7 +562,12 @@ __device__ __forceinline__ void wait_tiles()
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-template <int D, int MQ>
+//
+// ROWS, for many query rows: the four waves take 16 MQ rows each instead, and every
+// tile, which they fetch together into one ring (a quarter of its codes each; the
+// groups each for itself): the cache is read once for 64 MQ rows and nothing is
+// merged.
+template <int D, int MQ, bool ROWS>
 __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4_geom g, int n_q, int n_kv,
                                                                    const uint16_t* q, long long q_ld, float cs,
                                                                    float* part, att_plan plan, void* out, int out_t,
@@ -568,12 +576,14 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     constexpr int KW = D / 32;       // code words of a lane's part of a K row: k-steps of S
     constexpr int NBD = D / 16;      // 16-row blocks of O^T, code words of a lane's V
     constexpr int LDO = D + 4;       // LDS row stride of the merge
-    constexpr int TB = tile_bytes(D), PIECES = D / 32 + 1;
-    constexpr int BUF = 4 * RING * TB > 4 * 16 * LDO * 4 ? 4 * RING * TB : 4 * 16 * LDO * 4;
-    __shared__ __attribute__((aligned(1024))) uint8_t s_buf[BUF];  // the waves' rings, then the merge
+    constexpr int TB = tile_bytes(D), PIECES = ROWS ? 2 : D / 32 + 1;   // a wave's loads of a tile
+    constexpr int RING = ROWS ? 3 : 2;                             // tiles in LDS or on the way (one more: the same times)
+    constexpr int SLOT = ROWS ? 32 * D + 4 * 256 : TB;             // a ring's place: the tile, or its codes and four times its groups
+    constexpr int RINGS = ROWS ? RING * SLOT : 4 * RING * SLOT, MERGE = ROWS ? 0 : 4 * 16 * LDO * 4;
+    constexpr int STEP = ROWS ? 32 : 128;                          // positions between a wave's tiles
+    __shared__ __attribute__((aligned(1024))) uint8_t s_buf[RINGS > MERGE ? RINGS : MERGE];   // the rings, then the merge
     __shared__ float2 s_par[4 * 64];
     __shared__ float s_ml[4][2][16];
-    float (*s_o)[16 * LDO] = (float (*)[16 * LDO])s_buf;
 
     const int item = blockIdx.y, kvh = blockIdx.x, zsl = blockIdx.z;
     const att_item it = plan.item ? plan.item[item] : own_item(r, plan, item);
@@ -582,33 +592,37 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     const int basepos = __builtin_amdgcn_readfirstlane(it.basepos);
     const int p0 = __builtin_amdgcn_readfirstlane(it.p0), p1 = __builtin_amdgcn_readfirstlane(it.p1);
     const int nlive = __builtin_amdgcn_readfirstlane(it.nlive);
-    const int G = n_q / n_kv, QR = G * r.n, qbase = zsl * 16 * MQ;
+    const int G = n_q / n_kv, QR = G * r.n;
+    constexpr int SROWS = ROWS ? 64 * MQ : 16 * MQ;                // the slice's rows, and the wave's
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qslice = zsl * SROWS, qbase = ROWS ? qslice + 16 * MQ * w : qslice;
     // a slice of rows of one head that all lie past the sequence's
-    if (nlive == 0 || (qbase % r.n >= nlive && qbase % r.n + 16 * MQ <= r.n)) return;
+    if (nlive == 0 || (qslice % r.n >= nlive && qslice % r.n + SROWS <= r.n)) return;
     if (p0 == 0 && zsl == 0 && kvh == 0 && threadIdx.x == 0) {
         if (slot < 0 || slot >= r.max_slots) raise(r.err, ERR_SLOT);
         else if (basepos < 0 || basepos > r.max_ctx - nlive) raise(r.err, ERR_CTX);
     }
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int cq = lane >> 4, lr = lane & 15;
-    // the last position that a live row of the slice sees, and up to where all of its rows see everything
-    int pe = p1, all = basepos;
-    {
-        const int last = min(qbase + 16 * MQ, QR) - 1, i = last % r.n;
-        if (last - i <= qbase) {                              // rows of one head
-            pe = min(p1, basepos + min(i + 1, nlive));
-            all = basepos + qbase % r.n;
-        }
-    }
+    // past the last position that a live row of rows [q0, q0 + rows) sees
+    auto seen_to = [&](int q0, int rows) {
+        const int last = min(q0 + rows, QR) - 1, i = last % r.n;
+        if (last < q0) return p0;
+        return last - i > q0 ? p1 : q0 % r.n >= nlive ? p0 : min(p1, basepos + min(i + 1, nlive));   // several heads, one
+    };
+    const int pe = seen_to(qbase, 16 * MQ), pslice = seen_to(qslice, SROWS);
+    // up to where all of the wave's rows see everything
+    const int all = qbase % r.n + 16 * MQ <= r.n ? basepos + qbase % r.n : basepos;
 
-    // tile i of the wave is at positions wq0 + 128 i
-    const int wq0 = p0 + 32 * w;
+    // tile i of the wave is at positions wq0 + STEP i; nt tiles are fetched, of which it uses `own`
+    const int wq0 = ROWS ? p0 : p0 + 32 * w;
     const bool usable = slot >= 0 && slot < r.max_slots;           // else p0 == p1 == 0: no tile
-    const int nt = usable && wq0 < pe ? (pe - wq0 + 127) >> 7 : 0;
-    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_buf + w * (RING * TB);
+    const int nt = usable ? max(pslice - wq0 + STEP - 1, 0) / STEP : 0, own = ROWS ? min(nt, max(pe - wq0 + STEP - 1, 0) / STEP) : nt;
+    const uint8_t* slots_at = s_buf + (ROWS ? 0 : w * (RING * SLOT));
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)slots_at;
     const uint8_t* head = g.pages + kvh * g.HS;
     // a lane's pieces of a tile: K row 8 (lr/4) + 4 pt + lr%4, words (D/32) cq + 0..; V group cq, words NBD lr + 0..
-    uint32_t src[PIECES];
+    constexpr int NSRC = D / 32 + 1;
+    uint32_t src[NSRC];
     if constexpr (D == 128) {
         src[0] = (8 * (lr >> 2) + (lr & 3)) * 64 + cq * 16;
         src[1] = src[0] + 256;
@@ -618,7 +632,11 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         src[0] = 16 * lane;
         src[1] = 1024 + 16 * lane;
     }
-    src[PIECES - 1] = 32 * D + 4 * lane;                           // the params: 64 lanes x 4 bytes
+    src[NSRC - 1] = 32 * D + 4 * lane;                             // the groups: 64 lanes x 4 bytes
+    if constexpr (ROWS) {                                          // the wave's quarter of the codes (of 64 dims 32 lanes of it)
+        if constexpr (D == 128) src[0] = w == 0 ? src[0] : w == 1 ? src[1] : w == 2 ? src[2] : src[3];
+        else src[0] = 512 * w + 16 * lane;
+    }
     // the pages of the tiles [kw, kw + 128), lane l holding those of kw + l and
     // kw + 64 + l (-1: missing): one table load in 128 tiles
     int pgw[2] = {-1, -1}, kw = -(1 << 20);
@@ -628,24 +646,31 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
             kw = i;
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-                const int bj = wq0 + (i + 64 * hf + lane) * 128;
-                pgw[hf] = bj < pe ? kv4_page(g, slot, bj / g.P) : -1;
-                if (pgw[hf] < 0 && bj < pe && r.err) ((volatile __attribute__((address_space(1))) uint32_t*)r.err)[ERR_PAGE] = 1u;
+                const int bj = wq0 + (i + 64 * hf + lane) * STEP;
+                pgw[hf] = bj < pslice ? kv4_page(g, slot, bj / g.P) : -1;
+                if (pgw[hf] < 0 && bj < pslice && r.err) ((volatile __attribute__((address_space(1))) uint32_t*)r.err)[ERR_PAGE] = 1u;
             }
         }
-        const int j = i - kw, blk = wq0 + 128 * i, in = __builtin_amdgcn_readfirstlane(blk % g.P);
+        const int j = i - kw, blk = wq0 + STEP * i, in = __builtin_amdgcn_readfirstlane(blk % g.P);
         const int pa = __builtin_amdgcn_readlane(pgw[0], j & 63), pb = __builtin_amdgcn_readlane(pgw[1], j & 63);
         const int pg = j < 64 ? pa : pb;
         there = (there & ~(1u << (i & 31))) | (uint32_t)(pg >= 0) << (i & 31);
         // no page: the first tile of the pool is fetched and not used, so that every tile counts alike
         const uint8_t* t = head + (pg < 0 ? 0 : pg * g.PS + (in >> 5) * (long long)TB);
-        const uint32_t to = ring + at * TB;
+        const uint32_t to = ring + at * SLOT;
+        if constexpr (ROWS) {
+            if (D == 128 || lane < 32) tile_dma16(t, src[0], to + 8 * D * w);
+            tile_dma4(t, src[NSRC - 1], to + 32 * D + 256 * w);
+        } else {
 #pragma unroll
-        for (int k = 0; k < PIECES - 1; ++k) tile_dma16(t, src[k], to + 1024 * k);
-        tile_dma4(t, src[PIECES - 1], to + 32 * D);
+            for (int k = 0; k < NSRC - 1; ++k) tile_dma16(t, src[k], to + 1024 * k);
+            tile_dma4(t, src[NSRC - 1], to + 32 * D);
+        }
     };
+    // (the barrier that opens a tile of a common ring frees the one before)
+    constexpr int AHEAD = ROWS ? RING - 1 : RING;
 #pragma unroll
-    for (int u = 0; u < RING; ++u)
+    for (int u = 0; u < AHEAD; ++u)
         if (u < nt) issue(u, u);
 
     // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7 times the power of two that
@@ -722,7 +747,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     auto block = [&](int blk, const uint8_t* t, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
         alignas(16) uint32_t kc[2][KW], vc[NBD];
-        const uint32_t raw = *(const uint32_t*)(t + 32 * D + 4 * lane);
+        const uint32_t raw = *(const uint32_t*)(t + 32 * D + (ROWS ? 256 * w : 0) + 4 * lane);
         if constexpr (D == 128) {
             *(u32x4*)kc[0] = *(const u32x4*)(t + 16 * lane);
             *(u32x4*)kc[1] = *(const u32x4*)(t + 1024 + 16 * lane);
@@ -832,46 +857,76 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         for (int mt = 0; mt < MQ; ++mt) oc[mt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(mid, pf[mt], oc[mt], 0, 0, 0);
     };
     // a tile waits for its own pieces; once it is used, its place is filled with the tile RING further
-    auto tile = [&](int i, auto masked) {
-        const int at = i % RING;
-        if (i + 1 < nt) wait_tiles<PIECES>();                      // all but the next tile's
+    auto tile = [&](int i, auto masked, bool use) {
+        if (nt - 1 - i >= AHEAD - 1) wait_tiles<PIECES * (AHEAD - 1)>();
         else wait_tiles<0>();
-        if (there >> (i & 31) & 1) block(wq0 + 128 * i, s_buf + w * (RING * TB) + at * TB, masked);   // else no page: nothing to see
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // read before the place is filled again
-        if (i + RING < nt) issue(i + RING, at);
+        if constexpr (ROWS) {
+            lds_barrier();                                         // everyone's pieces are in, and the last tile is done with
+            if (i + AHEAD < nt) issue(i + AHEAD, (i + AHEAD) % RING);
+        }
+        if (use && there >> (i & 31) & 1) block(wq0 + STEP * i, slots_at + i % RING * SLOT, masked);   // else no page: nothing to see
+        if constexpr (!ROWS) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // read before the place is filled again
+            if (i + AHEAD < nt) issue(i + AHEAD, i % RING);
+        }
     };
     // the tiles that every row sees as a whole, then the others
-    const int whole = min(nt, max(0, (min(pe, all + 1) - wq0 + 96) >> 7));
+    const int whole = min(own, max(0, (min(pe, all + 1) - wq0 + STEP - 32) / STEP));
     int i = 0;
-    for (; i < whole; ++i) tile(i, std::false_type());
-    for (; i < nt; ++i) tile(i, std::true_type());
+    for (; i < whole; ++i) tile(i, std::false_type(), true);
+    for (; i < nt; ++i) tile(i, std::true_type(), i < own);
 
-    // merge the four waves, 16 query rows at a time
 #pragma unroll
     for (int mt = 0; mt < MQ; ++mt) {
         lsum[mt] += __shfl_xor(lsum[mt], 16, WAVE);
         lsum[mt] += __shfl_xor(lsum[mt], 32, WAVE);
         zsum[mt] += __shfl_xor(zsum[mt], 16, WAVE);
         zsum[mt] += __shfl_xor(zsum[mt], 32, WAVE);
+    }
+    // four of row lr's sums, the dims NBD (4 cq + i) + nb + 0..3
+    auto sums = [&](int mt, int i, int nb) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(o[mt][nb + e][i] - oc[mt][i], 16777216.f, zsum[mt]);
+        return make_float4(v[0], v[1], v[2], v[3]);
+    };
+    // dims d.. of a row of the slice: to the partial results, or the output itself
+    auto put = [&](int qrow, int d, float top, float l, float4 x) {
+        const int h = qrow / r.n, i = qrow - h * r.n;
+        if (qrow >= QR || i >= nlive) return;
+        if (it.nch > 1) {
+            float* pp = part + part_at(item, n_kv, kvh, QR, qrow, D);
+            if (d == 0) *(float2*)pp = make_float2(top, l);
+            *(float4*)(pp + 4 + d) = x;
+            return;
+        }
+        const bool none = l == 0.f || basepos + i < 0 || basepos + i >= r.max_ctx;
+        kv4_store4(out, out_t, (size_t)(row0 + i) * out_ld + (size_t)(kvh * G + h) * D + d,
+                   none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x / l, x.y / l, x.z / l, x.w / l));
+    };
+    if constexpr (ROWS) {
+#pragma unroll
+        for (int mt = 0; mt < MQ; ++mt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int nb = 0; nb < NBD; nb += 4)
+                    put(qbase + 16 * mt + lr, NBD * (4 * cq + i) + nb, ref[mt], lsum[mt], sums(mt, i, nb));
+        return;
+    }
+    // merge the four waves, 16 query rows at a time
+    float (*s_o)[16 * LDO] = (float (*)[16 * LDO])s_buf;
+#pragma unroll
+    for (int mt = 0; mt < MQ; ++mt) {
         __syncthreads();
         if (cq == 0) { s_ml[w][0][lr] = ref[mt]; s_ml[w][1][lr] = lsum[mt]; }
-        // lane (cq, lr) holds dims NBD (4 cq + i) + nb of row lr
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int nb = 0; nb < NBD; nb += 4)
-            {
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(o[mt][nb + e][i] - oc[mt][i], 16777216.f, zsum[mt]);
-                *(float4*)(&s_o[w][lr * LDO + NBD * (4 * cq + i) + nb]) = make_float4(v[0], v[1], v[2], v[3]);
-            }
+            for (int nb = 0; nb < NBD; nb += 4) *(float4*)(&s_o[w][lr * LDO + NBD * (4 * cq + i) + nb]) = sums(mt, i, nb);
         __syncthreads();
         for (int idx = threadIdx.x; idx < 16 * D / 4; idx += 256) {
-            const int qr = idx / (D / 4), d = 4 * (idx - qr * (D / 4)), qrow = qbase + 16 * mt + qr;
-            if (qrow >= QR) continue;
-            const int h = qrow / r.n, i = qrow - h * r.n;
-            if (i >= nlive) continue;
+            const int qr = idx / (D / 4), d = 4 * (idx - qr * (D / 4));
             float mm = s_ml[0][0][qr];
 #pragma unroll
             for (int ww = 1; ww < 4; ++ww) mm = fmaxf(mm, s_ml[ww][0][qr]);
@@ -884,16 +939,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
                 ls += s_ml[ww][1][qr] * f;
                 os = make_float4(os.x + x.x * f, os.y + x.y * f, os.z + x.z * f, os.w + x.w * f);
             }
-            if (it.nch > 1) {
-                float* pp = part + part_at(item, n_kv, kvh, QR, qrow, D);
-                if (d == 0) *(float2*)pp = make_float2(mm, ls);
-                *(float4*)(pp + 4 + d) = os;
-                continue;
-            }
-            const bool none = ls == 0.f || basepos + i < 0 || basepos + i >= r.max_ctx;
-            const size_t oi = (size_t)(row0 + i) * out_ld + (size_t)(kvh * G + h) * D + d;
-            const float4 v = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(os.x / ls, os.y / ls, os.z / ls, os.w / ls);
-            kv4_store4(out, out_t, oi, v);
+            put(qbase + 16 * mt + qr, d, mm, ls, os);
         }
     }
 }
@@ -992,7 +1038,10 @@ void launch_rope_table(const sd_rope_cfg& c, int n_pos, float* table, hipStream_
         hi = fmin(ceil(at(c.low)), c.rot_dim - 1.0);
         mul = c.attn_factor > 0 ? c.attn_factor : 0.1 * log(c.factor) + 1.0;
     }
-    k_rope_table<<<(n_pos + ROPE_PB - 1) / ROPE_PB, 256, 0, s>>>(c, lo, hi, mul, n_pos, (float2*)table);
+    auto blocks = [&](int fine) { return (n_pos + fine * fine - 1) / (fine * fine); };
+    // from 256 groups of the larger kind on, one a CU
+    if (blocks(16) >= 256) k_rope_table<16><<<blocks(16), 512, 0, s>>>(c, lo, hi, mul, n_pos, (float2*)table);
+    else k_rope_table<8><<<blocks(8), 512, 0, s>>>(c, lo, hi, mul, n_pos, (float2*)table);
 }
 
 template <typename T>
@@ -1036,11 +1085,14 @@ static void kv4_attn_d(const rows_t& r, const att_plan& pl, const kv4_geom& g, i
         if (ev0) hipExtLaunchKernelGGL(kern, grid, block, 0, s, ev0, ev1, 0, r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
         else kern<<<grid, block, 0, s>>>(r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
     };
+    if (pl.by_rows) {
+        go(k_kv4_attn<D, 2, true>);
+        return;
+    }
     switch (pl.mq) {
-        case 1: go(k_kv4_attn<D, 1>); break;
-        case 2: go(k_kv4_attn<D, 2>); break;
-        case 3: go(k_kv4_attn<D, 3>); break;
-        default: go(k_kv4_attn<D, 4>); break;
+        case 1: go(k_kv4_attn<D, 1, false>); break;
+        case 2: go(k_kv4_attn<D, 2, false>); break;
+        default: go(k_kv4_attn<D, 3, false>); break;
     }
 }
 

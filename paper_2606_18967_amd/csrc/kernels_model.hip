@@ -1221,14 +1221,29 @@ void launch_rope_kv(const rows_t& r, const float* qkv, const float* P, int S, co
                                                  (uint16_t*)c.v, c.g, layer, q_out, first, upw);
 }
 
-att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32)
+// The 4-bit cache's attention by its query rows a KV head: up to 48 in one slice of one
+// to three tiles; up to 64 in two slices of two tiles (64 sequences at 8192 positions,
+// 60 rows: 235 us, one slice of four tiles 283; 40 rows: 208 in three tiles, 229 in two
+// slices); more than that divided among a work-group's waves (4 x 509 rows behind
+// up to 1034 positions: 67 us, 139 in slices of four tiles, 84 of two).  Items are cut
+// as for the other caches, which bounds the partial results.
+constexpr int KV4_ONE_SLICE = 48, KV4_BY_ROWS = 64;
+
+att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32, bool kv4)
 {
     att_plan p = {};
     const int QR = n_q / n_kv * n;
     p.mq = QR > 48 ? 4 : (QR + 15) / 16;
     p.zs = (QR + 16 * p.mq - 1) / (16 * p.mq);
     p.min_chunk = kv_f32 ? ATT_CH : ATT_MIN_CHUNK;
-    p.target = ATT_TARGET_WGS / (n_kv * p.zs);
+    int slices = p.zs;
+    if (kv4 && QR > KV4_ONE_SLICE) {
+        p.by_rows = QR > KV4_BY_ROWS;
+        p.mq = 2;
+        p.zs = (QR + 127) / 128;
+        if (!p.by_rows) slices = p.zs = 2;
+    }
+    p.target = ATT_TARGET_WGS / (n_kv * slices);
     if (p.target < 1) p.target = 1;
     const long long cap = (long long)B * ((max_ctx + p.min_chunk - 1) / p.min_chunk);   // chunks the cache has room for
     p.max_items = B >= p.target ? B : (cap < p.target ? (int)cap : p.target);

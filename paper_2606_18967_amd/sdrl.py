@@ -183,7 +183,16 @@ def _dev(t: torch.Tensor, name: str, dtype=None, shape=None, dev=None):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the current stream's handle without the Stream object around it (2 us a call)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _ptr(t, name: str, dtype, shape, dev) -> int:
+    """A contiguous device tensor's address, checked as _dev does, in the order that is quick when all is well."""
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and (shape is None or t.shape == shape) \
+            and t.is_contiguous():
+        return t.data_ptr()
+    return _dev(t, name, dtype, shape, dev).value
 
 
 class Engine:
@@ -280,7 +289,7 @@ class Engine:
         """Prefill, draft, verify, AR step and rollback run on the 4-bit cache from here on."""
         if cache.device != self.device:
             raise ValueError(f"cache on {cache.device}, engine is on {self.device}")
-        _check(lib().sd_bind_kv4(self.h, C.byref(cache.c)))
+        _check(lib().sd_bind_kv4(self.h, cache._ref))
         self._keep_kv = cache
 
     def set_rope(self, rope: "RopeConfig"):
@@ -497,8 +506,8 @@ def rope_table(rope: RopeConfig, n_pos: int, out: torch.Tensor | None = None) ->
     """(cos, sin) of the positions [0, n_pos): fp32 [n_pos][rot_dim / 2][2] on the current device."""
     if out is None:
         out = torch.empty((n_pos, rope.rot_dim // 2, 2), dtype=torch.float32, device="cuda")
-    _check(lib().sd_rope_table(C.byref(rope.c), n_pos,
-                               _dev(out, "out", torch.float32, (n_pos, rope.rot_dim // 2, 2), _current()), _stream()))
+    _check(lib().sd_rope_table(C.byref(rope.c), n_pos, _ptr(out, "out", torch.float32, (n_pos, rope.rot_dim // 2, 2), _current()),
+                               _stream()))
     return out
 
 
@@ -536,6 +545,8 @@ class KV4Cache:
         self.flags = torch.zeros(5, dtype=torch.int32, device=self.device)
         self.c = KV4Struct(*ptrs, C.c_void_p(self.flags.data_ptr()), n_pages, self.page_size, block_table.shape[1],
                            n_layers, n_kv, head_dim, slots, max_ctx)
+        self._ref = C.byref(self.c)
+        self._ws_bytes = {}
 
     def check(self):
         """Waits for the current stream and raises what calls found out of range since the last check."""
@@ -548,14 +559,14 @@ class KV4Cache:
         raise SDError(SD_E_INVAL, "device: " + "; ".join(w for w, x in zip(what, f) if x and w))
 
 
-def _rows(t: torch.Tensor, name: str, dtype, shape, dev):
+def _rows(t, name: str, dtype, shape, dev):
     """Rows [B][n][heads][head_dim] at a common row stride: the pointer and the stride in elements."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != dev:
+    if not isinstance(t, torch.Tensor) or t.device != dev:
         raise ValueError(f"{name}: expected a tensor on {dev}")
     if t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     B, n, heads, D = shape
     st = t.stride()
     ld = st[1] if n > 1 else st[0] if B > 1 else heads * D
@@ -565,11 +576,11 @@ def _rows(t: torch.Tensor, name: str, dtype, shape, dev):
 
 
 def _kv4_args(cache: KV4Cache, slots, lens):
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"cache on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    dev = cache.device
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"cache on {dev}, the current device is cuda:{torch.cuda.current_device()}")
     B = slots.numel()
-    return B, _dev(slots, "slots", torch.int32, (B,), cache.device), \
-        _dev(lens, "lens", torch.int32, (B,), cache.device) if lens is not None else None
+    return B, _ptr(slots, "slots", torch.int32, (B,), dev), None if lens is None else _ptr(lens, "lens", torch.int32, (B,), dev)
 
 
 def kv4_append(cache: KV4Cache, layer: int, slots, k, v, q=None, q_out=None, rope=None, layout: str = "half", lens=None):
@@ -578,37 +589,36 @@ def kv4_append(cache: KV4Cache, layer: int, slots, k, v, q=None, q_out=None, rop
     "half" or "interleaved" layout, and rotates q [B][n][n_q][head_dim] into q_out (bf16).  lens [B]: rows of
     each sequence.  kv_len is not changed."""
     B, sp, lp = _kv4_args(cache, slots, lens)
-    dev, D, n = cache.device, cache.head_dim, k.shape[1]
-    if k.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"k: expected bfloat16 or float32, got {k.dtype}")
+    dev, D, n, dtype = cache.device, cache.head_dim, k.shape[1], k.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"k: expected bfloat16 or float32, got {dtype}")
     if layout not in ("half", "interleaved"):
         raise ValueError(f"layout: expected 'half' or 'interleaved', got {layout!r}")
     shape = (B, n, cache.n_kv, D)
-    (kp, k_ld), (vp, v_ld) = _rows(k, "k", k.dtype, shape, dev), _rows(v, "v", k.dtype, shape, dev)
+    (kp, k_ld), (vp, v_ld) = _rows(k, "k", dtype, shape, dev), _rows(v, "v", dtype, shape, dev)
     qp, q_ld, n_q, op = None, 0, 0, None
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if q is not None:
         n_q = q.shape[2]
-        qp, q_ld = _rows(q, "q", k.dtype, (B, n, n_q, D), dev)
-        op = _dev(q_out, "q_out", torch.bfloat16, (B, n, n_q, D), dev)
-    ra = RopeArgs(None, 0, 0, 0)
+        qp, q_ld = _rows(q, "q", dtype, (B, n, n_q, D), dev)
+        op = _ptr(q_out, "q_out", torch.bfloat16, (B, n, n_q, D), dev)
+    ra = None
     if rope is not None and rope.shape[1]:
-        ra = RopeArgs(_dev(rope, "rope", torch.float32, (rope.shape[0], rope.shape[1], 2), dev), rope.shape[0],
-                      2 * rope.shape[1], layout == "interleaved")
-    _check(lib().sd_kv4_append(C.byref(cache.c), layer, B, n, sp, lp,
-                               SD_DTYPE_BF16 if k.dtype == torch.bfloat16 else SD_DTYPE_F32, kp, k_ld, vp, v_ld, qp, q_ld,
-                               n_q, op, C.byref(ra), _stream()))
+        ra = C.byref(RopeArgs(_ptr(rope, "rope", torch.float32, (rope.shape[0], rope.shape[1], 2), dev), rope.shape[0],
+                              2 * rope.shape[1], layout == "interleaved"))
+    _check(lib().sd_kv4_append(cache._ref, layer, B, n, sp, lp, SD_DTYPE_BF16 if dtype == torch.bfloat16 else SD_DTYPE_F32,
+                               kp, k_ld, vp, v_ld, qp, q_ld, n_q, op, ra, _stream()))
 
 
 def kv4_read(cache: KV4Cache, layer: int, slots, start, k_out, v_out, lens=None):
     """The stored values of positions start[b] + i of a layer into k_out, v_out (bf16 [B][n][n_kv][head_dim])."""
     B, sp, lp = _kv4_args(cache, slots, lens)
-    n = k_out.shape[1]
+    dev, n = cache.device, k_out.shape[1]
     shape = (B, n, cache.n_kv, cache.head_dim)
-    _check(lib().sd_kv4_read(C.byref(cache.c), layer, B, n, sp, _dev(start, "start", torch.int32, (B,), cache.device), lp,
-                             _dev(k_out, "k_out", torch.bfloat16, shape, cache.device),
-                             _dev(v_out, "v_out", torch.bfloat16, shape, cache.device), _stream()))
+    _check(lib().sd_kv4_read(cache._ref, layer, B, n, sp, _ptr(start, "start", torch.int32, (B,), dev), lp,
+                             _ptr(k_out, "k_out", torch.bfloat16, shape, dev), _ptr(v_out, "v_out", torch.bfloat16, shape, dev),
+                             _stream()))
 
 
 def kv4_attention(cache: KV4Cache, layer: int, slots, q, out=None, scale: float | None = None, lens=None, workspace=None):
@@ -616,24 +626,28 @@ def kv4_attention(cache: KV4Cache, layer: int, slots, q, out=None, scale: float 
     each row's own (append them first) into out (bf16, same shape); scale defaults to 1/sqrt(head_dim).  workspace:
     a uint8 tensor of kv4_workspace_bytes, for callers that keep one (not for calls that may overlap)."""
     B, sp, lp = _kv4_args(cache, slots, lens)
-    shape = (B, q.shape[1], q.shape[2], cache.head_dim)
-    qp, q_ld = _rows(q, "q", torch.bfloat16, shape, cache.device)
+    dev, n, n_q = cache.device, q.shape[1], q.shape[2]
+    shape = (B, n, n_q, cache.head_dim)
+    qp, q_ld = _rows(q, "q", torch.bfloat16, shape, dev)
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-    op, o_ld = _rows(out, "out", torch.bfloat16, shape, cache.device)
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    op, o_ld = _rows(out, "out", torch.bfloat16, shape, dev)
     if workspace is None:
-        workspace = torch.empty(kv4_workspace_bytes(cache, B, shape[1], shape[2]), dtype=torch.uint8, device=cache.device)
-    _check(lib().sd_kv4_attention(C.byref(cache.c), layer, B, shape[1], sp, lp, shape[2], qp, q_ld,
+        workspace = torch.empty(kv4_workspace_bytes(cache, B, n, n_q), dtype=torch.uint8, device=dev)
+    _check(lib().sd_kv4_attention(cache._ref, layer, B, n, sp, lp, n_q, qp, q_ld,
                                   cache.head_dim ** -0.5 if scale is None else scale, op, o_ld,
-                                  _dev(workspace, "workspace", torch.uint8, None, cache.device), workspace.numel(), _stream()))
+                                  _ptr(workspace, "workspace", torch.uint8, None, dev), workspace.numel(), _stream()))
     return out
 
 
 def kv4_workspace_bytes(cache: KV4Cache, B: int, n: int, n_q: int) -> int:
     """Bytes of kv4_attention's workspace."""
-    nb = int(lib().sd_kv4_workspace_bytes(C.byref(cache.c), B, n, n_q))
-    if not nb:
-        raise SDError(SD_E_INVAL, lib().sd_last_error().decode(errors="replace"))
+    nb = cache._ws_bytes.get((B, n, n_q))
+    if nb is None:
+        nb = int(lib().sd_kv4_workspace_bytes(cache._ref, B, n, n_q))
+        if not nb:
+            raise SDError(SD_E_INVAL, lib().sd_last_error().decode(errors="replace"))
+        cache._ws_bytes[B, n, n_q] = nb
     return nb
 
 
