@@ -126,3 +126,53 @@ def attend(q, k, v, see, scale):
     p /= p.sum()
     val = vs[:, None] * vc + vz[:, None]
     return p @ val, 2.0 ** -8 * (p @ np.abs(vs[:, None] * vc)) + 2.0 ** -14 * (p @ np.abs(val))
+
+
+class Decoder:
+    """One sequence through the decoder in 64 bits over a 4-bit cache, with the engine's roundings of what its
+    kernels exchange: activations in bf16 (target) or fp16 (drafter), rotated queries in bf16, cached rows as their
+    codes stand for.  weights: the binding order's tensors in float64; proj[l]: (Wqkv, Wo, Wgu, Wdown) to use."""
+
+    def __init__(self, cfg, weights, proj, table, half=False):
+        self.cfg, self.w, self.proj, self.table = cfg, weights, proj, table
+        self.act = (lambda x: x.astype(np.float16).astype(np.float64)) if half else \
+            (lambda x: bf16(x.astype(np.float32)).astype(np.float64))
+
+    def norm(self, h, gain):
+        return h / np.sqrt((h * h).mean(-1, keepdims=True) + self.cfg["rms_eps"]) * gain
+
+    def forward(self, tokens, pos0, K, V, steps=None):
+        """Logits [n][vocab] of tokens at pos0.., writing their rows into K, V [L][n_kv][cap][D] (values).  With the
+        steps [L][n_kv][cap] of K and V given, their rows are there already, as the device stored them (one value near
+        a border in another code is half a step, which would hide other errors): they must stand for the rows computed
+        here to within half a step, s and z rounded to bf16, and 2e-2 of the row's largest value for the GEMM."""
+        c = self.cfg
+        nq, nkv, D, n = c["n_q"], c["n_kv"], c["head_dim"], len(tokens)
+        pos = pos0 + np.arange(n)
+        h = self.w[0][tokens]
+        for l in range(c["n_layers"]):
+            wqkv, wo, wgu, wdown = self.proj[l]
+            x = (self.act(self.norm(h, self.w[3 + 6 * l])) @ wqkv.T).astype(np.float32).reshape(n, nq + 2 * nkv, D)
+            q = bf16(rotate(x[:, :nq], self.table, pos[:, None], D, "half")).astype(np.float64)
+            for buf, y in ((K, rotate(x[:, nq:nq + nkv], self.table, pos[:, None], D, "half")), (V, x[:, nq + nkv:])):
+                if steps is not None:
+                    s = steps[0 if buf is K else 1][l][:, pos]
+                    got, y = buf[l][:, pos], y.swapaxes(0, 1).astype(np.float64)
+                    top = np.abs(y).max(-1, keepdims=True)
+                    assert (np.abs(got - y) <= 0.5 * s[..., None] + (2.0 ** -7 + 2e-2) * top).all(), (l, buf is K)
+                    continue
+                code, s, z = quantize(y)
+                buf[l][:, pos] = (z[..., None].astype(np.float64) + s[..., None].astype(np.float64) * (code - 8)).swapaxes(0, 1)
+            o = np.empty((n, nq, D))
+            for i in range(n):
+                for hh in range(nq):
+                    kk, vv = K[l][hh * nkv // nq][:pos[i] + 1], V[l][hh * nkv // nq][:pos[i] + 1]
+                    sc = kk @ q[i, hh] / math.sqrt(D)
+                    p = np.exp(sc - sc.max())
+                    o[i, hh] = p @ vv / p.sum()
+            h = h + self.act(o.reshape(n, -1)) @ wo.T
+            gu = self.act(self.norm(h, self.w[3 + 6 * l + 3])) @ wgu.T
+            g, u = gu[:, :c["ffn"]], gu[:, c["ffn"]:]
+            h = h + self.act(g / (1 + np.exp(-g)) * u) @ wdown.T
+        a = bf16(self.norm(h, self.w[1]).astype(np.float32)).astype(np.float64)
+        return a @ self.w[2].T
