@@ -45,6 +45,7 @@ def parse():
                     help="drafter format: RTN int4 symmetric (default), int4 asymmetric, int8")
     ap.add_argument("--page-size", type=int, default=0,
                     help="bind a paged KV cache with pages of this many positions, shuffled (0: dense cache)")
+    ap.add_argument("--kv4", action="store_true", help="hold the KV cache in 4 bits (pages of --page-size or 64)")
     ap.add_argument("--graph", action="store_true",
                     help="time the SD steps as replays of one captured HIP graph")
     ap.add_argument("--batch", type=int, default=0, help="sequences (default: the workload's)")
@@ -94,8 +95,8 @@ def kernel_sources_hash(files=None):
     return h.hexdigest()[:16]
 
 
-def workload_key(model, B, S, gamma, drafter, page):
-    return f"{model} B={B} S={S} gamma={gamma} {drafter} page={page}"
+def workload_key(model, B, S, gamma, drafter, page, kv4=False):
+    return f"{model} B={B} S={S} gamma={gamma} {drafter} page={page}" + (" kv4" if kv4 else "")
 
 
 # the workload the committed counter runs time (bench.py's defaults)
@@ -148,7 +149,11 @@ COUNTED = {
 DRAFTER_BYTES_PER_WEIGHT = {"w4": 0.5 + 2 / 128, "w4a": 0.5 + 3 / 128, "w8": 1 + 2 / 128}
 
 
-def algorithmic_per_launch(cfg, B, gamma, ctx, drafter="w4"):
+# the kernels of the attention classes on a 4-bit cache
+KV4_KERNEL_OF_CLASS = {"attn_decode": "k_kv4_attn<128, 1, false>", "attn_verify": "k_kv4_attn<128, 2, false>"}
+
+
+def algorithmic_per_launch(cfg, B, gamma, ctx, drafter="w4", kv4=False):
     """Bytes (HBM-bound classes) or FLOPs (MFMA-bound) one launch of each
     timing class must move or do, for a mean cached length ctx (kv_len at the
     start of the step): the sizes of what the operation reads and writes, not
@@ -160,6 +165,9 @@ def algorithmic_per_launch(cfg, B, gamma, ctx, drafter="w4"):
     # each token's projection row is read and its new K/V row written
     attn_d = B * kv_pos * (ctx + (gamma + 1) / 2) + B * (qkv_row + kv_pos)
     attn_v = B * kv_pos * (ctx + gamma + 1) + B * (gamma + 1) * (qkv_row + kv_pos)
+    if kv4:                                  # codes and groups; the rows' queries in, outputs out (the append is its own kernel)
+        attn_d = B * nkv * (d + 8) * (ctx + (gamma + 1) / 2) + B * nq * d * 4
+        attn_v = B * nkv * (d + 8) * (ctx + gamma + 1) + B * (gamma + 1) * nq * d * 4
     w_layer = H * (nq + 2 * nkv) * d + nq * d * H + 3 * H * F          # projection weights per layer
     q4 = w_layer * DRAFTER_BYTES_PER_WEIGHT[drafter] / 4                # mean drafter launch (4 per layer)
     rows_v = B * (gamma + 1)
@@ -284,7 +292,12 @@ def main():
     W = synth.make_weights(cfg, seed, dev)
     eng = sdrl.Engine(cfg, B, max_ctx, gamma)
     eng.bind_weights(W)
-    if args.page_size:
+    if args.kv4:
+        from paper_2606_18967_amd import calibrate
+        P = args.page_size or 64
+        order = torch.randperm(B * ((max_ctx + P - 1) // P), generator=torch.Generator().manual_seed(seed + 3))
+        kv_len = calibrate.bind_kv4_context(eng, S, seed + 100, P, order).kv_len
+    elif args.page_size:
         # paged cache: every sequence's pages drawn at random from one pool
         P = args.page_size
         pps = (max_ctx + P - 1) // P
@@ -407,7 +420,7 @@ def main():
     H, V, d, nkv, nq, F, L = (cfg[x] for x in ("hidden", "vocab", "head_dim", "n_kv", "n_q", "ffn", "n_layers"))
     ctx_prof = 0.5 * (kv_before + kv_after)             # mean kv_len at the start of the profiled steps
     dom = max(classes, key=lambda c: classes[c]["ms_per_step"])
-    algo = algorithmic_per_launch(cfg, B, gamma, ctx_prof, args.drafter)
+    algo = algorithmic_per_launch(cfg, B, gamma, ctx_prof, args.drafter, args.kv4)
     bound, amount = algo.get(dom, ("hbm", float("nan")))
     us = classes[dom]["us_per_launch"]
     if bound == "hbm":
@@ -416,8 +429,10 @@ def main():
         achieved, peak, unit = amount / (us * 1e-6) / 1e12, BF16_PEAK_TFLOPS, "TFLOP/s"
     roof = dict(bound=bound, achieved=round(achieved, 1), peak=peak, unit=unit,
                 frac=round(achieved / peak, 4),
-                traffic=measured_traffic(dom, workload_key(args.model, B, S, gamma, args.drafter, args.page_size)),
-                kernel=KERNEL_OF_CLASS.get(dom, dom), timing_class=dom,
+                traffic=measured_traffic(dom, workload_key(args.model, B, S, gamma, args.drafter, args.page_size,
+                                                           args.kv4)),
+                kernel=(KV4_KERNEL_OF_CLASS if args.kv4 and dom in KV4_KERNEL_OF_CLASS else KERNEL_OF_CLASS).get(dom, dom),
+                timing_class=dom,
                 algorithmic_per_launch=amount, us_per_launch=round(us, 2))
     others = {}
     for name, (b, amt) in algo.items():
@@ -427,7 +442,7 @@ def main():
 
     # ---- CPU oracle on a bounded sample of the same workload
     cpu = None
-    if not args.no_cpu_baseline and not args.page_size:
+    if not args.no_cpu_baseline and not args.page_size and not args.kv4:
         cpu = cpu_baseline(args, cfg, W, k, v, S, gamma, T, seed, args.drafter, tau, first_tok)
 
     rec = {
@@ -447,6 +462,7 @@ def main():
                                + {"w4": "int4 g128", "w4a": "asymmetric int4 g128", "w8": "int8 g128"}[args.drafter]
                                + f" drafter, B={B}, KV context {S} (random N(0,1)), gamma={gamma}, T=1.0",
                    "drafter": args.drafter, "hip_graph": bool(args.graph), "kv_page_size": args.page_size,
+                   **({"kv_cache_bits": 4} if args.kv4 else {}),
                    "batch": B, "context": S, "gamma": gamma, "temperature": T, "layers": L, "hidden": H,
                    "heads": f"{nq}q/{nkv}kv x {d}", "ffn": F, "vocab": V},
         "roofline": roof,

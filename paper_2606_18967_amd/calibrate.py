@@ -136,12 +136,36 @@ def f_eff(n: int = 8192, reps: int = 10) -> float:
     return 2.0 * n ** 3 * reps / (e0.elapsed_time(e1) * 1e-3)
 
 
+def bind_kv4_context(eng: sdrl.Engine, S: int, seed: int, page: int = 64, order=None) -> sdrl.KV4Cache:
+    """A 4-bit cache for every slot of the engine, bound, with random N(0, 1) keys (taken as rotated) and values in
+    positions [0, S) and kv_len = S; pages in the order given (a permutation), by default as they come."""
+    import torch
+    c, dev = eng.cfg, eng.device
+    per = -(-eng.max_ctx // page)
+    n = eng.max_slots * per
+    table = torch.arange(n) if order is None else order
+    cache = eng.alloc_kv4(n, page, table.to(torch.int32).reshape(eng.max_slots, per).to(dev))
+    g = torch.Generator(device=dev).manual_seed(seed)
+    slots = torch.arange(eng.max_slots, dtype=torch.int32, device=dev)
+    rows = max(1, (1 << 26) // (eng.max_slots * c["n_kv"] * c["head_dim"]))      # bounds the random rows in hand
+    for layer in range(c["n_layers"]):
+        for p in range(0, S, rows):
+            shape = (eng.max_slots, min(rows, S - p), c["n_kv"], c["head_dim"])
+            k, v = (torch.randn(shape, generator=g, device=dev) for _ in range(2))
+            cache.kv_len.fill_(p)
+            sdrl.kv4_append(cache, layer, slots, k, v)
+    cache.kv_len.fill_(S)
+    cache.check()
+    eng.bind_kv4(cache)
+    return cache
+
+
 class Sweep:
     """Times T_p, T_q, T_V with the engine's kernels on one model over a grid
-    of (B, S, gamma).  KV context is random N(0, 1) (synth.fill_kv_context);
-    kv_len is reset to S before each measurement."""
+    of (B, S, gamma).  KV context is random N(0, 1) (synth.fill_kv_context, or
+    bind_kv4_context for a 4-bit cache); kv_len is reset to S before each measurement."""
 
-    def __init__(self, cfg: dict, Bmax: int, Smax: int, gmax: int, seed: int = 2, fmt: str = "w4"):
+    def __init__(self, cfg: dict, Bmax: int, Smax: int, gmax: int, seed: int = 2, fmt: str = "w4", kv4: bool = False):
         import torch
         self.torch = torch
         self.cfg = cfg
@@ -149,9 +173,13 @@ class Sweep:
         self.W = synth.make_weights(cfg, seed, self.dev)
         self.eng = sdrl.Engine(cfg, Bmax, Smax + 12 * (gmax + 1) + 64, gmax)
         self.eng.bind_weights(self.W)
-        self.k, self.v, self.kv_len = self.eng.alloc_kv()
-        self.eng.bind_kv(self.k, self.v, self.kv_len)
-        synth.fill_kv_context(self.k, self.v, Smax, seed + 100)
+        if kv4:
+            self.cache = bind_kv4_context(self.eng, Smax, seed + 100)
+            self.kv_len = self.cache.kv_len
+        else:
+            self.k, self.v, self.kv_len = self.eng.alloc_kv()
+            self.eng.bind_kv(self.k, self.v, self.kv_len)
+            synth.fill_kv_context(self.k, self.v, Smax, seed + 100)
         self.qbuf = self.eng.refresh_drafter(fmt=fmt)
         self.seed = seed
         self.V = cfg["vocab"]
@@ -250,13 +278,13 @@ def drafter_tradeoff(cfg: dict, fmts=("w4", "w4a", "w8"), Bs=(1, 16, 64), S=2048
     return rows
 
 
-def run(cfg: dict, Bs, Ss, gammas, taus, eps=0.05, reps=8, log=print, fmt: str = "w4"):
+def run(cfg: dict, Bs, Ss, gammas, taus, eps=0.05, reps=8, log=print, fmt: str = "w4", kv4: bool = False):
     torch_started = time.time()
     F = f_eff()
     log(f"F_eff {F / 1e12:.0f} TFLOP/s")
-    base = sdrl.cost_init(cfg)
+    base = sdrl.cost_init(cfg, kv_bytes=sdrl.kv4_bytes_per_element(cfg["head_dim"]) if kv4 else 2.0)
     base.F_eff = F
-    sw = Sweep(cfg, max(Bs), max(Ss), max(gammas), fmt=fmt)
+    sw = Sweep(cfg, max(Bs), max(Ss), max(gammas), fmt=fmt, kv4=kv4)
     samples, meas = [], {}
     for S in Ss:
         for B in Bs:
@@ -291,6 +319,7 @@ def main(argv=None):
     ap.add_argument("--out", default="")
     ap.add_argument("--drafter-tradeoff", action="store_true",
                     help="only compare the drafter formats (latency against acceptance) at S = max(--S)")
+    ap.add_argument("--kv4", action="store_true", help="hold the KV cache in 4 bits")
     a = ap.parse_args(argv)
     cfg = dict(synth.TINY, dtype="bf16", name="tiny-bf16") if a.model == "TINY_BF16" else getattr(synth, a.model)
     ints = lambda s: [int(x) for x in s.split(",") if x]
@@ -304,7 +333,7 @@ def main(argv=None):
         print(txt)
         return
     res = run(cfg, ints(a.B), ints(a.S), ints(a.gamma), [float(x) for x in a.tau.split(",")], a.eps, a.reps,
-              log=lambda *x: print(*x, file=sys.stderr, flush=True))
+              log=lambda *x: print(*x, file=sys.stderr, flush=True), kv4=a.kv4)
     txt = json.dumps(res, indent=1, default=str)
     if a.out:
         with open(a.out, "w") as fh:

@@ -150,13 +150,13 @@ def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: 
 
 
 class Rollout:
-    """One model on the GPU with a dense KV cache for B sequences of up to
-    prompt + lmax positions, the drafter buffer, and flat device buffers
+    """One model on the GPU with a dense KV cache (kv4: a paged one in 4 bits)
+    for B sequences of up to prompt + lmax positions, the drafter buffer, and flat device buffers
     viewed at the live batch size and draft length of each iteration."""
 
     def __init__(self, cfg: dict, B: int, prompt: int, lmax: int, gmax: int = max(GAMMA_SET), seed: int = 3,
                  T: float = 1.0, fmt: str = "w4", graphs: bool = False, padded: bool | None = None,
-                 prefill: bool = False):
+                 prefill: bool = False, kv4: bool = False):
         import torch
         self.torch = torch
         self.cfg, self.B, self.prompt, self.gmax, self.seed, self.T, self.fmt = cfg, B, prompt, gmax, seed, T, fmt
@@ -169,8 +169,13 @@ class Rollout:
         self.eng = sdrl.Engine(cfg, B + self.spare, prompt + lmax + gmax + 2, gmax)
         self.W = synth.make_weights(cfg, seed, self.dev)
         self.eng.bind_weights(self.W)
-        self.k, self.v, self.kv_len = self.eng.alloc_kv()
-        self.eng.bind_kv(self.k, self.v, self.kv_len)
+        if kv4:
+            from . import calibrate
+            self.cache = calibrate.bind_kv4_context(self.eng, 0 if prefill else prompt, seed + 100)
+            self.kv_len = self.cache.kv_len
+        else:
+            self.k, self.v, self.kv_len = self.eng.alloc_kv()
+            self.eng.bind_kv(self.k, self.v, self.kv_len)
         self.prefill_s = None
         if prefill:
             # real prompts: `prompt` random tokens per sequence through the target (every slot, spares too)
@@ -182,7 +187,7 @@ class Rollout:
             self.eng.sync()
             self.prefill_s = time.perf_counter() - t0
             del toks
-        else:
+        elif not kv4:
             synth.fill_kv_context(self.k, self.v, prompt, seed + 100)
         self.qbuf = self.eng.refresh_drafter(fmt=fmt)
         V, dev, i32, f32 = cfg["vocab"], self.dev, torch.int32, torch.float32
@@ -372,11 +377,11 @@ def train(run_fn, policy: str, n_steps: int, lengths_fn, gset=GAMMA_SET, P=PATIE
     return out
 
 
-def calibrated_cost(cfg: dict, calib: dict):
+def calibrated_cost(cfg: dict, calib: dict, kv4: bool = False):
     """The toggle's cost model (Sec. 4.2): the architecture terms of cfg with
     the fitted parameters of calibrate.py (F_eff, BW_eff, rho_kappa, eta_D,
-    c_T, c_D, c_V)."""
-    m = sdrl.cost_init(cfg)
+    c_T, c_D, c_V), fitted on the same kind of cache."""
+    m = sdrl.cost_init(cfg, kv_bytes=sdrl.kv4_bytes_per_element(cfg["head_dim"]) if kv4 else 2.0)
     m.F_eff = float(calib["F_eff"])
     for k, v in calib["params"].items():
         setattr(m, k, float(v))
@@ -407,6 +412,7 @@ def main(argv=None):
     ap.add_argument("--graphs", action="store_true",
                     help="pad live batches to buckets of BUCKET rows and replay one captured HIP graph per "
                          "(bucket, draft length) and per AR bucket")
+    ap.add_argument("--kv4", action="store_true", help="hold the KV cache in 4 bits (paged)")
     ap.add_argument("--tau-carry", action="store_true",
                     help="carry the toggle's tau to a new draft length through the acceptance rate "
                          "(default: Algorithm 1 as written, the measured tau as it is)")
@@ -422,11 +428,11 @@ def main(argv=None):
         from . import calibrate
         log("calibrating the cost model ...")
         calib = calibrate.run(cfg, ints(a.calib_B), ints(a.calib_S), [GAMMA_SET[0]], [2.0, 3.0, 4.0], EPS, 6, log=log,
-                              fmt=a.drafter)
+                              fmt=a.drafter, kv4=a.kv4)
         calib = dict(F_eff=calib["F_eff"], params=calib["params"], agreement=calib["agreement"])
-    cost = calibrated_cost(cfg, calib)
+    cost = calibrated_cost(cfg, calib, a.kv4)
     log("building the rollout engine ...")
-    ro = Rollout(cfg, a.B, a.prompt, a.lmax, seed=a.seed, fmt=a.drafter, graphs=a.graphs, prefill=a.prefill)
+    ro = Rollout(cfg, a.B, a.prompt, a.lmax, seed=a.seed, fmt=a.drafter, graphs=a.graphs, prefill=a.prefill, kv4=a.kv4)
     if ro.prefill_s is not None:
         log(f"prefill of {a.B} x {a.prompt} tokens: {ro.prefill_s:.2f} s")
     lengths_fn = lambda t: response_lengths(a.B, a.median, a.sigma, a.lmin, a.lmax, a.seed * 1000 + t)
@@ -447,7 +453,7 @@ def main(argv=None):
     ro.close()
     L0 = lengths_fn(0)
     summary = dict(model=cfg["name"], drafter=a.drafter, B=a.B, prompt=a.prompt, tau_carry=a.tau_carry,
-                   graphs=a.graphs, prefill_s=ro.prefill_s,
+                   graphs=a.graphs, kv4=a.kv4, prefill_s=ro.prefill_s,
                    lengths=dict(median=a.median, sigma=a.sigma, lo=a.lmin, hi=a.lmax, mean_step0=float(L0.mean()),
                                 max_step0=int(L0.max())),
                    calib=dict(F_eff=calib["F_eff"], params=calib["params"]),

@@ -640,6 +640,11 @@ def kv4_attention(cache: KV4Cache, layer: int, slots, q, out=None, scale: float 
     return out
 
 
+def kv4_bytes_per_element(head_dim: int) -> float:
+    """Bytes a cached value takes in 4 bits, its share of the group included (cost_init's kv_bytes)."""
+    return 0.5 + 4.0 / head_dim
+
+
 def kv4_workspace_bytes(cache: KV4Cache, B: int, n: int, n_q: int) -> int:
     """Bytes of kv4_attention's workspace."""
     nb = cache._ws_bytes.get((B, n, n_q))

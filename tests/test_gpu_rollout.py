@@ -83,3 +83,27 @@ def test_graph_rollout_equals_padded_eager_rollout(policy, gamma):
     assert [t[4] for t in rg.trace] == [t[4] for t in re_.trace]
     assert [t[:2] for t in rg.trace] == [t[:2] for t in re_.trace]
     assert rg.graphs >= 2 and re_.graphs == 0
+
+
+@pytest.mark.parametrize("prefill,graphs", [(False, False), (True, True)])
+def test_tiny_rollout_on_a_4_bit_cache(prefill, graphs):
+    """The same rollout with the cache in 4 bits: it completes, caches every emitted token, and repeats itself."""
+    import torch
+    from paper_2606_18967_amd import rollout, sdrl
+    torch.cuda.set_device(0)
+    say(f"rollout on a 4-bit cache, prefill={prefill} graphs={graphs}")
+    ro = rollout.Rollout(rollout.MODELS["TINY_BF16"], B=6, prompt=16, lmax=40, seed=5, kv4=True, prefill=prefill, graphs=graphs)
+    L = np.array([3, 9, 1, 17, 5, 12])
+    cost = sdrl.cost_init(ro.cfg, kv_bytes=sdrl.kv4_bytes_per_element(ro.cfg["head_dim"]))
+    taus = []
+    for rep in range(2):
+        if prefill:
+            ro.kv_len.zero_()
+            toks = torch.arange(16 * ro.kv_len.numel(), dtype=torch.int32, device="cuda").reshape(-1, 16) % ro.cfg["vocab"]
+            ro.eng.prefill(torch.arange(ro.kv_len.numel(), dtype=torch.int32, device="cuda"), toks.contiguous())
+        res, st = ro.run("sd", 5, 5.0, cost, 0.05, L, step=1)
+        kv = ro.kv_len.cpu().numpy()[:6]
+        assert (kv - ro.prompt == st["gen"]).all() and (st["gen"] >= L).all()
+        taus.append((res.tau, st["gen"].tolist()))
+    assert taus[0] == taus[1]
+    ro.close()
