@@ -780,12 +780,15 @@ static void attend_kv4(sd_engine e, const workspace& ws, const rows_t& r, const 
 {
     const sd_model_cfg& c = e->c;
     const int D = c.head_dim, qd = c.n_q * D, kd = c.n_kv * D, ld = qd + 2 * kd;
-    auto src = [&](int col) { return kv4_src<float>{ws.qkv + col, (size_t)ld, ws.gpart + col, S, (size_t)r.B * r.n * ld}; };
+    auto whole = [&](int col) { return kv4_src<float>{ws.qkv + col, (size_t)ld}; };
+    auto parts = [&](int col) { return kv4_src<f32_parts>{ws.gpart + col, (size_t)ld, S, (size_t)r.B * r.n * ld}; };
     const kv4_geom g = kv4_layer(e->geo4, l);
     uint16_t* q = (uint16_t*)ws.qrot;
     { tscope t(e, T_MISC, s);
-      launch_kv4_append(r, g, c.n_q, c.n_kv, D, src(qd), src(qd + kd), src(0), kv_only ? nullptr : q,
-                        kv4_rope{e->rope, e->max_ctx, D, 0}, s); }
+      const kv4_rope ro = {e->rope, e->max_ctx, D, 0};
+      uint16_t* qo = kv_only ? nullptr : q;
+      if (S > 1) launch_kv4_append(r, g, c.n_q, c.n_kv, D, parts(qd), parts(qd + kd), parts(0), qo, ro, s);
+      else launch_kv4_append(r, g, c.n_q, c.n_kv, D, whole(qd), whole(qd + kd), whole(0), qo, ro, s); }
     if (kv_only) return;
     { kscope t(e, r.n == 1 ? T_ATTN_D : T_ATTN_V);
       launch_kv4_attention(r, plan, g, c.n_q, c.n_kv, D, q, qd, 1.f / sqrtf((float)D), ws.att_part, ws.att, at, qd, s, t.start,

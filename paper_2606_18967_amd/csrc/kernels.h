@@ -220,22 +220,27 @@ inline kv4_geom kv4_layer(kv4_geom g, int layer)
     g.pages += layer * g.LS;
     return g;
 }
-// rows of row stride ld (elements); floats may be S > 1 split-K partials P of
-// stride st
+// rows of row stride ld (elements) of floats, bf16 bits or, as f32_parts, S > 1
+// split-K partials P of stride st
+struct f32_parts {};
 template <typename T>
 struct kv4_src {
     const T* x;
     size_t ld;
-    const T* P = nullptr;
-    int S = 1;
-    size_t st = 0;
+};
+template <>
+struct kv4_src<f32_parts> {
+    const float* P;
+    size_t ld;
+    int S;
+    size_t st;
 };
 struct kv4_rope {
     const float2* table;
     int len, rot, interleaved;
 };
 void launch_rope_table(const sd_rope_cfg& c, int n_pos, float* table, hipStream_t s);
-// T: float or uint16_t (bf16 bits).  q_out NULL: K and V alone
+// T: float, uint16_t (bf16 bits) or f32_parts.  q_out NULL: K and V alone
 template <typename T>
 void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, int D, kv4_src<T> k, kv4_src<T> v, kv4_src<T> q,
                        uint16_t* q_out, const kv4_rope& ro, hipStream_t s);

@@ -82,72 +82,81 @@ __global__ void __launch_bounds__(512) k_rope_table(sd_rope_cfg c, double lo, do
 }
 
 // ------------------------------------------------------------------ append
-// Eight consecutive inputs as they are loaded, and as floats; the projection's
-// split-K partials (S > 1) are summed on read.
+// A lane's eight dims d0 .. d0 + 7 of a head as they are loaded (words w, values y).
 template <typename T> struct oct;
 template <> struct oct<float> {
-    float4 a, b;
-    __device__ __forceinline__ void load(const kv4_src<float>& x, size_t i)
+    static constexpr int NW = 8;
+    uint32_t w[NW];
+    __device__ __forceinline__ void load(const kv4_src<float>& x, size_t i) { put(*(const float4*)(x.x + i), *(const float4*)(x.x + i + 4)); }
+    __device__ __forceinline__ void put(float4 a, float4 b)
     {
-        if (x.S > 1) {
-            a = b = make_float4(0.f, 0.f, 0.f, 0.f);
-            add_splits2(a, b, x.P, x.S, x.st, i, i + 4);
-        } else {
-            a = *(const float4*)(x.x + i);
-            b = *(const float4*)(x.x + i + 4);
-        }
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[e]);
     }
-    __device__ __forceinline__ void get(float (&y)[8]) const
+    static __device__ __forceinline__ void get(const uint32_t (&w)[NW], float (&y)[8])
     {
-        y[0] = a.x, y[1] = a.y, y[2] = a.z, y[3] = a.w;
-        y[4] = b.x, y[5] = b.y, y[6] = b.z, y[7] = b.w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __uint_as_float(w[e]);
+    }
+};
+template <> struct oct<f32_parts> : oct<float> {
+    __device__ __forceinline__ void load(const kv4_src<f32_parts>& x, size_t i)
+    {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        add_splits2(a, b, x.P, x.S, x.st, i, i + 4);
+        put(a, b);
     }
 };
 template <> struct oct<uint16_t> {
-    u32x4 v;
-    __device__ __forceinline__ void load(const kv4_src<uint16_t>& x, size_t i) { v = *(const u32x4*)(x.x + i); }
-    __device__ __forceinline__ void get(float (&y)[8]) const
+    static constexpr int NW = 4;
+    uint32_t w[NW];
+    __device__ __forceinline__ void load(const kv4_src<uint16_t>& x, size_t i)
+    {
+        const u32x4 v = *(const u32x4*)(x.x + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = v[e];
+    }
+    static __device__ __forceinline__ void get(const uint32_t (&w)[NW], float (&y)[8])
     {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            y[2 * e] = __uint_as_float(v[e] << 16);
-            y[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+            y[2 * e] = __uint_as_float(w[e] << 16);
+            y[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
         }
     }
 };
 
-// A lane's eight dims d0 .. d0 + 7 of a head, and with the half layout the eight
-// that they turn with.
-template <typename T>
-struct rows8 {
-    oct<T> own, other;
-    __device__ __forceinline__ void fetch(const kv4_src<T>& x, size_t at, int d0, const kv4_rope& ro)
-    {
-        own.load(x, at + d0);
-        if (d0 < ro.rot && !ro.interleaved) other.load(x, at + (d0 < ro.rot / 2 ? d0 + ro.rot / 2 : d0 - ro.rot / 2));
-    }
-    // rotated, the products and their sum in type A, rounded to fp32; t: the lane's (cos, sin)
-    template <typename A>
-    __device__ __forceinline__ void turn(const float2 (&t)[8], int d0, const kv4_rope& ro, float (&y)[8]) const
-    {
-        own.get(y);
+// The dims rotated, the products and their sum in type A, rounded to fp32; t: the
+// lane's (cos, sin).  With the half layout a lane's dims turn with those of the lane
+// rot/16 further or before.
+template <typename A, typename T>
+__device__ __forceinline__ void turn(const oct<T>& x, const float2 (&t)[8], int d0, const kv4_rope& ro, float (&y)[8])
+{
+    x.get(x.w, y);
+    if (ro.rot == 0) return;
+    if (ro.interleaved) {
         if (d0 >= ro.rot) return;
-        if (ro.interleaved) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const A a = y[2 * j], b = y[2 * j + 1], c = t[j].x, s = t[j].y;
-                y[2 * j] = (float)(a * c - b * s);
-                y[2 * j + 1] = (float)(a * s + b * c);
-            }
-        } else {
-            float o[8];
-            other.get(o);
-            const A sg = d0 < ro.rot / 2 ? (A)-1 : (A)1;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (float)((A)y[j] * (A)t[j].x + sg * (A)o[j] * (A)t[j].y);
+        for (int j = 0; j < 4; ++j) {
+            const A a = y[2 * j], b = y[2 * j + 1], c = t[j].x, s = t[j].y;
+            y[2 * j] = (float)(a * c - b * s);
+            y[2 * j + 1] = (float)(a * s + b * c);
         }
+        return;
     }
-};
+    const bool first = d0 < ro.rot / 2;
+    const int lane = threadIdx.x & 63, from = d0 >= ro.rot ? lane : first ? lane + ro.rot / 16 : lane - ro.rot / 16;
+    uint32_t ow[oct<T>::NW];
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < oct<T>::NW; ++e) ow[e] = __shfl(x.w[e], from, WAVE);
+    x.get(ow, o);
+    if (d0 >= ro.rot) return;
+    const A sg = first ? (A)-1 : (A)1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = (float)((A)y[j] * (A)t[j].x + sg * (A)o[j] * (A)t[j].y);
+}
 // the table's entries for a lane's dims at a position
 __device__ __forceinline__ void turns(const kv4_rope& ro, int pos, int d0, float2 (&t)[8])
 {
@@ -227,11 +236,12 @@ __device__ __forceinline__ uint32_t quantize8(const float (&y)[8], bool live, ui
 
 // One wave takes the new rows among 8 consecutive positions of one KV head's K or
 // V (the words of V hold 8 positions, so a word has one writer), D/8 lanes a row;
-// further waves rotate the queries, D/8 lanes a head, QPASS times 512/D heads of a
-// row each.  K is rotated in
+// further waves rotate the queries, D/8 lanes a head, q_passes times 512/D heads of
+// a row each.  K is rotated in
 // fp64 so that its codes are those of the exact rotation (a value next to a border
 // moves by a whole step otherwise); its products are few against the row's bytes.
-constexpr int QPASS = 4;
+template <typename T>
+constexpr int q_passes() { return std::is_same<T, f32_parts>::value ? 2 : 4; }   // partials come with few rows
 constexpr int KV4_APPEND_WAVES = 4096;
 
 template <typename T, int D>
@@ -244,7 +254,7 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
     const int lw = lane % LPR, lt = lane / LPR, d0 = 8 * lw;
     if (wave >= kv_waves) {                                        // queries: QH heads of one row
         if (!q_out) return;                                        // the last work-group's waves past K and V
-        constexpr int QH = QPASS * RPW;
+        constexpr int QPASS = q_passes<T>(), QH = QPASS * RPW;
         const int qw = (n_q + QH - 1) / QH, unit = wave - kv_waves, idx = unit / qw, h0 = (unit - idx * qw) * QH + lt;
         const int b = idx / r.n, i = idx - b * r.n;
         if (b >= r.B || (r.lim && i >= r.lim[b])) return;
@@ -254,17 +264,17 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         if (slot >= 0 && slot < r.max_slots) pos = r.kv_len[slot] + r.off + i;
         const bool ok = pos >= 0 && pos < r.max_ctx && (ro.rot == 0 || pos < ro.len);
         float2 tr[8] = {};
-        rows8<T> x[QPASS] = {};
+        oct<T> x[QPASS] = {};
         if (ok) {
 #pragma unroll
             for (int ps = 0; ps < QPASS; ++ps)                     // past the last head: it again, not stored
-                x[ps].fetch(xq, row * xq.ld + (size_t)min(h0 + ps * RPW, n_q - 1) * D, d0, ro);
+                x[ps].load(xq, row * xq.ld + (size_t)min(h0 + ps * RPW, n_q - 1) * D + d0);
             turns(ro, pos, d0, tr);
         }
 #pragma unroll
         for (int ps = 0; ps < QPASS; ++ps) {
             float y[8];
-            x[ps].template turn<float>(tr, d0, ro, y);
+            turn<float>(x[ps], tr, d0, ro, y);
             if (h0 + ps * RPW < n_q)
                 *(u32x4*)(q_out + (row * n_q + h0 + ps * RPW) * D + d0) =
                     (u32x4){pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
@@ -303,13 +313,13 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         constexpr bool V = decltype(vtag)::value;
         const kv4_src<T>& src = V ? xv : xk;
         const kv4_rope rk = V ? kv4_rope{nullptr, 0, 0, 0} : ro;
-        rows8<T> next[NP] = {};
+        oct<T> next[NP] = {};
         float2 tr[NP][8] = {};
         auto fetch = [&](int h) {
 #pragma unroll
             for (int ps = 0; ps < NP; ++ps) {
                 const int pos = pg0 + ps * RPW + lt;
-                if (pos >= lo && pos < hi) next[ps].fetch(src, (row0 + (pos - base)) * src.ld + (size_t)h * D, d0, rk);
+                if (pos >= lo && pos < hi) next[ps].load(src, (row0 + (pos - base)) * src.ld + (size_t)h * D + d0);
             }
         };
         fetch(h0);
@@ -323,7 +333,7 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         for (int t = 0; t < 8; ++t)
             if (pg0 + t >= lo && pg0 + t < hi) mask |= 0xfu << nib(t);
         for (int h = h0; h < h1; ++h, tile += g.HS) {
-            rows8<T> now[NP];
+            oct<T> now[NP];
 #pragma unroll
             for (int ps = 0; ps < NP; ++ps) now[ps] = next[ps];
             if (h + 1 < h1) fetch(h + 1);
@@ -334,7 +344,7 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
                 const bool live = pos >= lo && pos < hi;
                 float y[8];
                 uint32_t code[8];
-                now[ps].template turn<double>(tr[ps], d0, rk, y);
+                turn<double>(now[ps], tr[ps], d0, rk, y);
                 const uint32_t par = quantize8<LPR>(y, live, code);
                 if (V) {
                     const int sh = nib(t);
@@ -1054,7 +1064,7 @@ void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, in
     int hpw = one > KV4_APPEND_WAVES ? (int)min((long long)n_kv, one / KV4_APPEND_WAVES) : 1;
     const int hw = (n_kv + hpw - 1) / hpw;
     hpw = (n_kv + hw - 1) / hw;                                   // evenly
-    const long long kvw = (long long)r.B * ngr * 2 * ((n_kv + hpw - 1) / hpw), qh = QPASS * 512 / D;
+    const long long kvw = (long long)r.B * ngr * 2 * ((n_kv + hpw - 1) / hpw), qh = q_passes<T>() * 512 / D;
     const long long qw = q_out ? (long long)r.B * r.n * ((n_q + qh - 1) / qh) : 0;
     const unsigned blocks = (unsigned)((kvw + qw + 3) / 4);
     if (D == 128) k_kv4_append<T, 128><<<blocks, 256, 0, s>>>(r, g, n_q, n_kv, k, v, q, q_out, ro, ngr, hpw, (int)kvw);
@@ -1062,6 +1072,8 @@ void launch_kv4_append(const rows_t& r, const kv4_geom& g, int n_q, int n_kv, in
 }
 template void launch_kv4_append<float>(const rows_t&, const kv4_geom&, int, int, int, kv4_src<float>, kv4_src<float>,
                                        kv4_src<float>, uint16_t*, const kv4_rope&, hipStream_t);
+template void launch_kv4_append<f32_parts>(const rows_t&, const kv4_geom&, int, int, int, kv4_src<f32_parts>, kv4_src<f32_parts>,
+                                           kv4_src<f32_parts>, uint16_t*, const kv4_rope&, hipStream_t);
 template void launch_kv4_append<uint16_t>(const rows_t&, const kv4_geom&, int, int, int, kv4_src<uint16_t>, kv4_src<uint16_t>,
                                           kv4_src<uint16_t>, uint16_t*, const kv4_rope&, hipStream_t);
 
