@@ -602,12 +602,12 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     const int basepos = __builtin_amdgcn_readfirstlane(it.basepos);
     const int p0 = __builtin_amdgcn_readfirstlane(it.p0), p1 = __builtin_amdgcn_readfirstlane(it.p1);
     const int nlive = __builtin_amdgcn_readfirstlane(it.nlive);
-    const int G = n_q / n_kv, QR = G * r.n;
+    // the sequence's query rows, head by head (QR of them; a stored item has room for G n)
+    const int G = n_q / n_kv, QR = G * nlive;
     constexpr int SROWS = ROWS ? 64 * MQ : 16 * MQ;                // the slice's rows, and the wave's
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qslice = zsl * SROWS, qbase = ROWS ? qslice + 16 * MQ * w : qslice;
-    // a slice of rows of one head that all lie past the sequence's
-    if (nlive == 0 || (qslice % r.n >= nlive && qslice % r.n + SROWS <= r.n)) return;
+    if (qslice >= QR) return;                                      // a slice past them
     if (p0 == 0 && zsl == 0 && kvh == 0 && threadIdx.x == 0) {
         if (slot < 0 || slot >= r.max_slots) raise(r.err, ERR_SLOT);
         else if (basepos < 0 || basepos > r.max_ctx - nlive) raise(r.err, ERR_CTX);
@@ -615,13 +615,12 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     const int cq = lane >> 4, lr = lane & 15;
     // past the last position that a live row of rows [q0, q0 + rows) sees
     auto seen_to = [&](int q0, int rows) {
-        const int last = min(q0 + rows, QR) - 1, i = last % r.n;
-        if (last < q0) return p0;
-        return last - i > q0 ? p1 : q0 % r.n >= nlive ? p0 : min(p1, basepos + min(i + 1, nlive));   // several heads, one
+        const int last = min(q0 + rows, QR) - 1, i = last % nlive;
+        return last < q0 ? p0 : last - i > q0 ? p1 : min(p1, basepos + i + 1);   // no row, rows of several heads, of one
     };
     const int pe = seen_to(qbase, 16 * MQ), pslice = seen_to(qslice, SROWS);
     // up to where all of the wave's rows see everything
-    const int all = qbase % r.n + 16 * MQ <= r.n ? basepos + qbase % r.n : basepos;
+    const int all = qbase % nlive + 16 * MQ <= nlive ? basepos + qbase % nlive : basepos;
 
     // tile i of the wave is at positions wq0 + STEP i; nt tiles are fetched, of which it uses `own`
     const int wq0 = ROWS ? p0 : p0 + 32 * w;
@@ -695,8 +694,8 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         float top = 0.f;
 #pragma unroll
         for (int mt = 0; mt < MQ; ++mt) {
-            const int qrow = qbase + 16 * mt + lr, h = qrow / r.n, i = qrow - h * r.n, pos = basepos + i;
-            const bool live = qrow < QR && i < nlive && pos >= 0 && pos < r.max_ctx;
+            const int qrow = qbase + 16 * mt + lr, h = qrow / nlive, i = qrow - h * nlive, pos = basepos + i;
+            const bool live = qrow < QR && pos >= 0 && pos < r.max_ctx;
             lim[mt] = live ? pos : -1;
             const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
 #pragma unroll
@@ -902,10 +901,10 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     };
     // dims d.. of a row of the slice: to the partial results, or the output itself
     auto put = [&](int qrow, int d, float top, float l, float4 x) {
-        const int h = qrow / r.n, i = qrow - h * r.n;
-        if (qrow >= QR || i >= nlive) return;
+        const int h = qrow / nlive, i = qrow - h * nlive;
+        if (qrow >= QR) return;
         if (it.nch > 1) {
-            float* pp = part + part_at(item, n_kv, kvh, QR, qrow, D);
+            float* pp = part + part_at(item, n_kv, kvh, G * r.n, qrow, D);
             if (d == 0) *(float2*)pp = make_float2(top, l);
             *(float4*)(pp + 4 + d) = x;
             return;
@@ -966,13 +965,14 @@ __global__ void __launch_bounds__(256) k_kv4_combine(rows_t r, att_plan plan, in
     __shared__ float2 s_ml[NG];
     __shared__ float4 s_o[NG][D4];
     const int idx = blockIdx.x / n_q, hq = blockIdx.x - idx * n_q, b = idx / r.n, i = idx - b * r.n;
-    if (r.lim && i >= r.lim[b]) return;
+    const int nlive = r.lim ? min(r.lim[b], r.n) : r.n;
+    if (i >= nlive) return;
     const size_t row = r.row0 ? r.row0[b] + i : idx;
     const int2 sq = plan.seq[b];
     const int nch = sq.y;
     if (nch <= 1) return;                                         // the attention wrote the output
     const int G = n_q / n_kv, QR = G * r.n, kvh = hq / G, d4 = threadIdx.x % D4, gp = threadIdx.x / D4;
-    const float* pp = part + part_at(sq.x, n_kv, kvh, QR, (hq - kvh * G) * r.n + i, D);
+    const float* pp = part + part_at(sq.x, n_kv, kvh, QR, (hq - kvh * G) * nlive + i, D);
     const size_t st = (size_t)n_kv * QR * (D + 4);                // to the next item
     float mm = KV4_REF0, ls = 0.f;
     float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
