@@ -572,9 +572,9 @@ extern "C" sd_status sd_kv4_append(const sd_kv4_cache* c, int32_t layer, int32_t
             return fail(SD_E_INVAL, "the rotary table must be 16-byte aligned and hold at least one position");
         ro = kv4_rope{(const float2*)rope->table, rope->len, rope->rot_dim, rope->interleaved != 0};
     }
-    // work-groups of the launch, and the 32-bit wave numbers they are made of
-    const double waves = (double)B * (n / 8 + 2) * 2 * c->n_kv + (q ? (double)B * n * n_q / 4 + 1 : 0.0);
-    if (waves > 1e9) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
+    // a launch has fewer than 2^32 threads
+    const double waves = (double)B * (n / 8 + 2) * 2 * c->n_kv + (q ? (double)B * n * (n_q / (2048 / D) + 1) : 0.0);
+    if (waves > 6e7) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
     const rows_t r = kv4_rows(*c, B, n, slots, lens);
     const kv4_geom g = kv4_layer(kv4_geom_of(*c), layer);
     const hipStream_t s = (hipStream_t)stream;
@@ -596,7 +596,7 @@ extern "C" sd_status sd_kv4_read(const sd_kv4_cache* c, int32_t layer, int32_t B
     if (st != SD_OK) return st;
     if (!start || !k_out || !v_out) return fail(SD_E_INVAL, "NULL start, k_out or v_out");
     if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return fail(SD_E_INVAL, "k_out and v_out must be 16-byte aligned");
-    if ((double)B * (n / 8 + 2) * 2 * c->n_kv > 1e9) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
+    if ((double)B * (n / 8 + 2) * 2 * c->n_kv * (c->head_dim / 8) > 4e9) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
     launch_kv4_read(kv4_rows(*c, B, n, slots, lens), kv4_layer(kv4_geom_of(*c), layer), c->n_kv, c->head_dim, start,
                     (uint16_t*)k_out, (uint16_t*)v_out, (hipStream_t)stream);
     return launched("sd_kv4_read");
@@ -663,6 +663,8 @@ extern "C" sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c)
     if (c->max_slots < e->max_slots || c->max_ctx < e->max_ctx)
         return fail(SD_E_INVAL, "the cache's max_slots and max_ctx (%d, %d) must cover the engine's (%d, %d)", c->max_slots,
                     c->max_ctx, e->max_slots, e->max_ctx);
+    if ((double)e->max_slots * e->max_ctx >= 2147483648.0)
+        return fail(SD_E_UNSUPPORTED, "max_slots * max_ctx = %.0f positions are too many", (double)e->max_slots * e->max_ctx);
     for (workspace* w : {&e->ws, &e->pf}) {
         if (!w->rows || w->qrot) continue;
         const size_t need = (size_t)w->rows * m.n_q * m.head_dim * 2;

@@ -247,6 +247,21 @@ def test_attention_batch_past_the_item_target():
     attention_case(64, 8, 8, 150, 2, base, lens, 32, 83)
 
 
+def test_attention_of_many_sequences_cut_into_items():
+    """One KV head, so fewer sequences than work-groups are wanted; more than 64 of them, lengths far apart."""
+    base = [(211 * b) % 1500 if b % 9 else 0 for b in range(100)]
+    lens = [(b * 5) % 4 for b in range(100)]
+    attention_case(64, 4, 1, 100, 3, base, lens, 64, 101, poison=True)
+    attention_case(128, 2, 1, 70, 1, base[:70], None, 32, 102)
+
+
+@pytest.mark.parametrize("n", [15, 60])
+def test_attention_of_many_rows_over_a_long_context(n):
+    """Two slices of tiles, and rows divided among the waves, each with a context cut into several items."""
+    attention_case(128, 4, 1, 2, n, [2500, 900], [n, n - 4], 64, 103 + n, poison=True)
+    attention_case(64, 4, 1, 3, n, [0, 1333, 31], None, 32, 104 + n)
+
+
 def test_attention_scale_and_loud_keys():
     attention_case(128, 4, 1, 1, 4, [200], None, 64, 85, scale=0.25, loud=6.0)
     attention_case(64, 4, 2, 1, 4, [200], None, 64, 86, scale=-0.5)
@@ -324,6 +339,54 @@ def test_device_range_errors():
     with pytest.raises(sdrl.SDError, match="rotary table"):
         cache.check()
     assert bool((q_out[:, 2:] == 0).all() and (q_out[:, :2] != 0).any())
+
+
+def test_row_counts_of_many_sequences_are_checked():
+    say("row counts")
+    cache = make_cache(1, 1, 64, 80, 64, 32, 6)
+    slots, q = i32(range(80)), torch.zeros((80, 2, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (-1, 3):
+        lens = torch.full((80,), 2, dtype=torch.int32, device="cuda")
+        lens[77] = bad
+        sdrl.kv4_attention(cache, 0, slots, q, lens=lens)
+        with pytest.raises(sdrl.SDError, match="row count"):
+            cache.check()
+
+
+def test_tensors_are_checked():
+    """What the entry points refuse before a launch."""
+    say("refusals")
+    cache = make_cache(2, 2, 64, 3, 64, 32, 7)
+    slots, lens = i32([0, 2]), i32([1, 3])
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    k, q, o = torch.zeros((2, 3, 2, 64), **bf), torch.zeros((2, 3, 4, 64), **bf), torch.zeros((2, 3, 4, 64), **bf)
+    table = sdrl.rope_table(sdrl.RopeConfig(1e4, 64), 64)
+    ws = torch.zeros(sdrl.kv4_workspace_bytes(cache, 2, 3, 4), dtype=torch.uint8, device="cuda")
+    hc = host(cache)
+    wide = torch.zeros((2, 3, 2, 72), **bf)[..., :64]                  # heads that are not contiguous
+    skew = torch.zeros((2, 4, 2, 64), **bf)[:, :3]                     # sequences at another stride than n rows
+    odd = torch.zeros(2 * 3 * 132, **bf).as_strided((2, 3, 2, 64), (396, 132, 64, 1))   # rows of 264 bytes
+    app = dict(layer=0, slots=slots, k=k, v=k, q=q, q_out=o, rope=table, lens=lens)
+    for kw in (dict(layer=2), dict(layer=-1), dict(slots=slots.long()), dict(slots=slots.cpu()), dict(slots=slots[:1]),
+               dict(lens=i32([1])), dict(lens=lens.float()), dict(k=k.half()), dict(k=k.float()), dict(v=k.float()), dict(k=wide),
+               dict(v=skew), dict(k=odd), dict(k=k[:, :2]), dict(k=k.cpu()), dict(q=None), dict(q_out=None), dict(q_out=o.float()),
+               dict(q=q.float()), dict(q_out=o[:, :, :2]), dict(rope=table[..., :1]), dict(rope=table.double()),
+               dict(rope=table[:, ::2]), dict(layout="pairs"), dict(k=k[..., :32], v=k[..., :32])):
+        with pytest.raises((ValueError, sdrl.SDError)):
+            sdrl.kv4_append(cache, **{**app, **kw})
+    att = dict(layer=0, slots=slots, q=q, out=o, lens=lens, workspace=ws)
+    for kw in (dict(layer=2), dict(slots=slots[:1]), dict(q=q.float()), dict(q=q[:, :, :3]), dict(out=o.float()),
+               dict(out=o[:, :2]), dict(workspace=ws[:-256]), dict(workspace=ws[16:]), dict(workspace=ws.cpu()),
+               dict(workspace=ws.float()), dict(scale=float("nan")), dict(lens=i32([1, 2, 3]))):
+        with pytest.raises((ValueError, sdrl.SDError)):
+            sdrl.kv4_attention(cache, **{**att, **kw})
+    rd = dict(layer=0, slots=slots, start=slots, k_out=k, v_out=k.clone(), lens=lens)
+    for kw in (dict(layer=2), dict(start=slots.long()), dict(start=slots[:1]), dict(k_out=k.float()), dict(v_out=k[:, :2]),
+               dict(k_out=wide), dict(slots=slots.cpu())):
+        with pytest.raises((ValueError, sdrl.SDError)):
+            sdrl.kv4_read(cache, **{**rd, **kw})
+    same_pool(cache, hc)
+    cache.check()
 
 
 def test_offsets_past_4_gb():

@@ -309,6 +309,12 @@ def test_device_errors_and_refusals():
         setattr(c, name, val)
         assert L.sd_bind_kv4(eng.h, C.byref(c)) == sdrl.SD_E_INVAL, name
     eng.close()
+    wide = sdrl.Engine(MHA, 2048, 1 << 20, 1)
+    c = sdrl.KV4Struct.from_buffer_copy(cache.c)
+    c.n_layers, c.n_kv, c.head_dim = MHA["n_layers"], MHA["n_kv"], MHA["head_dim"]
+    c.max_slots, c.max_ctx, c.pages_per_seq = 2048, 1 << 20, 1 << 15
+    assert L.sd_bind_kv4(wide.h, C.byref(c)) == sdrl.SD_E_UNSUPPORTED  # positions past 31 bits in all
+    wide.close()
     f32, *_ = make_engine(synth.TINY, [w.cuda() for w in synth.make_weights(synth.TINY, 1, "cpu")], 2, 64, 2)
     c = sdrl.kv4_pages(8, 2, 4, 64, 32)
     cache = sdrl.KV4Cache(c, torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda"), 64)

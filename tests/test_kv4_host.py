@@ -60,6 +60,8 @@ def test_append_is_checked():
         assert call(rope=C.byref(sdrl.RopeArgs(*args))) == INVAL, args
     big = cache(max_slots=1 << 20, max_ctx=1 << 20, pages_per_seq=1 << 15)
     assert call(big, B=1 << 20, n=1 << 20) == UNSUPPORTED
+    small = cache(max_slots=128, max_ctx=1 << 20, pages_per_seq=1 << 15, n_kv=1, head_dim=64)   # mostly query rows
+    assert call(small, B=128, n=1 << 20, n_q=1) == UNSUPPORTED
 
 
 def test_read_and_attention_are_checked():
