@@ -626,6 +626,13 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     const int wq0 = ROWS ? p0 : p0 + 32 * w;
     const bool usable = slot >= 0 && slot < r.max_slots;           // else p0 == p1 == 0: no tile
     const int nt = usable ? max(pslice - wq0 + STEP - 1, 0) / STEP : 0, own = ROWS ? min(nt, max(pe - wq0 + STEP - 1, 0) / STEP) : nt;
+    // Those that every row sees as a whole come first, each item's from another one on:
+    // sequences of a size whose pages lie in order read the same memory channels at a
+    // time otherwise (64 at 8192 positions in pages of 64, of 256: 102 and 112 us, 94 and
+    // 96 so; pages in random order 98 and 97).
+    const int whole = min(own, max(0, (min(pe, all + 1) - wq0 + STEP - 32) / STEP));
+    const int from = ROWS || whole == 0 ? 0 : item * 13 % whole;
+    auto place = [&](int i) { return ROWS || i >= whole ? i : i + from < whole ? i + from : i + from - whole; };
     const uint8_t* slots_at = s_buf + (ROWS ? 0 : w * (RING * SLOT));
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)slots_at;
     const uint8_t* head = g.pages + kvh * g.HS;
@@ -646,21 +653,21 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         if constexpr (D == 128) src[0] = w == 0 ? src[0] : w == 1 ? src[1] : w == 2 ? src[2] : src[3];
         else src[0] = 512 * w + 16 * lane;
     }
-    // the pages of the tiles [kw, kw + 128), lane l holding those of kw + l and
+    // the pages of the steps [kw, kw + 128), lane l holding those of kw + l and
     // kw + 64 + l (-1: missing): one table load in 128 tiles
     int pgw[2] = {-1, -1}, kw = -(1 << 20);
-    uint32_t there = 0;                                            // bit i % 32: tile i has a page
+    uint32_t there = 0;                                            // bit i % 32: step i's tile has a page
     auto issue = [&](int i, int at) {
         if (i < kw || i >= kw + 128) {
             kw = i;
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-                const int bj = wq0 + (i + 64 * hf + lane) * STEP;
+                const int bj = wq0 + place(i + 64 * hf + lane) * STEP;
                 pgw[hf] = bj < pslice ? kv4_page(g, slot, bj / g.P) : -1;
                 if (pgw[hf] < 0 && bj < pslice && r.err) ((volatile __attribute__((address_space(1))) uint32_t*)r.err)[ERR_PAGE] = 1u;
             }
         }
-        const int j = i - kw, blk = wq0 + STEP * i, in = __builtin_amdgcn_readfirstlane(blk % g.P);
+        const int j = i - kw, blk = wq0 + STEP * place(i), in = __builtin_amdgcn_readfirstlane(blk % g.P);
         const int pa = __builtin_amdgcn_readlane(pgw[0], j & 63), pb = __builtin_amdgcn_readlane(pgw[1], j & 63);
         const int pg = j < 64 ? pa : pb;
         there = (there & ~(1u << (i & 31))) | (uint32_t)(pg >= 0) << (i & 31);
@@ -880,14 +887,13 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
             lds_barrier();                                         // everyone's pieces are in, and the last tile is done with
             if (i + AHEAD < nt) issue(i + AHEAD, (i + AHEAD) % RING);
         }
-        if (use && there >> (i & 31) & 1) block(wq0 + STEP * i, slots_at + i % RING * SLOT, masked);   // else no page: nothing to see
+        if (use && there >> (i & 31) & 1) block(wq0 + STEP * place(i), slots_at + i % RING * SLOT, masked);   // else no page: nothing to see
         if constexpr (!ROWS) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // read before the place is filled again
             if (i + AHEAD < nt) issue(i + AHEAD, i % RING);
         }
     };
     // the tiles that every row sees as a whole, then the others
-    const int whole = min(own, max(0, (min(pe, all + 1) - wq0 + STEP - 32) / STEP));
     int i = 0;
     for (; i < whole; ++i) tile(i, std::false_type(), true);
     for (; i < nt; ++i) tile(i, std::true_type(), i < own);
