@@ -595,14 +595,14 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     __shared__ float2 s_par[4 * 64];
     __shared__ float s_ml[4][2][16];
 
-    const int item = blockIdx.y, kvh = blockIdx.x, zsl = blockIdx.z;
+    const int item = blockIdx.y, kvh = blockIdx.x, zsl = gridDim.z - 1 - blockIdx.z;   // the last rows, which see most, first
     const att_item it = plan.item ? plan.item[item] : own_item(r, plan, item);
     if (it.nch == 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(it.row0), slot = __builtin_amdgcn_readfirstlane(it.slot);
     const int basepos = __builtin_amdgcn_readfirstlane(it.basepos);
     const int p0 = __builtin_amdgcn_readfirstlane(it.p0), p1 = __builtin_amdgcn_readfirstlane(it.p1);
     const int nlive = __builtin_amdgcn_readfirstlane(it.nlive);
-    // the sequence's query rows, head by head (QR of them; a stored item has room for G n)
+    // the sequence's query rows, the G heads of a position side by side (QR of them; a stored item has room for G n)
     const int G = n_q / n_kv, QR = G * nlive;
     constexpr int SROWS = ROWS ? 64 * MQ : 16 * MQ;                // the slice's rows, and the wave's
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -615,12 +615,12 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     const int cq = lane >> 4, lr = lane & 15;
     // past the last position that a live row of rows [q0, q0 + rows) sees
     auto seen_to = [&](int q0, int rows) {
-        const int last = min(q0 + rows, QR) - 1, i = last % nlive;
-        return last < q0 ? p0 : last - i > q0 ? p1 : min(p1, basepos + i + 1);   // no row, rows of several heads, of one
+        const int last = min(q0 + rows, QR) - 1;
+        return last < q0 ? p0 : min(p1, basepos + last / G + 1);
     };
     const int pe = seen_to(qbase, 16 * MQ), pslice = seen_to(qslice, SROWS);
     // up to where all of the wave's rows see everything
-    const int all = qbase % nlive + 16 * MQ <= nlive ? basepos + qbase % nlive : basepos;
+    const int all = basepos + qbase / G;
 
     // tile i of the wave is at positions wq0 + STEP i; nt tiles are fetched, of which it uses `own`
     const int wq0 = ROWS ? p0 : p0 + 32 * w;
@@ -701,7 +701,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         float top = 0.f;
 #pragma unroll
         for (int mt = 0; mt < MQ; ++mt) {
-            const int qrow = qbase + 16 * mt + lr, h = qrow / nlive, i = qrow - h * nlive, pos = basepos + i;
+            const int qrow = qbase + 16 * mt + lr, i = qrow / G, h = qrow - i * G, pos = basepos + i;
             const bool live = qrow < QR && pos >= 0 && pos < r.max_ctx;
             lim[mt] = live ? pos : -1;
             const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
@@ -914,7 +914,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     };
     // dims d.. of a row of the slice: to the partial results, or the output itself
     auto put = [&](int qrow, int d, float top, float l, float4 x) {
-        const int h = qrow / nlive, i = qrow - h * nlive;
+        const int i = qrow / G, h = qrow - i * G;
         if (qrow >= QR) return;
         if (it.nch > 1) {
             float* pp = part + part_at(item, n_kv, kvh, G * r.n, qrow, D);
@@ -985,7 +985,7 @@ __global__ void __launch_bounds__(256) k_kv4_combine(rows_t r, att_plan plan, in
     const int nch = sq.y;
     if (nch <= 1) return;                                         // the attention wrote the output
     const int G = n_q / n_kv, QR = G * r.n, kvh = hq / G, d4 = threadIdx.x % D4, gp = threadIdx.x / D4;
-    const float* pp = part + part_at(sq.x, n_kv, kvh, QR, (hq - kvh * G) * nlive + i, D);
+    const float* pp = part + part_at(sq.x, n_kv, kvh, QR, i * G + hq - kvh * G, D);
     const size_t st = (size_t)n_kv * QR * (D + 4);                // to the next item
     float mm = KV4_REF0, ls = 0.f;
     float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
