@@ -1111,7 +1111,8 @@ static void kv4_attn_d(const rows_t& r, const att_plan& pl, const kv4_geom& g, i
         else kern<<<grid, block, 0, s>>>(r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
     };
     if (pl.by_rows) {
-        go(k_kv4_attn<D, 2, true>);
+        if (pl.mq == 1) go(k_kv4_attn<D, 1, true>);
+        else go(k_kv4_attn<D, 2, true>);
         return;
     }
     switch (pl.mq) {

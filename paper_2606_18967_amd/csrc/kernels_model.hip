@@ -1225,8 +1225,11 @@ void launch_rope_kv(const rows_t& r, const float* qkv, const float* P, int S, co
 // to three tiles; up to 64 in two slices of two tiles (64 sequences at 8192 positions,
 // 60 rows: 235 us, one slice of four tiles 283; 40 rows: 208 in three tiles, 229 in two
 // slices); more than that divided among a work-group's waves (4 x 509 rows behind
-// up to 1034 positions: 67 us, 139 in slices of four tiles, 84 of two).  Items are cut
-// as for the other caches, which bounds the partial results.
+// up to 1034 positions, 32 / 8 heads: 52 us, in slices of four tiles 139, of two 84).
+// Those take two tiles each, or one where two would leave CUs without a work-group (one
+// sequence of 300 rows: 13 us, 18 with two; of 1000: 35 and 43; of 2500, which fills
+// them: 101 and 96; 16 of 100 behind 900: 65 and 51).
+// Items are cut as for the other caches, which bounds the partial results.
 constexpr int KV4_ONE_SLICE = 48, KV4_BY_ROWS = 64;
 
 att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32, bool kv4)
@@ -1242,6 +1245,7 @@ att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32
         p.mq = 2;
         p.zs = (QR + 127) / 128;
         if (!p.by_rows) slices = p.zs = 2;
+        else if ((long long)B * n_kv * p.zs < ATT_TARGET_WGS) p.mq = 1, p.zs = (QR + 63) / 64;
     }
     p.target = ATT_TARGET_WGS / (n_kv * slices);
     if (p.target < 1) p.target = 1;

@@ -262,6 +262,12 @@ def test_attention_of_many_rows_over_a_long_context(n):
     attention_case(64, 4, 1, 3, n, [0, 1333, 31], None, 32, 104 + n)
 
 
+def test_attention_of_many_rows_that_fill_the_device():
+    """Rows divided among the waves in two tiles each, the sequences as they come and longest first."""
+    attention_case(128, 8, 4, 64, 65, [(13 * b) % 40 for b in range(64)], None, 32, 107)
+    attention_case(64, 16, 4, 130, 17, [(37 * b) % 90 for b in range(130)], [17 - b % 18 for b in range(130)], 32, 108, poison=True)
+
+
 def test_attention_scale_and_loud_keys():
     attention_case(128, 4, 1, 1, 4, [200], None, 64, 85, scale=0.25, loud=6.0)
     attention_case(64, 4, 2, 1, 4, [200], None, 64, 86, scale=-0.5)
