@@ -29,6 +29,10 @@ __device__ __forceinline__ int kv4_page(const kv4_geom& g, int slot, int lp)
     return pg >= 0 && pg < g.n_pages ? pg : -1;
 }
 
+// a first position (kv_len and the like hold anything) kept where sums with row numbers
+// stay in 32 bits; past 2^24 either way (the longest cache) no row has a place
+__device__ __forceinline__ int kv4_base(long long pos) { return (int)min(max(pos, -(1ll << 25)), 1ll << 25); }
+
 __device__ __forceinline__ void raise(uint32_t* err, int kind)
 {
     if (err) flag_error(err, kind);
@@ -261,7 +265,7 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         const size_t row = r.row0 ? r.row0[b] + i : idx;
         const int slot = r.slots[b];
         int pos = -1;
-        if (slot >= 0 && slot < r.max_slots) pos = r.kv_len[slot] + r.off + i;
+        if (slot >= 0 && slot < r.max_slots) pos = kv4_base((long long)r.kv_len[slot] + r.off) + i;
         const bool ok = pos >= 0 && pos < r.max_ctx && (ro.rot == 0 || pos < ro.len);
         float2 tr[8] = {};
         oct<T> x[QPASS] = {};
@@ -294,7 +298,7 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         if (first && nlive > 0) raise(r.err, ERR_SLOT);
         return;
     }
-    const int base = r.kv_len[slot] + r.off;
+    const int base = kv4_base((long long)r.kv_len[slot] + r.off);
     const int stop = ro.rot ? min(r.max_ctx, ro.len) : r.max_ctx;  // first position without a table row or a place
     if (first && nlive > 0 && (base < 0 || base > stop - nlive)) raise(r.err, ERR_CTX);
     // the group's positions [pg0, pg0 + 8), the rows' [lo, hi)
@@ -599,7 +603,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
     const att_item it = plan.item ? plan.item[item] : own_item(r, plan, item);
     if (it.nch == 0) return;
     const int row0 = __builtin_amdgcn_readfirstlane(it.row0), slot = __builtin_amdgcn_readfirstlane(it.slot);
-    const int basepos = __builtin_amdgcn_readfirstlane(it.basepos);
+    const int basepos = kv4_base(__builtin_amdgcn_readfirstlane(it.basepos));
     const int p0 = __builtin_amdgcn_readfirstlane(it.p0), p1 = __builtin_amdgcn_readfirstlane(it.p1);
     const int nlive = __builtin_amdgcn_readfirstlane(it.nlive);
     // the sequence's query rows, the G heads of a position side by side (QR of them; a stored item has room for G n)

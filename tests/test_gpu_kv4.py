@@ -347,6 +347,38 @@ def test_device_range_errors():
     assert bool((q_out[:, 2:] == 0).all() and (q_out[:, :2] != 0).any())
 
 
+@pytest.mark.parametrize("B", [2, 70])
+@pytest.mark.parametrize("n", [1, 4, 80])
+def test_lengths_out_of_range_end_at_once(B, n):
+    """Whatever kv_len holds: rows without a place are zeros, and no kernel walks 2^31 positions for them."""
+    say("lengths", B, n)
+    cache = make_cache(1, 1, 64, B, 128, 32, 8)
+    slots, q = i32(range(B)), torch.randn((B, n, 2, 64)).bfloat16().cuda()
+    k, q_out, out = torch.randn((B, n, 1, 64)).bfloat16().cuda(), torch.empty_like(q), torch.empty_like(q)
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for length in (-(1 << 31), -(1 << 31) + 100, -(1 << 24), -n, 128, 1 << 24, (1 << 31) - 100, (1 << 31) - 1):
+        cache.kv_len.fill_(length)
+        q_out.fill_(9.0), out.fill_(9.0)
+        start.record()
+        sdrl.kv4_append(cache, 0, slots, k, k, q, q_out)
+        sdrl.kv4_attention(cache, 0, slots, q, out)
+        end.record()
+        with pytest.raises(sdrl.SDError, match="position outside"):
+            cache.check()
+        assert bool((out == 0).all() and (q_out == 0).all()) and start.elapsed_time(end) < 100
+    if n < 4:
+        return
+    cache.kv_len.fill_(-2)                                           # rows from the third on are positions 0, 1, ..
+    sdrl.kv4_append(cache, 0, slots, k, k, q, q_out)
+    sdrl.kv4_attention(cache, 0, slots, q, out)
+    with pytest.raises(sdrl.SDError, match="position outside"):
+        cache.check()
+    assert bool((out[:, :2] == 0).all() and (q_out[:, :2] == 0).all() and (q_out[:, 2:] == q[:, 2:]).all())
+    cache.kv_len.fill_(0)
+    want = sdrl.kv4_attention(cache, 0, slots, q[:, 2:].contiguous()).float()
+    assert float((out[:, 2:].float() - want).abs().max()) <= 2.0 ** -6 * float(want.abs().max())
+
+
 def test_row_counts_of_many_sequences_are_checked():
     say("row counts")
     cache = make_cache(1, 1, 64, 80, 64, 32, 6)
