@@ -241,9 +241,15 @@ __device__ __forceinline__ uint32_t quantize8(const float (&y)[8], bool live, ui
 // One wave takes the new rows among 8 consecutive positions of one KV head's K or
 // V (the words of V hold 8 positions, so a word has one writer), D/8 lanes a row;
 // further waves rotate the queries, D/8 lanes a head, q_passes times 512/D heads of
-// a row each.  K is rotated in
-// fp64 so that its codes are those of the exact rotation (a value next to a border
-// moves by a whole step otherwise); its products are few against the row's bytes.
+// a row each.  K is rotated in fp64 so that its codes are those of the exact rotation (a
+// value next to a border moves by a whole step otherwise); its products are few
+// against the row's bytes.
+// Few rows are bound by the chain of loads length, page, row, and a V word's other
+// nibbles: a row of 32 / 8 heads of 128 takes 4.3 us, 64 x 5 rows of 40 / 8 7.5 (both
+// halves of a group's words in scattered pages).  Many are bound by memory: 16 x 1536 rows,
+// half of them there, of 32 / 8 heads 80 us (3.5 TB/s, 278 MB).  A wave to each of
+// few KV heads keeps KV4_APPEND_WAVES of them; past that a wave takes its group's heads one
+// after the other, the next one's loads under way, and positions and table entries once.
 template <typename T>
 constexpr int q_passes() { return std::is_same<T, f32_parts>::value ? 2 : 4; }   // partials come with few rows
 constexpr int KV4_APPEND_WAVES = 4096;
@@ -396,7 +402,8 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
 }
 
 // ------------------------------------------------------------------ read
-// A thread takes 8 dims of K or V of the rows among 8 consecutive positions.
+// A thread takes 8 dims of K or V of the rows among 8 consecutive positions, so a V word
+// is read once (12288 rows of 8 heads of 128: 24 us, 3.2 TB/s; one row 3.1).
 template <int D>
 __global__ void __launch_bounds__(256) k_kv4_read(rows_t r, kv4_geom g, int n_kv, uint16_t* k_out, uint16_t* v_out,
                                                   const int32_t* start, int ngr, long long total)
@@ -558,6 +565,13 @@ __device__ att_item own_item(const rows_t& r, const att_plan& pl, int item)
 // would exceed that, to where the tile's largest P s is 2^7, so small terms are
 // lost at 2^-24 of a row's largest and not earlier (P itself stays below 2^75 where
 // s is smaller than 2^-60).  Sums and statistics in fp32.
+//   What bounds it: single rows the cache's bytes (64 sequences of 32 or 40 / 8 heads of 128
+// at 2048, 8192 and 32768 positions 28, 94 and 342 us: 5.1, 6.1 and 6.7 TB/s; a launch and
+// the first tiles' way take 5); one short sequence its chain of launch, plan, page,
+// tile (2048 positions 7.7 us, the combine 4); 64 x 5 verify rows at 8192 positions
+// bytes and vector units alike (106 us, 5.4 TB/s); a prefill the vector units: 46 cycles a
+// score of 64 lanes in the softmax, 5 instructions a code word, 17 products of 16
+// cycles a 16-row tile (8 x 512 rows at 4096 positions 306 us, 840 TFLOP/s).
 constexpr float KV4_REF0 = -1e30f;     // the reference of a row that has seen no position
 
 // 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
@@ -973,7 +987,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
 // The items of a sequence merged: a work-group takes one row and head, D/4 lanes an
 // item, so 1024/D items at a time; its partial sums are added in a fixed order.
 // One round trip to memory is all it takes up to 8 * 1024/D items (one sequence's
-// 64 items by one thread a dim: 21 us).
+// 64 items 4.6 us, by one thread a dim 21), most of it the launch.
 template <int D>
 __global__ void __launch_bounds__(256) k_kv4_combine(rows_t r, att_plan plan, int n_q, int n_kv, const float* part,
                                                      void* out, int out_t, long long out_ld)
