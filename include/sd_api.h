@@ -217,7 +217,8 @@ size_t sd_kv4_page_bytes(int32_t n_layers, int32_t n_kv, int32_t head_dim, int32
  * named once in a call.  Rows are addressed as base + (b*n + i)*ld + head *
  * head_dim + d, ld in elements, with base 16-byte aligned and ld a multiple of
  * 8 (bf16) or 4 (fp32), at least heads*head_dim.  The structs are read before
- * the call returns.  Errors: SD_E_INVAL. */
+ * the call returns.  Errors: SD_E_INVAL, SD_E_UNSUPPORTED (more rows or
+ * positions than one launch takes). */
 
 /* How sd_kv4_append rotates q and k: by a table of `len` positions
  * (sd_rope_table), pairs (i, i + rot_dim/2) or, interleaved, (2i, 2i + 1) of the
