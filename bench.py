@@ -461,7 +461,7 @@ def main():
         "config": {"workload": WORKLOAD_NAMES[args.model] + ", bf16 target + "
                                + {"w4": "int4 g128", "w4a": "asymmetric int4 g128", "w8": "int8 g128"}[args.drafter]
                                + f" drafter, B={B}, KV context {S} (random N(0,1)), gamma={gamma}, T=1.0",
-                   "drafter": args.drafter, "hip_graph": bool(args.graph), "kv_page_size": args.page_size,
+                   "drafter": args.drafter, "hip_graph": bool(args.graph), "kv_page_size": P if args.kv4 else args.page_size,
                    **({"kv_cache_bits": 4} if args.kv4 else {}),
                    "batch": B, "context": S, "gamma": gamma, "temperature": T, "layers": L, "hidden": H,
                    "heads": f"{nq}q/{nkv}kv x {d}", "ffn": F, "vocab": V},
