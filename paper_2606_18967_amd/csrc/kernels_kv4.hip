@@ -247,11 +247,14 @@ __device__ __forceinline__ uint32_t quantize8(const float (&y)[8], bool live, ui
 // Few rows are bound by the chain of loads length, page, row, and a V word's other
 // nibbles: a row of 32 / 8 heads of 128 takes 4.3 us, 64 x 5 rows of 40 / 8 7.5 (both
 // halves of a group's words in scattered pages).  Many are bound by memory: 16 x 1536 rows,
-// half of them there, of 32 / 8 heads 80 us (3.5 TB/s, 278 MB).  A wave to each of
-// few KV heads keeps KV4_APPEND_WAVES of them; past that a wave takes its group's heads one
-// after the other, the next one's loads under way, and positions and table entries once.
+// half of them there, of 32 / 8 heads 80 us (3.5 TB/s, 278 MB), all of them 115 (4.8).
+// A wave takes one KV head, or where there are more than KV4_APPEND_WAVES of them its
+// group's heads one after the other, the next one's loads under way, and positions and table
+// entries once (16 x 1536 rows, 2048 and 4096 waves at least 115 us, 8192 120, a head a wave
+// always 143; 16 x 100 rows 1024 14.1, 4096 13.1).  Query passes a wave: 1, 2, 4 of
+// them 158, 129, 115 us; with few rows, as split-K partials have, 2 (64 x 5: 6.4, 4: 6.7).
 template <typename T>
-constexpr int q_passes() { return std::is_same<T, f32_parts>::value ? 2 : 4; }   // partials come with few rows
+constexpr int q_passes() { return std::is_same<T, f32_parts>::value ? 2 : 4; }
 constexpr int KV4_APPEND_WAVES = 4096;
 
 template <typename T, int D>
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
     if (wave >= kv_waves) {                                        // queries: QH heads of one row
         if (!q_out) return;                                        // the last work-group's waves past K and V
         constexpr int QPASS = q_passes<T>(), QH = QPASS * RPW;
-        const int qw = (n_q + QH - 1) / QH, unit = wave - kv_waves, idx = unit / qw, h0 = (unit - idx * qw) * QH + lt;
+        const int qw = (n_q + QH - 1) / QH, unit = wave - kv_waves, idx = unit / qw, hb = (unit - idx * qw) * QH, h0 = hb + lt;
         const int b = idx / r.n, i = idx - b * r.n;
         if (b >= r.B || (r.lim && i >= r.lim[b])) return;
         const size_t row = r.row0 ? r.row0[b] + i : idx;
@@ -278,11 +281,12 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
         if (ok) {
 #pragma unroll
             for (int ps = 0; ps < QPASS; ++ps)                     // past the last head: it again, not stored
-                x[ps].load(xq, row * xq.ld + (size_t)min(h0 + ps * RPW, n_q - 1) * D + d0);
+                if (hb + ps * RPW < n_q) x[ps].load(xq, row * xq.ld + (size_t)min(h0 + ps * RPW, n_q - 1) * D + d0);
             turns(ro, pos, d0, tr);
         }
 #pragma unroll
         for (int ps = 0; ps < QPASS; ++ps) {
+            if (hb + ps * RPW >= n_q) break;
             float y[8];
             turn<float>(x[ps], tr, d0, ro, y);
             if (h0 + ps * RPW < n_q)
