@@ -600,7 +600,7 @@ __device__ __forceinline__ void wait_tiles()
 // groups each for itself): the cache is read once for 64 MQ rows and nothing is
 // merged.
 template <int D, int MQ, bool ROWS>
-__global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4_geom g, int n_q, int n_kv,
+__global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n_q, int n_kv,
                                                                    const uint16_t* q, long long q_ld, float cs,
                                                                    float* part, att_plan plan, void* out, int out_t,
                                                                    long long out_ld)
@@ -802,7 +802,7 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         floatx4 st[MQ][2];
-        __builtin_amdgcn_sched_barrier(0);                         // the products start together (8 x 512 rows: 337 -> 317 us)
+        __builtin_amdgcn_sched_barrier(0);                         // the products start together (64 x 5 rows: 112 -> 108 us)
 #pragma unroll
         for (int pt = 0; pt < 2; ++pt)
 #pragma unroll
@@ -821,8 +821,8 @@ __global__ void __launch_bounds__(256, MQ <= 2 ? 2 : 1) k_kv4_attn(rows_t r, kv4
         }
         // The vector units bound a tile (some 1250 cycles of them beside 550 of products, D =
         // 128, MQ = 2), so a wave in its softmax goes before one that waits on its products.
-        // With and without, us: 64 x 5 rows at 8192 positions of 40 / 8 heads 111 / 115, 8 x 512
-        // at 4096 of 32 / 8 317 / 370, single rows alike.
+        // With and without, us: 64 x 5 rows at 8192 positions of 40 / 8 heads 108 / 115, 8 x 512
+        // at 4096 of 32 / 8 312 / 335, single rows alike.
         __builtin_amdgcn_s_setprio(1);
         half8 pf[MQ];
 #pragma unroll
@@ -1132,16 +1132,8 @@ static void kv4_attn_d(const rows_t& r, const att_plan& pl, const kv4_geom& g, i
         if (ev0) hipExtLaunchKernelGGL(kern, grid, block, 0, s, ev0, ev1, 0, r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
         else kern<<<grid, block, 0, s>>>(r, g, n_q, n_kv, q, q_ld, cs, part, pl, out, (int)out_t, out_ld);
     };
-    if (pl.by_rows) {
-        if (pl.mq == 1) go(k_kv4_attn<D, 1, true>);
-        else go(k_kv4_attn<D, 2, true>);
-        return;
-    }
-    switch (pl.mq) {
-        case 1: go(k_kv4_attn<D, 1, false>); break;
-        case 2: go(k_kv4_attn<D, 2, false>); break;
-        default: go(k_kv4_attn<D, 3, false>); break;
-    }
+    if (pl.mq == 1) go(pl.by_rows ? k_kv4_attn<D, 1, true> : k_kv4_attn<D, 1, false>);
+    else go(pl.by_rows ? k_kv4_attn<D, 2, true> : k_kv4_attn<D, 2, false>);
 }
 
 void launch_kv4_attention(const rows_t& r, const att_plan& pl, const kv4_geom& g, int n_q, int n_kv, int D, const uint16_t* q,

@@ -1221,16 +1221,17 @@ void launch_rope_kv(const rows_t& r, const float* qkv, const float* P, int S, co
                                                  (uint16_t*)c.v, c.g, layer, q_out, first, upw);
 }
 
-// The 4-bit cache's attention by its query rows a KV head: up to 48 in one slice of one
-// to three tiles; up to 64 in two slices of two tiles (64 sequences at 8192 positions,
-// 60 rows: 235 us, one slice of four tiles 283; 40 rows: 208 in three tiles, 229 in two
-// slices); more than that divided among a work-group's waves (4 x 509 rows behind
-// up to 1034 positions, 32 / 8 heads: 52 us, in slices of four tiles 139, of two 84).
+// The 4-bit cache's attention by its query rows a KV head: up to 32 in one slice of one or
+// two tiles; up to 64 in two slices of two (three tiles a wave leave room for one
+// work-group a CU: 48 rows of 64 sequences at 8192 positions 219 us, 214 in two slices, of
+// 16 at 4096 62 and 45, of one at 131000 78 and 61); more than that divided among a
+// work-group's waves (60 rows of 64 sequences at 8192 positions: 309 us so, 219 in two
+// slices; 4 x 509 rows behind up to 1034, 32 / 8 heads: 52 us so, in slices of two 84).
 // Those take two tiles each, or one where two would leave CUs without a work-group (one
 // sequence of 300 rows: 13 us, 18 with two; of 1000: 35 and 43; of 2500, which fills
 // them: 101 and 96; 16 of 100 behind 900: 65 and 51).
 // Items are cut as for the other caches, which bounds the partial results.
-constexpr int KV4_ONE_SLICE = 48, KV4_BY_ROWS = 64;
+constexpr int KV4_ONE_SLICE = 32, KV4_BY_ROWS = 64;
 
 att_plan attention_plan(int B, int n, int n_q, int n_kv, int max_ctx, int kv_f32, bool kv4)
 {
