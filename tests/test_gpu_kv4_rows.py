@@ -1,0 +1,100 @@
+"""Rows of the 4-bit attention past the cache's last position, where a sequence is cut into items and where it is
+whole; every row against 64 bits under the bound of the kernel's own arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import kv4_ref as ref
+from paper_2606_18967_amd import sdrl
+
+from gpu_common import i32, say
+from test_gpu_kv4 import host, make_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def filled(D, n_kv, B, ctx, max_ctx, page, seed, loud=1.0):
+    """A cache whose slots hold ctx random positions, and its values on the host by slot and KV head:
+    (codes - 8 [ctx][D], s [ctx], z [ctx]) of K and V in float64."""
+    cache = make_cache(1, n_kv, D, B, max_ctx, page, seed)
+    g = torch.Generator().manual_seed(seed + 1)
+    k, v = (torch.randn((B, ctx, n_kv, D), generator=g) for _ in range(2))
+    sdrl.kv4_append(cache, 0, i32(range(B)), (k * loud).cuda(), v.cuda())
+    cache.check()
+    hc = host(cache)
+    return cache, [[tuple(hc.rows(b, 0, h, ctx, is_v) for is_v in (False, True)) for h in range(n_kv)] for b in range(B)]
+
+
+def attend(q, k, v, scale):
+    """Attention of q [D] over k, v = (c, s, z) in 64 bits, the bound on what the kernel may be off, and None, or the
+    position that takes all the weight, where no smaller bound on the scores is needed.  The kernel's roundings:
+    - a score, in fp32: 16 half steps (2^-24) of its terms' sizes, and the factor scale log2 e rounded to fp32;
+    - P s in fp16: 2^-11 of each, and 2^-28 of the largest for the ones below fp16's normal numbers;
+    - sums over codes 0..15 and the centre's eight of them in fp32: a half step for each tile of 32 positions and 8 more;
+    - P, its sum and the merges in fp32: 2^-18;   - the output in bf16: 2^-8."""
+    (kc, ks, kz), (vc, vs, vz) = k, v
+    sc = scale * (ks * (kc @ q) + kz * q.sum())
+    size = abs(scale) * (ks * (15 * np.abs(q).sum() + 8 * abs(q.sum())) + np.abs(kz) * np.abs(q).sum())
+    off = float((16 * 2.0 ** -24 * size + 2.0 ** -22 * np.abs(sc)).max())
+    order = np.argsort(sc)
+    p = np.exp(sc - sc.max())
+    p /= p.sum()
+    val = vs[:, None] * vc + vz[:, None]
+    at = None
+    if off > 2.0 ** -6:
+        gap = sc[order[-1]] - sc[order[-2]] if len(sc) > 1 else np.inf
+        if gap < 2 * off + 25:                                     # e^-25 < 2^-36: one position, or no statement
+            return None, None, None
+        at, off = int(order[-1]), 0.0
+    ps = p * vs
+    tiles = len(sc) / 32 + 8
+    tol = (2.0 ** -11 * (ps @ np.abs(vc)) + 2.0 ** -28 * ps.max() * np.abs(vc).sum(0) + tiles * 2.0 ** -24 * 23 * ps.sum()
+           + (2 * off + 2.0 ** -18) * (p @ np.abs(val)))
+    want = p @ val
+    return want, tol + 2.0 ** -8 * np.abs(want), at
+
+
+def check_rows(got, q, vals, base, n_kv, max_ctx, scale, skip=()):
+    """Every row of one sequence but those in skip (row, head); the number of rows without a statement."""
+    n, n_q = q.shape[:2]
+    G, none, worst = n_q // n_kv, 0, 0.0
+    for i in range(n):
+        for h in range(n_q):
+            if (i, h) in skip:
+                continue
+            if base + i >= max_ctx:
+                assert (got[i, h] == 0).all(), (i, h)
+                continue
+            k, v = (tuple(x[:base + i + 1] for x in t) for t in vals[h // G])
+            want, tol, _ = attend(q[i, h], k, v, scale)
+            if want is None:
+                none += 1
+                continue
+            err = np.abs(got[i, h] - want)
+            worst = max(worst, float((err / tol).max()))
+            assert (err <= tol).all(), (i, h, float((err / tol).max()))
+    say("worst error / bound", round(worst, 3))
+    return none
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+# n_kv and n: one tile, two, two slices of two, rows divided among the waves; contexts cut into several items but for the last
+@pytest.mark.parametrize("D,n_q,n_kv,n,max_ctx", [(128, 4, 1, 1, 2048), (128, 4, 1, 5, 2048), (64, 4, 2, 5, 1536),
+                                                  (128, 8, 1, 5, 2048), (64, 2, 1, 80, 2048), (128, 4, 2, 4, 64)])
+def test_rows_past_max_ctx_are_zeros(D, n_q, n_kv, n, max_ctx):
+    say("past max_ctx", D, n_q, n_kv, n, max_ctx)
+    cache, vals = filled(D, n_kv, 2, max_ctx, max_ctx, 32, 7)
+    q = torch.randn((2, n, n_q, D), generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+    for length in (max_ctx - n // 2, max_ctx, max_ctx + 700, 2 ** 31 - 1):
+        cache.kv_len.copy_(i32([length, 40]))
+        out = torch.full_like(q, 9.0)
+        sdrl.kv4_attention(cache, 0, i32([0, 1]), q, out)
+        if length + n > max_ctx:
+            with pytest.raises(sdrl.SDError, match="position outside"):
+                cache.check()
+        cache.check()
+        for b, base in ((0, length), (1, 40)):
+            assert check_rows(f64(out[b]), f64(q[b]), vals[b], base, n_kv, max_ctx, D ** -0.5) == 0
