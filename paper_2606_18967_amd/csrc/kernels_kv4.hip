@@ -652,7 +652,8 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
     // sequences of a size whose pages lie in order read the same memory channels at a
     // time otherwise (64 at 8192 positions in pages of 64, of 256: 102 and 112 us, 94 and
     // 96 so; pages in random order 98 and 97).
-    const int whole = min(own, max(0, (min(pe, all + 1) - wq0 + STEP - 32) / STEP));
+    // (rows past max_ctx see nothing: with one of them every tile is masked)
+    const int whole = basepos > r.max_ctx - nlive ? 0 : min(own, max(0, (min(pe, all + 1) - wq0 + STEP - 32) / STEP));
     const int from = ROWS || whole == 0 ? 0 : item * 13 % whole;
     auto place = [&](int i) { return ROWS || i >= whole ? i : i + from < whole ? i + from : i + from - whole; };
     const uint8_t* slots_at = s_buf + (ROWS ? 0 : w * (RING * SLOT));
@@ -934,21 +935,18 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
         for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(o[mt][nb + e][i] - oc[mt][i], 16777216.f, zsum[mt]);
         return make_float4(v[0], v[1], v[2], v[3]);
     };
-    // dims d.. of a row of the slice: to the partial results, or the output itself.  A row without a place
-    // takes no part (it may have summed whole tiles): in the partial results it is a row that saw nothing
+    // dims d.. of a row of the slice: to the partial results, or the output itself
     auto put = [&](int qrow, int d, float top, float l, float4 x) {
-        const int i = qrow / G, h = qrow - i * G;
         if (qrow >= QR) return;
-        const bool none = l == 0.f || basepos + i < 0 || basepos + i >= r.max_ctx;
-        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
         if (it.nch > 1) {
             float* pp = part + part_at(item, n_kv, kvh, G * r.n, qrow, D);
-            if (d == 0) *(float2*)pp = none ? make_float2(KV4_REF0, 0.f) : make_float2(top, l);
-            *(float4*)(pp + 4 + d) = none ? zero : x;
+            if (d == 0) *(float2*)pp = make_float2(top, l);
+            *(float4*)(pp + 4 + d) = x;
             return;
         }
+        const int i = qrow / G, h = qrow - i * G;
         kv4_store4(out, out_t, (size_t)(row0 + i) * out_ld + (size_t)(kvh * G + h) * D + d,
-                   none ? zero : make_float4(x.x / l, x.y / l, x.z / l, x.w / l));
+                   l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x / l, x.y / l, x.z / l, x.w / l));
     };
     if constexpr (ROWS) {
 #pragma unroll
