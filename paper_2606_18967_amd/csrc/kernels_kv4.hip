@@ -191,6 +191,16 @@ __device__ __forceinline__ float row_reduce(float v, F f)
     return v;
 }
 
+// f over the lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them
+template <typename F>
+__device__ __forceinline__ float across_rows(float v, F f)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // A lane's part of quantizing a row (the group (s, z) of the row's D/8 lanes):
 // CODE0 + code of each value, clamp(rint((y - z)/s) + 8, 0, 15).  A sum with
 // CODE0 + 8 = 1.5 * 2^23 + 8 rounds to the nearest integer, ties to even.  The
@@ -557,7 +567,7 @@ __device__ att_item own_item(const rows_t& r, const att_plan& pl, int item)
 // take), c 2^-20 in bits 4..7; a word's eight codes are four ANDs and a shift,
 // and the other operand's elements 2, 3, 6 and 7 carry the factor 1/16.
 //   S^T = K Q^T with v_mfma_f32_16x16x32_f16, the queries scaled by a power of
-// two a row (bf16 values keep all their bits).  Row j of tile half pt is position
+// two (see the query fragments).  Row j of tile half pt is position
 // 8 (j/4) + 4 pt + j%4, so that a lane's eight scores are the positions
 // 8 (lane/16) + 0..7 of query row lane % 16: the B operand of O^T += V^T P^T, whose
 // A operand is one word of V codes a lane (8 positions of one dim).  P s goes in
@@ -616,6 +626,7 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
     __shared__ __attribute__((aligned(1024))) uint8_t s_buf[RINGS > MERGE ? RINGS : MERGE];   // the rings, then the merge
     __shared__ float2 s_par[4 * 64];
     __shared__ float s_ml[4][2][16];
+    __shared__ float s_back[4][MQ][16];                            // rows apart: what gives a row's power of two back
 
     const int item = blockIdx.y, kvh = blockIdx.x, zsl = gridDim.z - 1 - blockIdx.z;   // the last rows, which see most, first
     const att_item it = plan.item ? plan.item[item] : own_item(r, plan, item);
@@ -712,36 +723,54 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
     for (int u = 0; u < AHEAD; ++u)
         if (u < nt) issue(u, u);
 
-    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7 times the power of two that
-    // puts the slice's largest below 2^14 (what is lost of small ones is 2^-38 of
-    // it), elements 2, 3, 6, 7 over 16; the row's sum in the products' unit (2^-24);
-    // and the factor from that unit to a score in base 2
+    // query fragments: row lr's dims (D/4) cq + 8 ks + 0..7 times the power of two that puts the largest
+    // below 2^14, elements 2, 3, 6, 7 over 16; the row's sum in the products' unit (2^-24); and the factor from that
+    // unit to a score in base 2.  Rows of a size share one power of two, which the tiles' groups then carry: a bf16
+    // value keeps all its bits down to 2^-26 of the slice's largest (elements over 16; the others to 2^-30) and is off by
+    // 2^-34 of it below that, 2^-25 of the largest of a row whose exponent is 8 less.  Where one is smaller, or infinite,
+    // or the common factor could leave fp32, the rows are `apart`: each has its own power of two, which the products give
+    // back, and an infinite or NaN query stays in its row.
     half8 qf[MQ][KW];
     float qsum[MQ], unit;
+    uint64_t apart;                                                // 0 or a ballot
     int lim[MQ];
+    floatx4 mid8[MQ];                                              // what the centre 8 takes off a score's products
     {
         u32x4 v[MQ][KW];
-        float top = 0.f;
+        float top[MQ], most = 0.f;
+        auto larger = [](float a, float b) { return fmaxf(a, b); };
 #pragma unroll
         for (int mt = 0; mt < MQ; ++mt) {
             const int qrow = qbase + 16 * mt + lr, i = qrow / G, h = qrow - i * G, pos = basepos + i;
             const bool live = qrow < QR && pos >= 0 && pos < r.max_ctx;
             lim[mt] = live ? pos : -1;
             const uint16_t* qp = q + (size_t)(row0 + (live ? i : 0)) * q_ld + (size_t)(kvh * G + (live ? h : 0)) * D + (D / 4) * cq;
+            top[mt] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KW; ++ks) {
                 v[mt][ks] = live ? *(const u32x4*)(qp + 8 * ks) : (u32x4){0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(v[mt][ks][e] << 16)), fabsf(__uint_as_float(v[mt][ks][e] & 0xffff0000u))));
+                    top[mt] = fmaxf(top[mt], fmaxf(fabsf(__uint_as_float(v[mt][ks][e] << 16)), fabsf(__uint_as_float(v[mt][ks][e] & 0xffff0000u))));
             }
+            top[mt] = across_rows(top[mt], larger);
+            most = fmaxf(most, top[mt]);
         }
-        top = wave_max(top);
-        const int ex = min(max(267 - (int)(__float_as_uint(top) >> 23), 1), 253);
-        const float up = __uint_as_float((uint32_t)ex << 23);
-        unit = cs * __uint_as_float((uint32_t)(254 - ex) << 23) * 16777216.f;
+        auto exponent = [](float x) { return (int)(__float_as_uint(x) >> 23); };
+        const int em = exponent(row_reduce<16>(most, larger));
+        bool far = em > 187;                                       // 2^61
+#pragma unroll
+        for (int mt = 0; mt < MQ; ++mt) far |= top[mt] > 0.f && exponent(top[mt]) < em - 8;
+        apart = __builtin_amdgcn_ballot_w64(far);
+        auto shift_of = [](int e) { return min(267 - e, 253); };   // biased, of the power of two for a largest of exponent e
+        auto back_of = [&](int e) { return __uint_as_float((uint32_t)(254 - shift_of(e)) << 23); };
+        unit = apart ? cs : cs * back_of(em) * 16777216.f;
 #pragma unroll
         for (int mt = 0; mt < MQ; ++mt) {
+            const int er = apart ? exponent(top[mt]) : em;
+            const float up = __uint_as_float((uint32_t)shift_of(er) << 23);
+            const float back = back_of(er);
+            s_back[w][mt][lr] = back;
             float sum = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KW; ++ks)
@@ -753,9 +782,10 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
                     qf[mt][ks][2 * e] = (_Float16)(a * f);
                     qf[mt][ks][2 * e + 1] = (_Float16)(b * f);
                 }
-            sum += __shfl_xor(sum, 16, WAVE);
-            sum += __shfl_xor(sum, 32, WAVE);
-            qsum[mt] = sum * 5.9604644775390625e-08f;              // 2^-24
+            sum = across_rows(sum, [](float a, float b) { return a + b; });
+            const float in_unit = sum * 5.9604644775390625e-08f;   // 2^-24
+            mid8[mt] = (floatx4){-8.f * in_unit, -8.f * in_unit, -8.f * in_unit, -8.f * in_unit};
+            qsum[mt] = apart ? sum * back : in_unit;
         }
     }
     // a tile's groups in fp32, a lane a group: (s, z) of a key in score units, (s, z) of a
@@ -773,10 +803,6 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
 #pragma unroll
         for (int nb = 0; nb < NBD; ++nb) o[mt][nb] = (floatx4){0.f, 0.f, 0.f, 0.f};
     }
-
-    floatx4 mid8[MQ];                                              // what the centre 8 takes off a score's products
-#pragma unroll
-    for (int mt = 0; mt < MQ; ++mt) mid8[mt] = (floatx4){-8.f * qsum[mt], -8.f * qsum[mt], -8.f * qsum[mt], -8.f * qsum[mt]};
 
     // a word's codes in fp16 (see above)
     auto codes = [](uint32_t x) {
@@ -848,9 +874,13 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
                     for (int e = 0; e < 8; ++e) top = fmaxf(top, p[e] * 0x1p-60f);
                 return top;
             };
-            float top = weights();
+            const float top = weights();
             // (infinite references, of infinite scores, stay)
-            if (__builtin_amdgcn_ballot_w64(top > 32768.f && ref[mt] < INFINITY)) {
+            if (__builtin_amdgcn_ballot_w64(top > 32768.f && ref[mt] < INFINITY) | apart) {
+                if (apart) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) st[mt][e >> 2][e & 3] = st[mt][e >> 2][e & 3] * 16777216.f * s_back[w][mt][lr];
+                }
                 float bm = KV4_REF0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -858,11 +888,8 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
                     asm volatile("" : "+v"(v));                    // keeps the logarithms on this path
                     if (seen[e]) bm = fmaxf(bm, score(e, fmaxf(__builtin_amdgcn_logf(v), -60.f)));
                 }
-                bm = fmaxf(bm, __shfl_xor(bm, 16, WAVE));
-                bm = fmaxf(bm, __shfl_xor(bm, 32, WAVE));
-                top = fmaxf(top, __shfl_xor(top, 16, WAVE));
-                top = fmaxf(top, __shfl_xor(top, 32, WAVE));
-                const float to = top > 32768.f ? fmaxf(bm - 7.f, ref[mt]) : ref[mt];
+                bm = across_rows(bm, [](float a, float b) { return fmaxf(a, b); });
+                const float to = bm > ref[mt] + 15.f ? bm - 7.f : ref[mt];
                 const float corr = to == ref[mt] ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - to);
                 ref[mt] = to;
                 lsum[mt] *= corr;

@@ -1,5 +1,6 @@
-"""Rows of the 4-bit attention past the cache's last position, where a sequence is cut into items and where it is
-whole; every row against 64 bits under the bound of the kernel's own arithmetic."""
+"""Rows of the 4-bit attention that must not depend on their neighbours: rows past the cache's last position where a
+sequence is cut into items, next to queries that are infinite, NaN or of far larger size; every row against 64 bits
+under the bound of the kernel's own arithmetic."""
 import numpy as np
 import pytest
 import torch
@@ -98,3 +99,47 @@ def test_rows_past_max_ctx_are_zeros(D, n_q, n_kv, n, max_ctx):
         cache.check()
         for b, base in ((0, length), (1, 40)):
             assert check_rows(f64(out[b]), f64(q[b]), vals[b], base, n_kv, max_ctx, D ** -0.5) == 0
+
+
+LOUD = [float("inf"), -float("inf"), float("nan"), 2.0 ** 27, -2.0 ** 40, 2.0 ** 100, 2.0 ** 121, 2.0 ** -9, 2.0 ** -30, 0.0]
+
+
+@pytest.mark.parametrize("D,n_q,n_kv,B,n,base", [(128, 4, 1, 2, 1, 1500), (128, 8, 2, 2, 5, 90), (64, 4, 4, 2, 5, 1300),
+                                                 (128, 12, 1, 1, 4, 700), (64, 4, 2, 2, 50, 60), (128, 4, 1, 1, 70, 900)])
+@pytest.mark.parametrize("other", LOUD)
+def test_a_row_does_not_depend_on_its_neighbours(D, n_q, n_kv, B, n, base, other):
+    """One row is not finite in one value, or of another size than the rest; the others are right all the same."""
+    say("neighbours", D, n_q, n_kv, B, n, base, other)
+    ctx = base + n
+    cache, vals = filled(D, n_kv, B, ctx, ctx + 3, 32, 11)
+    cache.kv_len.fill_(base)
+    q = torch.randn((B, n, n_q, D), generator=torch.Generator().manual_seed(5))
+    at = (n - 1, n_q - 1)                                          # the last position, which the others precede
+    if np.isfinite(other):
+        q[:, at[0], at[1]] *= other
+    else:
+        q[:, at[0], at[1], 3] = other
+    q = q.bfloat16().cuda()
+    got = f64(sdrl.kv4_attention(cache, 0, i32(range(B)), q))
+    cache.check()
+    for b in range(B):
+        assert check_rows(got[b], f64(q[b]), vals[b], base, n_kv, ctx + 3, D ** -0.5, skip=[at]) == 0
+        if not np.isfinite(other):
+            assert np.isnan(got[b][at]).all()
+        elif abs(other) <= 1.0:
+            h = at[1] * n_kv // n_q
+            want, tol, _ = attend(f64(q[b])[at], *vals[b][h], D ** -0.5)
+            assert want is None or (np.abs(got[b][at] - want) <= tol).all()
+
+
+def test_rows_of_every_size_side_by_side():
+    """Rows from 2^-60 to 2^16 in one slice."""
+    say("sizes side by side")
+    D, n_q, n, base = 128, 4, 8, 600
+    cache, vals = filled(D, 1, 1, base + n, base + n, 64, 13)
+    cache.kv_len.fill_(base)
+    q = torch.randn((1, n, n_q, D), generator=torch.Generator().manual_seed(6))
+    q *= (2.0 ** torch.linspace(-60, 16, n * n_q)).reshape(1, n, n_q, 1)
+    q = q.bfloat16().cuda()
+    got = f64(sdrl.kv4_attention(cache, 0, i32([0]), q))[0]
+    assert check_rows(got, f64(q[0]), vals[0], base, 1, base + n, D ** -0.5) == 0
