@@ -586,7 +586,7 @@ __device__ att_item own_item(const rows_t& r, const att_plan& pl, int item)
 // bytes and vector units alike (106 us, 5.4 TB/s); a prefill the vector units: 46 cycles a
 // score of 64 lanes in the softmax, 5 instructions a code word, 17 products of 16
 // cycles a 16-row tile (8 x 512 rows at 4096 positions 306 us, 840 TFLOP/s).
-constexpr float KV4_REF0 = -1e30f;     // the reference of a row that has seen no position
+constexpr float KV4_REF0 = -3.4028235e38f;     // the reference of a row that has seen no position: below every score
 
 // 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
 // `lds` on; non-temporal.  The compiler's wait counts do not see them.
@@ -793,6 +793,7 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
     float2* par = (float2*)(s_par + 64 * w);
     const float par_s = lane < 32 ? unit : lane & 2 ? 0.0625f : 1.f, par_z = lane < 32 ? unit : 1.f;
 
+    float limit = apart ? -1.f : 32768.f;                          // of P s; -1: every tile takes the path that moves references
     float ref[MQ], lsum[MQ], zsum[MQ];
     floatx4 o[MQ][NBD], oc[MQ];
 #pragma unroll
@@ -859,12 +860,11 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
             const int last = min(pe - 1, lim[mt]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) seen[e] = !MASKED || blk + 8 * cq + e <= last;   // what a row does not see may hold anything
-            auto score = [&](int e, float from) { return __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], __builtin_fmaf(kz[e], qsum[mt], from)); };
-            auto weights = [&] {
+            auto weights = [&](auto above) {                       // P and P s of the scores above the reference
                 float top = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float a = score(e, -ref[mt]);
+                    const float a = above(e);
                     p[e] = __builtin_amdgcn_exp2f(seen[e] ? a : -INFINITY);
                     pv[e] = p[e] * (seen[e] ? vs[e] : 0.f);
                     top = fmaxf(top, pv[e]);
@@ -874,21 +874,26 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
                     for (int e = 0; e < 8; ++e) top = fmaxf(top, p[e] * 0x1p-60f);
                 return top;
             };
-            const float top = weights();
+            const float top =
+                weights([&](int e) { return __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], __builtin_fmaf(kz[e], qsum[mt], -ref[mt])); });
             // (infinite references, of infinite scores, stay)
-            if (__builtin_amdgcn_ballot_w64(top > 32768.f && ref[mt] < INFINITY) | apart) {
+            if (__builtin_amdgcn_ballot_w64(top > limit && ref[mt] < INFINITY)) {
                 if (apart) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) st[mt][e >> 2][e & 3] = st[mt][e >> 2][e & 3] * 16777216.f * s_back[w][mt][lr];
                 }
-                float bm = KV4_REF0;
+                // Here a score is rounded before the reference leaves it.  Past 2^20 units in the last place are no small
+                // part of P's range, so with a bound of that size every tile of the wave comes this way from then on
+                float sc[8], bm = KV4_REF0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float v = vs[e];
                     asm volatile("" : "+v"(v));                    // keeps the logarithms on this path
-                    if (seen[e]) bm = fmaxf(bm, score(e, fmaxf(__builtin_amdgcn_logf(v), -60.f)));
+                    sc[e] = __builtin_fmaf(ks[e], st[mt][e >> 2][e & 3], kz[e] * qsum[mt]);
+                    if (seen[e]) bm = fmaxf(bm, sc[e] + fmaxf(__builtin_amdgcn_logf(v), -60.f));
                 }
                 bm = across_rows(bm, [](float a, float b) { return fmaxf(a, b); });
+                if (__builtin_amdgcn_ballot_w64(fabsf(bm) > 0x1p20f && bm > KV4_REF0)) limit = -1.f;
                 const float to = bm > ref[mt] + 15.f ? bm - 7.f : ref[mt];
                 const float corr = to == ref[mt] ? 1.f : __builtin_amdgcn_exp2f(ref[mt] - to);
                 ref[mt] = to;
@@ -900,9 +905,14 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
 #pragma unroll
                     for (int nb = 0; nb < NBD; ++nb) o[mt][nb][i] *= corr;
                 }
-                weights();
+                weights([&](int e) { return sc[e] - ref[mt]; });
+                if (limit < 0.f) {                                 // what the reference's own rounding leaves above
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pv[e] = fminf(pv[e], 32768.f);   // (scores past 2^23, where a unit in the last place is large)
+                    for (int e = 0; e < 8; ++e) {
+                        p[e] = pv[e] > 32768.f ? 32768.f * __builtin_amdgcn_rcpf(vs[e]) : p[e];
+                        pv[e] = fminf(pv[e], 32768.f);
+                    }
+                }
             }
             float2v pr[4];
 #pragma unroll

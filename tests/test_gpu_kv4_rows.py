@@ -36,17 +36,17 @@ def attend(q, k, v, scale):
     (kc, ks, kz), (vc, vs, vz) = k, v
     sc = scale * (ks * (kc @ q) + kz * q.sum())
     size = abs(scale) * (ks * (15 * np.abs(q).sum() + 8 * abs(q.sum())) + np.abs(kz) * np.abs(q).sum())
-    off = float((16 * 2.0 ** -24 * size + 2.0 ** -22 * np.abs(sc)).max())
-    order = np.argsort(sc)
+    offs = 16 * 2.0 ** -24 * size + 2.0 ** -22 * np.abs(sc)
+    weigh = np.flatnonzero(sc + offs > (sc - offs).max() - 25)     # the others weigh below e^-25 < 2^-36 whatever the roundings
+    off = float(offs[weigh].max())
     p = np.exp(sc - sc.max())
     p /= p.sum()
     val = vs[:, None] * vc + vz[:, None]
     at = None
     if off > 2.0 ** -6:
-        gap = sc[order[-1]] - sc[order[-2]] if len(sc) > 1 else np.inf
-        if gap < 2 * off + 25:                                     # e^-25 < 2^-36: one position, or no statement
+        if len(weigh) > 1:                                         # one position, or no statement
             return None, None, None
-        at, off = int(order[-1]), 0.0
+        at, off = int(weigh[0]), 0.0
     ps = p * vs
     tiles = len(sc) / 32 + 8
     tol = (2.0 ** -11 * (ps @ np.abs(vc)) + 2.0 ** -28 * ps.max() * np.abs(vc).sum(0) + tiles * 2.0 ** -24 * 23 * ps.sum()
@@ -143,3 +143,47 @@ def test_rows_of_every_size_side_by_side():
     q = q.bfloat16().cuda()
     got = f64(sdrl.kv4_attention(cache, 0, i32([0]), q))[0]
     assert check_rows(got, f64(q[0]), vals[0], base, 1, base + n, D ** -0.5) == 0
+
+
+@pytest.mark.parametrize("D,n_q,n_kv,n,base", [(128, 4, 1, 1, 1500), (64, 4, 2, 5, 700), (128, 8, 2, 6, 90), (64, 2, 1, 70, 900)])
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 27, -2.0 ** 40, 2.0 ** 80, 2.0 ** 110])
+def test_scores_of_every_size(D, n_q, n_kv, n, base, size):
+    """Loud queries: one position takes all the weight and its value comes out, however large the scores are."""
+    say("loud queries", D, n_q, n_kv, n, base, size)
+    cache, vals = filled(D, n_kv, 1, base + n, base + n, 32, 17)
+    cache.kv_len.fill_(base)
+    q = (torch.randn((1, n, n_q, D), generator=torch.Generator().manual_seed(8)) * size).bfloat16().cuda()
+    got = f64(sdrl.kv4_attention(cache, 0, i32([0]), q))[0]
+    assert check_rows(got, f64(q[0]), vals[0], base, n_kv, base + n, D ** -0.5) <= n * n_q // 8 + 1   # ties within fp32's last places
+
+
+def test_loud_keys_that_come_late():
+    """Ordinary scores first, then keys of 2^30 times the size, in a tile that every row sees whole and in the last ones."""
+    say("late loud keys")
+    D, n_q, base, n = 128, 4, 1000, 4
+    for late in (500, 1001):
+        cache = make_cache(1, 1, D, 1, base + n, 32, 19)
+        g = torch.Generator().manual_seed(20)
+        k, v = (torch.randn((1, base + n, 1, D), generator=g) for _ in range(2))
+        k[0, late:] *= 2.0 ** 30
+        sdrl.kv4_append(cache, 0, i32([0]), k.cuda(), v.cuda())
+        cache.kv_len.fill_(base)
+        hc = host(cache)
+        vals = [tuple(hc.rows(0, 0, 0, base + n, is_v) for is_v in (False, True))]
+        q = torch.randn((1, n, n_q, D), generator=g).bfloat16().cuda()
+        got = f64(sdrl.kv4_attention(cache, 0, i32([0]), q))[0]
+        assert check_rows(got, f64(q[0]), vals, base, 1, base + n, D ** -0.5) <= 2
+
+
+def test_one_position_of_any_score():
+    """A row that sees one position returns its value, also where the score is below -1e30."""
+    say("one position")
+    D = 128
+    cache, vals = filled(D, 1, 2, 1, 64, 32, 23)
+    for size in (1.0, 2.0 ** 100, 2.0 ** 110):
+        for sign in (1, -1):
+            cache.kv_len.zero_()
+            q = (torch.randn((2, 1, 4, D), generator=torch.Generator().manual_seed(9)) * size * sign).bfloat16().cuda()
+            got = f64(sdrl.kv4_attention(cache, 0, i32([0, 1]), q))
+            for b in range(2):
+                assert check_rows(got[b], f64(q[b]), vals[b], 0, 1, 64, D ** -0.5) == 0
