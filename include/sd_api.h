@@ -193,9 +193,11 @@ sd_status sd_set_rope(sd_engine e, const sd_rope_cfg* cfg, void* stream);
  * are set to 1 and never cleared by the library, [0] slot outside [0,
  * max_slots), [2] position outside [0, max_ctx) or past the rotary table, [3]
  * block-table entry outside [0, n_pages), [4] row count outside [0, n] (it is
- * clamped).  What they concern is skipped: nothing of the cache is read or
- * written for it, its rows of q_out, k_out, v_out and out are zeros, and the
- * positions of a missing page are as if masked. */
+ * clamped).  What they concern is skipped.  A row without a slot or a position
+ * reads and writes nothing of the cache, and its rows of q_out, k_out, v_out
+ * and out are zeros.  The positions of a missing page are not stored, read back
+ * as zeros and are as if masked in attention; the queries at them are rotated
+ * into q_out and attend the positions that are there. */
 typedef struct {
     void* pages;                /* 16-byte aligned, n_pages * sd_kv4_page_bytes(...) */
     const int32_t* block_table; /* int32[max_slots][pages_per_seq] */

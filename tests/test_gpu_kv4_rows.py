@@ -9,7 +9,7 @@ import kv4_ref as ref
 from paper_2606_18967_amd import sdrl
 
 from gpu_common import i32, say
-from test_gpu_kv4 import host, make_cache
+from test_gpu_kv4 import attention_case, host, make_cache, same_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -187,3 +187,43 @@ def test_one_position_of_any_score():
             got = f64(sdrl.kv4_attention(cache, 0, i32([0, 1]), q))
             for b in range(2):
                 assert check_rows(got[b], f64(q[b]), vals[b], 0, 1, 64, D ** -0.5) == 0
+
+
+def test_rows_whose_own_page_is_missing():
+    """Nothing of them is stored and they read back as zeros; their queries are rotated, and attend what is there."""
+    say("own page missing")
+    D, n_q, n_kv, n, base = 128, 4, 2, 3, 62                       # positions 62, 63 and, on the missing page, 64
+    cache = make_cache(1, n_kv, D, 1, 128, 64, 29)
+    g = torch.Generator().manual_seed(30)
+    x = torch.randn((1, n, n_q + 2 * n_kv, D), generator=g).bfloat16().cuda()
+    q, k, v = x[:, :, :n_q], x[:, :, n_q:n_q + n_kv], x[:, :, n_q + n_kv:]
+    table = sdrl.rope_table(sdrl.RopeConfig(1e4, D), 128)
+    start = cache.pages.clone()
+    outs = []
+    for missing in (False, True):
+        cache.pages.copy_(start)
+        cache.kv_len.fill_(base)
+        if missing:
+            cache.block_table[0, 1] = cache.pages.shape[0]
+        q_out = torch.full((1, n, n_q, D), 9.0, dtype=torch.bfloat16, device="cuda")
+        ko = torch.full((1, n, n_kv, D), 9.0, dtype=torch.bfloat16, device="cuda")
+        vo = ko.clone()
+        lens = None if missing else i32([2])                       # the same rows stored as with the page missing
+        sdrl.kv4_append(cache, 0, i32([0]), k, v, q, q_out, rope=table)
+        if not missing:
+            cache.check()
+            cache.pages.copy_(start)
+            sdrl.kv4_append(cache, 0, i32([0]), k, v, rope=table, lens=lens)
+            hc = host(cache)
+            cache.check()
+        else:
+            same_pool(cache, hc)
+            sdrl.kv4_read(cache, 0, i32([0]), i32([base]), ko, vo)
+            assert bool((ko[:, 2] == 0).all() and (vo[:, 2] == 0).all() and (ko[:, :2] != 0).any())
+            with pytest.raises(sdrl.SDError, match="block-table"):
+                cache.check()
+        outs.append(q_out)
+    assert torch.equal(outs[0], outs[1])
+    cache = attention_case(128, 4, 2, 2, 2, [150, 60], None, 64, 92, hole=(0, 2))
+    with pytest.raises(sdrl.SDError, match="block-table"):
+        cache.check()
