@@ -227,3 +227,35 @@ def test_rows_whose_own_page_is_missing():
     cache = attention_case(128, 4, 2, 2, 2, [150, 60], None, 64, 92, hole=(0, 2))
     with pytest.raises(sdrl.SDError, match="block-table"):
         cache.check()
+
+
+@pytest.mark.parametrize("D,n_q,n_kv,n,base,page", [(128, 32, 8, 1, 333, 64), (128, 40, 8, 5, 200, 64), (64, 4, 4, 4, 2500, 32),
+                                                    (128, 4, 1, 12, 3000, 128), (64, 8, 1, 7, 61, 32), (128, 4, 2, 130, 77, 96),
+                                                    (64, 6, 2, 40, 1100, 64), (128, 16, 1, 1, 4000, 64)])
+@pytest.mark.parametrize("values", ["alike", "small", "large", "mixed", "shifted"])
+def test_rows_within_the_kernels_own_bound(D, n_q, n_kv, n, base, page, values):
+    """All forms of the kernel under attend()'s bound, whose term for P s is fp16's 2^-11: values of one size, of 2^-40 and
+    2^40 times it, of sizes from 2^-20 to 2^20 position by position, and of a mean far from zero."""
+    say("own bound", D, n_q, n_kv, n, base, values)
+    B, top = 2, base + n
+    cache = make_cache(1, n_kv, D, B, top + 5, page, 31)
+    g = torch.Generator().manual_seed(32)
+    k, v = (torch.randn((B, top, n_kv, D), generator=g) for _ in range(2))
+    if values == "mixed":
+        v *= 2.0 ** (40 * torch.rand((B, top, n_kv, 1), generator=g) - 20)
+    elif values == "shifted":
+        v += 20
+    else:
+        v *= {"alike": 1.0, "small": 2.0 ** -40, "large": 2.0 ** 40}[values]
+    sdrl.kv4_append(cache, 0, i32(range(B)), k.cuda(), v.cuda())
+    hc = host(cache)
+    lens = [n, (n + 1) // 2]
+    cache.kv_len.copy_(i32([base, base // 3]))
+    q = torch.randn((B, n, n_q, D), generator=g).bfloat16().cuda()
+    out = torch.full_like(q, 9.0)
+    sdrl.kv4_attention(cache, 0, i32(range(B)), q, out, lens=i32(lens))
+    cache.check()
+    for b, start in enumerate((base, base // 3)):
+        vals = [tuple(hc.rows(b, 0, h, top, is_v) for is_v in (False, True)) for h in range(n_kv)]
+        assert bool((out[b, lens[b]:] == 9.0).all())
+        assert check_rows(f64(out[b, :lens[b]]), f64(q[b, :lens[b]]), vals, start, n_kv, top + 5, D ** -0.5) == 0
