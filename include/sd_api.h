@@ -234,7 +234,8 @@ typedef struct {
 /* Stores the rows of k and v (sd_dtype `dtype`) in layer `layer` of the cache:
  * k rotated (products and sum exact, rounded once to fp32), both quantized.
  * q (same dtype, may be NULL) is rotated into q_out (bf16, contiguous
- * [B*n][n_q][head_dim]).  Positions around the new rows keep their contents. */
+ * [B*n][n_q][head_dim]), in fp32 with one more rounding to bf16.  Positions around
+ * the new rows keep their contents. */
 sd_status sd_kv4_append(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
                         const int32_t* lens, int32_t dtype, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
                         const void* q, int64_t q_ld, int32_t n_q, void* q_out, const sd_rope_args* rope, void* stream);
@@ -254,7 +255,12 @@ size_t sd_kv4_workspace_bytes(const sd_kv4_cache* c, int32_t B, int32_t n, int32
  * query head h reading KV head h/(n_q/n_kv).  q (bf16, rotated, row stride
  * q_ld) and out (bf16, row stride out_ld).  workspace: 256-byte aligned,
  * sd_kv4_workspace_bytes; its contents need no preparation, and calls whose
- * work may overlap need one each.  A row that sees no position gives zeros. */
+ * work may overlap need one each.  A row that sees no position gives zeros.
+ * Scores, the softmax's statistics and all sums are fp32.  The probabilities
+ * times s enter the second product in fp16: 2^-11 of each, and what is below
+ * 2^-28 of a row's largest is lost (and values whose s is below 2^-76).  A query
+ * that is not finite makes its own row NaN, a key or value that is not finite
+ * the rows that see it; a row whose scores leave fp32 is not defined. */
 sd_status sd_kv4_attention(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
                            const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld, float scale, void* out,
                            int64_t out_ld, void* workspace, size_t bytes, void* stream);

@@ -13,15 +13,15 @@ namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// bit of element e in a code word: the elements 2i and 2i + 1 of a word w are the
-// low halves' nibbles of w >> 4i, so one AND-OR makes a pair of bf16 of them
+// bit of element e in a code word: the elements 2i and 2i + 1 of a word are the
+// nibbles 4i bits up in its halves, so one AND makes a pair of fp16 of them
 __device__ __forceinline__ constexpr int nib(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
 
 // tile of 32 positions of one KV head (bytes)
 constexpr int tile_bytes(int D) { return 32 * D + 256; }
 
-// first tile of (page of a slot's position pos, layer, KV head), NULL where the
-// block table has no valid page
+// the page of a slot's positions [lp P, (lp + 1) P), -1 where the block table has
+// no valid one
 __device__ __forceinline__ int kv4_page(const kv4_geom& g, int slot, int lp)
 {
     if (lp < 0 || lp >= g.mpp) return -1;
@@ -571,21 +571,22 @@ __device__ att_item own_item(const rows_t& r, const att_plan& pl, int item)
 // 8 (j/4) + 4 pt + j%4, so that a lane's eight scores are the positions
 // 8 (lane/16) + 0..7 of query row lane % 16: the B operand of O^T += V^T P^T, whose
 // A operand is one word of V codes a lane (8 positions of one dim).  P s goes in
-// as fp16 (2^-11, an eighth of the output's own rounding), and one more product
-// with codes of 8 sums what the centre takes off again.  Neither K nor V touches
-// LDS.
+// as fp16, 2^-11 of each where the output's own rounding is 2^-8 (the error against 64
+// bits of the outputs is 1.66e-3 with P in 32 bits, 1.68e-3 so, at 131071 positions
+// 1.71e-3), and one more product with codes of 8 sums what the centre takes off again.
 // Online softmax in base 2.  A row's reference ref bounds the products' operand:
 // P s = exp2(score - ref) s <= 2^15; it moves, with all sums, only where a tile
 // would exceed that, to where the tile's largest P s is 2^7, so small terms are
-// lost at 2^-24 of a row's largest and not earlier (P itself stays below 2^75 where
-// s is smaller than 2^-60).  Sums and statistics in fp32.
+// off by 2^-28 of a row's largest (of elements over 16; the others by 2^-32).  P itself
+// stays below 2^75 where s is smaller than 2^-60.  Sums and statistics in fp32.
 //   What bounds it: single rows the cache's bytes (64 sequences of 32 or 40 / 8 heads of 128
 // at 2048, 8192 and 32768 positions 28, 94 and 342 us: 5.1, 6.1 and 6.7 TB/s; a launch and
 // the first tiles' way take 5); one short sequence its chain of launch, plan, page,
 // tile (2048 positions 7.7 us, the combine 4); 64 x 5 verify rows at 8192 positions
-// bytes and vector units alike (106 us, 5.4 TB/s); a prefill the vector units: 46 cycles a
-// score of 64 lanes in the softmax, 5 instructions a code word, 17 products of 16
-// cycles a 16-row tile (8 x 512 rows at 4096 positions 306 us, 840 TFLOP/s).
+// bytes and vector units alike (105 to 116 us on different boxes, 5 to 5.5 TB/s); a
+// prefill the vector units: 46 cycles a score of 64 lanes in the softmax, 5 instructions
+// a code word, 17 products of 16 cycles a 16-row tile (8 x 512 rows at 4096 positions
+// 306 us, 840 TFLOP/s).
 constexpr float KV4_REF0 = -3.4028235e38f;     // the reference of a row that has seen no position: below every score
 
 // 64 lanes x 16 (or 4) bytes at base + off straight into LDS, in lane order from byte
