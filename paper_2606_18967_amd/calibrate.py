@@ -302,7 +302,8 @@ def run(cfg: dict, Bs, Ss, gammas, taus, eps=0.05, reps=8, log=print, fmt: str =
     log("fit: " + ", ".join(f"{k} {v:.4g}" for k, v in params.items()) + f"  (rms log residual {r1:.3f} / {r2:.3f})")
     rows, agree = validate(base, params, meas, taus, eps)
     log(f"toggle decisions agreeing with the measured-time speedup: {agree * 100:.1f}% of {len(rows)} points")
-    return dict(cfg=cfg["name"], F_eff=F, params=params, rms_log_residual=dict(target=r1, draft_verify=r2),
+    return dict(cfg=cfg["name"], kv4=kv4, drafter=fmt, F_eff=F, params=params,
+                rms_log_residual=dict(target=r1, draft_verify=r2),
                 samples=samples, validation=rows, agreement=agree, eps=eps, measured_tau=tau_syn,
                 seconds=time.time() - torch_started)
 

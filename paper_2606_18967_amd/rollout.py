@@ -380,7 +380,12 @@ def train(run_fn, policy: str, n_steps: int, lengths_fn, gset=GAMMA_SET, P=PATIE
 def calibrated_cost(cfg: dict, calib: dict, kv4: bool = False):
     """The toggle's cost model (Sec. 4.2): the architecture terms of cfg with
     the fitted parameters of calibrate.py (F_eff, BW_eff, rho_kappa, eta_D,
-    c_T, c_D, c_V), fitted on the same kind of cache."""
+    c_T, c_D, c_V), fitted on the same kind of cache (its "kv4"; a fit that
+    does not say was made on a cache of the model's type): a fit of the other
+    kind is refused, its times would decide the toggle on the wrong bytes."""
+    if bool(calib.get("kv4", False)) != bool(kv4):
+        kind = lambda x: "a 4-bit KV cache" if x else "a KV cache of the model's type"
+        raise ValueError(f"the calibration was made on {kind(calib.get('kv4'))}, this rollout has {kind(kv4)}")
     m = sdrl.cost_init(cfg, kv_bytes=sdrl.kv4_bytes_per_element(cfg["head_dim"]) if kv4 else 2.0)
     m.F_eff = float(calib["F_eff"])
     for k, v in calib["params"].items():
@@ -429,7 +434,7 @@ def main(argv=None):
         log("calibrating the cost model ...")
         calib = calibrate.run(cfg, ints(a.calib_B), ints(a.calib_S), [GAMMA_SET[0]], [2.0, 3.0, 4.0], EPS, 6, log=log,
                               fmt=a.drafter, kv4=a.kv4)
-        calib = dict(F_eff=calib["F_eff"], params=calib["params"], agreement=calib["agreement"])
+        calib = dict(F_eff=calib["F_eff"], params=calib["params"], agreement=calib["agreement"], kv4=calib["kv4"])
     cost = calibrated_cost(cfg, calib, a.kv4)
     log("building the rollout engine ...")
     ro = Rollout(cfg, a.B, a.prompt, a.lmax, seed=a.seed, fmt=a.drafter, graphs=a.graphs, prefill=a.prefill, kv4=a.kv4)
@@ -456,7 +461,7 @@ def main(argv=None):
                    graphs=a.graphs, kv4=a.kv4, prefill_s=ro.prefill_s,
                    lengths=dict(median=a.median, sigma=a.sigma, lo=a.lmin, hi=a.lmax, mean_step0=float(L0.mean()),
                                 max_step0=int(L0.max())),
-                   calib=dict(F_eff=calib["F_eff"], params=calib["params"]),
+                   calib=dict(F_eff=calib["F_eff"], params=calib["params"], kv4=a.kv4),
                    makespan_s={p: [r.makespan_s for r in rs] for p, rs in results.items()},
                    results={p: [asdict(r) for r in rs] for p, rs in results.items()})
     if a.out:
