@@ -252,23 +252,24 @@ class Sweep:
 
 
 def drafter_tradeoff(cfg: dict, fmts=("w4", "w4a", "w8"), Bs=(1, 16, 64), S=2048, gamma=4, steps=10, reps=8,
-                     log=print):
+                     log=print, kv4: bool = False):
     """Latency against acceptance of the drafter formats (App. B.3, Table 4):
     per format and batch, the measured T_q / T_p, the model's tau and alpha
     at (B, S, gamma), and the SD speedup tau T_p / (gamma T_q + T_V) those
     measurements give; next to them the cost model's idealized T_q / T_p
     from bytes alone (weights at 16 bits, drafter projections at 4 or 8)."""
-    sw = Sweep(cfg, max(Bs), S, gamma)
+    sw = Sweep(cfg, max(Bs), S, gamma, kv4=kv4)
+    kv_bytes = sdrl.kv4_bytes_per_element(cfg["head_dim"]) if kv4 else 2.0
     rows = []
     for fmt in fmts:
         sw.set_drafter(fmt)
         bits = 8.0 if fmt == "w8" else 4.0
-        ideal = sdrl.cost_init(cfg, drafter_bits=bits, BW_eff=1.0, F_eff=1e30)
+        ideal = sdrl.cost_init(cfg, drafter_bits=bits, kv_bytes=kv_bytes, BW_eff=1.0, F_eff=1e30)
         for B in Bs:
             r = sw.measure(B, S, [gamma], reps)
             tau = sw.measured_tau(B, S, gamma, steps)
             tp, tq, _ = sdrl.cost_times(ideal, B, S, gamma)
-            row = dict(fmt=fmt, B=B, S=S, gamma=gamma, T_p=r["p"], T_q=r["q"], T_V=r[("v", gamma)],
+            row = dict(fmt=fmt, kv4=kv4, B=B, S=S, gamma=gamma, T_p=r["p"], T_q=r["q"], T_V=r[("v", gamma)],
                        tq_over_tp=r["q"] / r["p"], tq_over_tp_ideal=tq / tp, tau=tau,
                        alpha=sdrl.alpha_from_tau(min(tau, gamma + 1 - 1e-9), gamma),
                        speedup=tau * r["p"] / (gamma * r["q"] + r[("v", gamma)]))
@@ -326,7 +327,7 @@ def main(argv=None):
     ints = lambda s: [int(x) for x in s.split(",") if x]
     if a.drafter_tradeoff:
         rows = drafter_tradeoff(cfg, Bs=ints(a.B), S=max(ints(a.S)), gamma=max(ints(a.gamma)), reps=a.reps,
-                                log=lambda *x: print(*x, file=sys.stderr, flush=True))
+                                log=lambda *x: print(*x, file=sys.stderr, flush=True), kv4=a.kv4)
         txt = json.dumps(rows, indent=1)
         if a.out:
             with open(a.out, "w") as fh:

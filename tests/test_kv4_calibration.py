@@ -63,3 +63,13 @@ def test_the_rollout_command_refuses_the_other_kind(tmp_path, of):
     argv = ["--model", "TINY_BF16", "--calib", str(path)] + ([] if of else ["--kv4"])
     with pytest.raises(ValueError, match="calibration"):
         rollout.main(argv)
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+def test_the_drafter_comparison_runs_on_the_cache_that_is_asked_for(fake, capsys, kv4):
+    calibrate.main(["--drafter-tradeoff", "--B", "1,4", "--S", "512", "--gamma", "3"] + (["--kv4"] if kv4 else []))
+    rows = json.loads(capsys.readouterr().out)
+    assert FakeSweep.made == [kv4] and len(rows) == 6 and all(r["kv4"] is kv4 for r in rows)
+    ideal = sdrl.cost_init(synth.L4_8B, kv_bytes=sdrl.kv4_bytes_per_element(128) if kv4 else 2.0, BW_eff=1.0, F_eff=1e30)
+    tp, tq, _ = sdrl.cost_times(ideal, 4, 512, 3)
+    assert rows[1]["tq_over_tp_ideal"] == pytest.approx(tq / tp)
