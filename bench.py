@@ -149,7 +149,7 @@ COUNTED = {
 DRAFTER_BYTES_PER_WEIGHT = {"w4": 0.5 + 2 / 128, "w4a": 0.5 + 3 / 128, "w8": 1 + 2 / 128}
 
 
-# the kernels of the attention classes on a 4-bit cache
+# the kernels of the attention classes on a 4-bit cache (head_dim 128; 17 to 64 verify rows a KV head)
 KV4_KERNEL_OF_CLASS = {"attn_decode": "k_kv4_attn<128, 1, false>", "attn_verify": "k_kv4_attn<128, 2, false>"}
 
 

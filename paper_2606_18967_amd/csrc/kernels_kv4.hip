@@ -256,8 +256,10 @@ __device__ __forceinline__ uint32_t quantize8(const float (&y)[8], bool live, ui
 // against the row's bytes.
 // Few rows are bound by the chain of loads length, page, row, and a V word's other
 // nibbles: a row of 32 / 8 heads of 128 takes 4.3 us, 64 x 5 rows of 40 / 8 7.5 (both
-// halves of a group's words in scattered pages).  Many are bound by memory: 16 x 1536 rows,
-// half of them there, of 32 / 8 heads 80 us (3.5 TB/s, 278 MB), all of them 115 (4.8).
+// halves of a group's words in scattered pages).  Many are bound by memory: 16 x 1536 rows
+// of 32 / 8 heads 112 us (4.7 TB/s).  Rows that are absent cost their waves' start and
+// leave: half of those rows 66 us (4.0 TB/s), as many in a call without absent ones 61;
+// 10722 of them in ragged lengths 60.
 // A wave takes one KV head, or where there are more than KV4_APPEND_WAVES of them its
 // group's heads one after the other, the next one's loads under way, and positions and table
 // entries once (16 x 1536 rows, 2048 and 4096 waves at least 115 us, 8192 120, a head a wave
@@ -417,7 +419,9 @@ __global__ void __launch_bounds__(256) k_kv4_append(rows_t r, kv4_geom g, int n_
 
 // ------------------------------------------------------------------ read
 // A thread takes 8 dims of K or V of the rows among 8 consecutive positions, so a V word
-// is read once (12288 rows of 8 heads of 128: 24 us, 3.2 TB/s; one row 3.1).
+// is read once (12288 rows of 8 heads of 128: 19 us, 3.3 TB/s; 24576 33 us, 3.8; one row
+// 3.0).  What bounds it is its many narrow loads: K words of 4 bytes a lane, and the eight
+// rows' groups in every lane of them.
 template <int D>
 __global__ void __launch_bounds__(256) k_kv4_read(rows_t r, kv4_geom g, int n_kv, uint16_t* k_out, uint16_t* v_out,
                                                   const int32_t* start, int ngr, long long total)

@@ -623,8 +623,9 @@ def kv4_read(cache: KV4Cache, layer: int, slots, start, k_out, v_out, lens=None)
 
 def kv4_attention(cache: KV4Cache, layer: int, slots, q, out=None, scale: float | None = None, lens=None, workspace=None):
     """Attention of rows q [B][n][n_q][head_dim] (bf16, rotated) at positions kv_len + i over the positions up to
-    each row's own (append them first) into out (bf16, same shape); scale defaults to 1/sqrt(head_dim).  workspace:
-    a uint8 tensor of kv4_workspace_bytes, for callers that keep one (not for calls that may overlap)."""
+    each row's own (append them first) into out (bf16, same shape; rows past lens[b] are not written, and undefined in a
+    tensor made here); scale defaults to 1/sqrt(head_dim).  workspace: a uint8 tensor of kv4_workspace_bytes, for
+    callers that keep one (not for calls that may overlap)."""
     B, sp, lp = _kv4_args(cache, slots, lens)
     dev, n, n_q = cache.device, q.shape[1], q.shape[2]
     shape = (B, n, n_q, cache.head_dim)
