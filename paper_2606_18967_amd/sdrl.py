@@ -278,6 +278,11 @@ class Engine:
                                       pps, _dev(kv_len, "kv_len", torch.int32, (self.max_slots,), self.device)))
         self._keep_kv = (k, v, block_table, kv_len)
 
+    def _on_current_device(self):
+        # what follows allocates or launches on the current device
+        if self.device != _current():
+            raise ValueError(f"engine on {self.device}, the current device is {_current()}")
+
     def alloc_kv4(self, n_pages: int, page_size: int, block_table: torch.Tensor) -> "KV4Cache":
         """A 4-bit cache of n_pages pages for this model (KV4Cache); block_table as bind_kv_paged."""
         c = self.cfg
@@ -289,11 +294,13 @@ class Engine:
         """Prefill, draft, verify, AR step and rollback run on the 4-bit cache from here on."""
         if cache.device != self.device:
             raise ValueError(f"cache on {cache.device}, engine is on {self.device}")
+        self._on_current_device()
         _check(lib().sd_bind_kv4(self.h, cache._ref))
         self._keep_kv = cache
 
     def set_rope(self, rope: "RopeConfig"):
         """Replaces the engine's rotary table (on the current stream) for every later call."""
+        self._on_current_device()
         _check(lib().sd_set_rope(self.h, C.byref(rope.c), _stream()))
 
     def drafter_bytes(self, fmt: str = "w4") -> int:
