@@ -734,7 +734,9 @@ __global__ void __launch_bounds__(256, 2) k_kv4_attn(rows_t r, kv4_geom g, int n
     // value keeps all its bits down to 2^-26 of the slice's largest (elements over 16; the others to 2^-30) and is off by
     // 2^-34 of it below that, 2^-25 of the largest of a row whose exponent is 8 less.  Where one is smaller, or infinite,
     // or the common factor could leave fp32, the rows are `apart`: each has its own power of two, which the products give
-    // back, and an infinite or NaN query stays in its row.
+    // back on the path that moves references, and an infinite or NaN query stays in its row.  That path takes longer (us,
+    // with one head's queries 2^10 times the others': 64 rows at 8192 positions of 40 / 8 heads 100 instead of 92, 64 x 5
+    // 178 and 108, 8 x 512 at 4096 642 and 314).
     half8 qf[MQ][KW];
     float qsum[MQ], unit;
     uint64_t apart;                                                // 0 or a ballot
