@@ -289,7 +289,8 @@ def _plain_attention(st):
 
 
 def _softmax_parts(st):
-    """x = logits / T less the row's maximum, e^x, its sum, the tokens' log-probabilities and the entropy."""
+    """x = logits / T less the row's maximum, e^x, its sum and that one's logarithm, the tokens' log-probabilities, the
+    entropy, and the rows' norm: (largest logit, ln sum e^x)."""
     x = st["logits"].float() / st["T"]
     top = x.amax(1, keepdim=True)
     x = x - top
@@ -298,7 +299,7 @@ def _softmax_parts(st):
     z = torch.log(total)
     logp = (x.gather(1, st["tokens"].long()[:, None]) - z)[:, 0]
     entropy = (z - (e * x).sum(1, keepdim=True) / total)[:, 0]
-    return x, e, total, z, logp, entropy, (top + z)[:, 0]
+    return x, e, total, z, logp, entropy, torch.stack((st["logits"].amax(1).float(), z[:, 0]), 1)
 
 
 def _logits_gradient(st, x, e, total, z, entropy, dlogp, dentropy):
@@ -311,10 +312,10 @@ def _logits_gradient(st, x, e, total, z, entropy, dlogp, dentropy):
 
 
 def _plain_logp(st):
-    x, e, total, z, logp, entropy, lse = _softmax_parts(st)
+    x, e, total, z, logp, entropy, norm = _softmax_parts(st)
     if not st["grad"]:
-        return logp, entropy, lse
-    return logp, entropy, lse, _logits_gradient(st, x, e, total, z, entropy, st["dlogp"], st["dentropy"])
+        return logp, entropy, norm
+    return logp, entropy, norm, _logits_gradient(st, x, e, total, z, entropy, st["dlogp"], st["dentropy"])
 
 
 def _plain_policy(st):
@@ -371,11 +372,11 @@ def run(state):
             return sdrl.prefix_attention(cache, st["groups_"], LAYER, st["slots"], st["q"], st["out"], lens=st["lens"],
                                          workspace=st["workspace"])
         if st["op"] == "logp":
-            logp, entropy, lse = sdrl.token_logprobs(st["logits"], st["tokens"], st["T"], workspace=st["workspace"])
+            logp, entropy, norm = sdrl.token_logprobs(st["logits"], st["tokens"], st["T"], workspace=st["workspace"])
             if not st["grad"]:
-                return logp, entropy, lse
-            return logp, entropy, lse, sdrl.token_logprobs_grad(st["logits"], st["tokens"], lse, st["dlogp"], st["T"], entropy=entropy,
-                                                                dentropy=st["dentropy"], out=st["dlogits"])
+                return logp, entropy, norm
+            return logp, entropy, norm, sdrl.token_logprobs_grad(st["logits"], st["tokens"], norm, st["dlogp"], st["T"], entropy=entropy,
+                                                                 dentropy=st["dentropy"], out=st["dlogits"])
         out = sdrl.policy_loss(cache, st["logits"], st["tokens"], st["old"], st["advantage"], st["weight"], ref_logp=st["ref"],
                                behavior_logp=st["behavior"], dlogits=st["dlogits"], workspace=st["workspace"])
         return out.stats, out.logp, out.entropy, out.dlogits
@@ -455,7 +456,8 @@ def _exact_rows(st):
     """Row blocks, by torch's own softmax in 64 bits."""
     rows, V, T = st["rows"], st["V"], st["T"]
     policy = st["op"] == "policy"
-    logp, entropy, lse = (torch.zeros(rows, dtype=torch.float64, device="cuda") for _ in range(3))
+    logp, entropy = (torch.zeros(rows, dtype=torch.float64, device="cuda") for _ in range(2))
+    norm = torch.zeros((rows, 2), dtype=torch.float64, device="cuda")
     grad = torch.zeros((rows, V), dtype=torch.float32, device="cuda") if policy or st["grad"] else None
     sums = torch.zeros(6, dtype=torch.float64, device="cuda")
     step = max(1, (1 << 26) // V)
@@ -466,7 +468,8 @@ def _exact_rows(st):
         at = st["tokens"][cut].long()[:, None]
         lp = y.gather(1, at)[:, 0]
         H = -torch.where(p > 0, p * y, 0.0).sum(1)
-        lse[cut] = st["logits"][cut].double().gather(1, at)[:, 0] / T - lp
+        norm[cut, 0] = st["logits"][cut].double().max(1)[0]
+        norm[cut, 1] = -y.max(1)[0]
         if policy:
             w, old, A = st["weight"][cut].double(), st["old"][cut].double(), st["advantage"][cut].double()
             ratio_b = torch.exp(old - st["behavior"][cut].double())
@@ -493,7 +496,7 @@ def _exact_rows(st):
             grad[cut] = (d / T).float()
     if policy:
         return sums, logp, entropy, grad
-    return (logp, entropy, lse) if grad is None else (logp, entropy, lse, grad)
+    return (logp, entropy, norm) if grad is None else (logp, entropy, norm, grad)
 
 
 def exact(case, seed):
