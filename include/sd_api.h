@@ -274,6 +274,62 @@ sd_status sd_kv4_attention(const sd_kv4_cache* c, int32_t layer, int32_t B, int3
  * fp32 model), SD_E_NOMEM. */
 sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c);
 
+/* --------------------------------------- logits rows: what a learner needs of them
+ * The calls below need no engine and allocate nothing.  logits: rows x vocab of
+ * sd_dtype `dtype` at row stride ld >= vocab (elements; any element alignment),
+ * x = logits/temperature, p = softmax(x).  A row whose token is outside [0,
+ * vocab) (sd_accept's -1, padding) is absent: its logits are not read, its outputs
+ * are zeros.  A logit of -inf has p = 0 and no gradient; a row with a NaN, a +inf
+ * or no finite logit gives NaN.  Gradients have logits' type, are rounded once,
+ * and are written whole; dlogits may be logits itself (same stride), but not overlap it
+ * otherwise.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then only
+ * the loss's stats are written.  workspace: 256-byte aligned, its contents need no
+ * preparation, calls whose work may overlap need one each.  Errors: SD_E_INVAL,
+ * SD_E_UNSUPPORTED (more than 2^21 rows). */
+size_t sd_logits_workspace_bytes(int32_t rows, int32_t vocab);
+
+/* logp[r] = ln p(tokens[r]), entropy[r] = -sum p ln p (may be NULL), norm[r] = (the
+ * row's largest logit, ln sum e^(x - max x)) (float[rows][2], may be NULL). */
+sd_status sd_token_logprobs(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t ld,
+                            const int32_t* tokens, float temperature, float* logp, float* entropy, float* norm,
+                            void* workspace, size_t bytes, void* stream);
+
+/* The gradient of sum_r dlogp[r] logp[r] + dentropy[r] entropy[r] with respect to
+ * the logits, from sd_token_logprobs' norm and entropy:
+ *   dlogits[r][j] = (dlogp ([j = token] - p_j) - dentropy p_j (ln p_j + entropy))/T.
+ * entropy and dentropy go together (both may be NULL). */
+sd_status sd_token_logprobs_grad(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t ld,
+                                 const int32_t* tokens, float temperature, const float* norm, const float* dlogp,
+                                 const float* entropy, const float* dentropy, void* dlogits, int64_t dlogits_ld,
+                                 void* stream);
+
+/* The clipped policy loss of a batch of response tokens (GRPO's form, the training
+ * the rollouts are for: Sec. 5.1), with A = advantage, r = e^(logp - old_logp),
+ * d = ref_logp - logp and H the entropy:
+ *   l = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^d - d - 1)
+ *       - entropy_coef H,        loss = sum_r weight[r] l[r].
+ * weight carries the averaging (over tokens, or over sequences and then tokens); a
+ * row of weight 0 is absent.  With behavior_logp (the probabilities that the tokens
+ * were drawn with), rows whose e^(old_logp - behavior_logp) is outside [is_low,
+ * is_high], or NaN, are dropped: absent, but for stats[5].  ref_logp NULL: no KL term
+ * (kl_coef 0).  Outputs: stats[6] = the loss, and the weighted sums of its clipped
+ * term, of its KL term, of H, of the tokens whose gradient the clipping cuts, and of
+ * the dropped rows' weights; logp and entropy (may be NULL) as above; dlogits (may be
+ * NULL): the loss's gradient.  Where the ratio is at a border the unclipped side's
+ * gradient is taken. */
+typedef struct {
+    float temperature;
+    float clip_low, clip_high;      /* 0 <= clip_low <= 1, 0 <= clip_high */
+    float kl_coef, entropy_coef;
+    float is_low, is_high;          /* 0 <= is_low <= is_high, the latter may be infinite (read with behavior_logp) */
+    int32_t reserved;               /* 0 */
+} sd_policy_cfg;
+
+sd_status sd_policy_loss(const sd_policy_cfg* cfg, int32_t dtype, int32_t rows, int32_t vocab, const void* logits,
+                         int64_t ld, const int32_t* tokens, const float* old_logp, const float* behavior_logp,
+                         const float* ref_logp, const float* advantage, const float* weight, float* stats, float* logp,
+                         float* entropy, void* dlogits, int64_t dlogits_ld, void* workspace, size_t bytes, void* stream);
+
 /* Drafter weight formats (RTN, groups of 128 weights along K, one fp16 scale
  * per (output column, group)): int4 symmetric (Sec. 4.1, the default), int4
  * asymmetric with a zero point per (column, group) (App. B.2), and int8

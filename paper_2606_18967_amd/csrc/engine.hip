@@ -1106,6 +1106,104 @@ extern "C" sd_status sd_dense_gemm_bf16(const void* A, const void* W, float* C, 
     return SD_OK;
 }
 
+// ------------------------------------------------------------------ logits rows
+constexpr int LOGITS_MAX_ROWS = 1 << 21;     // a launch has fewer than 2^32 threads
+
+extern "C" size_t sd_logits_workspace_bytes(int32_t rows, int32_t vocab)
+{
+    if (rows < 0 || rows > LOGITS_MAX_ROWS || vocab < 1) return 0;
+    return align256(logits_work_floats(rows, vocab) * 4 + 1);
+}
+
+// rows of logits and, where `out` is not NULL, of their gradient
+static sd_status check_logits(int dtype, int rows, int vocab, const void* x, int64_t ld, const void* tok, float T,
+                              const void* out, int64_t out_ld)
+{
+    if (dtype != SD_DTYPE_F32 && dtype != SD_DTYPE_BF16) return fail(SD_E_INVAL, "dtype must be F32 or BF16");
+    if (rows < 0 || vocab < 1) return fail(SD_E_INVAL, "need rows >= 0 and vocab >= 1 (got %d, %d)", rows, vocab);
+    if (rows > LOGITS_MAX_ROWS) return fail(SD_E_UNSUPPORTED, "rows=%d are more than %d", rows, LOGITS_MAX_ROWS);
+    if (!(T > 0.f) || !isfinite(T) || !isfinite(1.4426950408889634f / T))
+        return fail(SD_E_INVAL, "temperature must be finite and > 0, its inverse too");
+    if (!rows) return SD_OK;
+    const int el = dtype == SD_DTYPE_F32 ? 4 : 2;
+    if (!x || !tok) return fail(SD_E_INVAL, "logits or tokens is NULL");
+    if ((uintptr_t)x % el || (uintptr_t)out % el) return fail(SD_E_INVAL, "logits and dlogits must be aligned to their elements");
+    if (ld < vocab || ld > INT_MAX) return fail(SD_E_INVAL, "ld=%lld outside [vocab, 2^31)", (long long)ld);
+    if (!out) return SD_OK;
+    if (out_ld < vocab || out_ld > INT_MAX) return fail(SD_E_INVAL, "dlogits_ld=%lld outside [vocab, 2^31)", (long long)out_ld);
+    const uintptr_t a = (uintptr_t)x, b = (uintptr_t)out;
+    const uintptr_t ae = a + ((uintptr_t)(rows - 1) * ld + vocab) * el, be = b + ((uintptr_t)(rows - 1) * out_ld + vocab) * el;
+    if (a < be && b < ae && !(a == b && (ld == out_ld || rows == 1)))
+        return fail(SD_E_INVAL, "dlogits must be logits itself, at the same stride, or not overlap it");
+    return SD_OK;
+}
+
+static sd_status check_logits_ws(int rows, int vocab, const void* ws, size_t bytes)
+{
+    if (!ws || ((uintptr_t)ws & 255)) return fail(SD_E_INVAL, "workspace is NULL or not 256-byte aligned");
+    const size_t need = sd_logits_workspace_bytes(rows, vocab);
+    if (bytes < need) return fail(SD_E_INVAL, "workspace holds %zu bytes, need %zu", bytes, need);
+    return SD_OK;
+}
+
+static logits_args logits_of(const void* x, int64_t ld, void* out, int64_t out_ld, int V, float T)
+{
+    return logits_args{x, ld, out, out_ld, V, T, 1.4426950408889634f / T, V};
+}
+
+extern "C" sd_status sd_token_logprobs(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t ld,
+                                       const int32_t* tokens, float T, float* logp, float* entropy, float* norm,
+                                       void* workspace, size_t bytes, void* stream)
+{
+    sd_status st = check_logits(dtype, rows, vocab, logits, ld, tokens, T, nullptr, 0);
+    if (st != SD_OK || !rows) return st;
+    if (!logp) return fail(SD_E_INVAL, "logp is NULL");
+    if ((st = check_logits_ws(rows, vocab, workspace, bytes)) != SD_OK) return st;
+    launch_token_logprobs(logits_of(logits, ld, nullptr, 0, vocab, T), logp_args{tokens, logp, entropy, norm}, rows,
+                          dtype == SD_DTYPE_F32, (float*)workspace, (hipStream_t)stream);
+    return launched("sd_token_logprobs");
+}
+
+extern "C" sd_status sd_token_logprobs_grad(int32_t dtype, int32_t rows, int32_t vocab, const void* logits, int64_t ld,
+                                            const int32_t* tokens, float T, const float* norm, const float* dlogp,
+                                            const float* entropy, const float* dentropy, void* dlogits, int64_t dlogits_ld,
+                                            void* stream)
+{
+    sd_status st = check_logits(dtype, rows, vocab, logits, ld, tokens, T, dlogits, dlogits_ld);
+    if (st != SD_OK || !rows) return st;
+    if (!norm || !dlogp || !dlogits) return fail(SD_E_INVAL, "NULL norm, dlogp or dlogits");
+    if (!entropy != !dentropy) return fail(SD_E_INVAL, "entropy and dentropy go together");
+    launch_token_logprobs_grad(logits_of(logits, ld, dlogits, dlogits_ld, vocab, T),
+                               logp_grad_args{tokens, norm, dlogp, entropy, dentropy}, rows, dtype == SD_DTYPE_F32,
+                               (hipStream_t)stream);
+    return launched("sd_token_logprobs_grad");
+}
+
+extern "C" sd_status sd_policy_loss(const sd_policy_cfg* cfg, int32_t dtype, int32_t rows, int32_t vocab, const void* logits,
+                                    int64_t ld, const int32_t* tokens, const float* old_logp, const float* behavior_logp,
+                                    const float* ref_logp, const float* advantage, const float* weight, float* stats,
+                                    float* logp, float* entropy, void* dlogits, int64_t dlogits_ld, void* workspace,
+                                    size_t bytes, void* stream)
+{
+    if (!cfg) return fail(SD_E_INVAL, "cfg is NULL");
+    sd_status st = check_logits(dtype, rows, vocab, logits, ld, tokens, cfg->temperature, dlogits, dlogits_ld);
+    if (st != SD_OK) return st;
+    if (cfg->reserved) return fail(SD_E_INVAL, "reserved must be 0");
+    if (!(cfg->clip_low >= 0.f && cfg->clip_low <= 1.f) || !(cfg->clip_high >= 0.f) || !isfinite(cfg->clip_high))
+        return fail(SD_E_INVAL, "need clip_low in [0, 1] and clip_high >= 0, finite");
+    if (!isfinite(cfg->kl_coef) || !isfinite(cfg->entropy_coef)) return fail(SD_E_INVAL, "kl_coef and entropy_coef must be finite");
+    if (behavior_logp && !(cfg->is_low >= 0.f && cfg->is_low <= cfg->is_high)) return fail(SD_E_INVAL, "need 0 <= is_low <= is_high");
+    if (!stats) return fail(SD_E_INVAL, "stats is NULL");
+    if (rows && (!old_logp || !advantage || !weight || !logp)) return fail(SD_E_INVAL, "NULL old_logp, advantage, weight or logp");
+    if (rows && !ref_logp && cfg->kl_coef != 0.f) return fail(SD_E_INVAL, "kl_coef needs ref_logp");
+    if ((st = check_logits_ws(rows, vocab, workspace, bytes)) != SD_OK) return st;
+    policy_args p = {tokens, old_logp, behavior_logp, ref_logp, advantage, weight, cfg->clip_low, cfg->clip_high, cfg->kl_coef,
+                     cfg->entropy_coef, (float)log((double)cfg->is_low), (float)log((double)cfg->is_high), logp, entropy, nullptr};
+    launch_policy_loss(logits_of(logits, ld, dlogits, dlogits_ld, vocab, cfg->temperature), p, rows, dtype == SD_DTYPE_F32,
+                       (float*)workspace, stats, (hipStream_t)stream);
+    return launched("sd_policy_loss");
+}
+
 extern "C" sd_status sd_timing(sd_engine e, int32_t on)
 {
     if (!e) return fail(SD_E_INVAL, "engine is NULL");

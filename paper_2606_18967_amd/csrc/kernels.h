@@ -275,3 +275,35 @@ void launch_accept(const rows_t& r, int gamma, int V, float T, rng_t rng, const 
                    float* work, hipStream_t s);
 size_t accept_work_floats(int B, int gamma);
 size_t accept_part_floats(int B, int gamma, int V);
+
+// ---- logits rows (kernels_logits.hip): x fp32 or bf16, row stride ld; c = log2(e)/T;
+// out: the gradient's rows (type of x), may be x, or NULL.  chunk is the launcher's.
+struct logits_args {
+    const void* x;
+    long long ld;
+    void* out;
+    long long out_ld;
+    int V;
+    float T, c;
+    int chunk;
+};
+struct logp_args {
+    const int32_t* tok;
+    float *logp, *entropy, *norm;  // the last two may be NULL
+};
+struct logp_grad_args {
+    const int32_t* tok;
+    const float *norm, *dlogp, *entropy, *dentropy;  // dentropy may be NULL, entropy with it
+};
+constexpr int POLICY_TERMS = 6;
+struct policy_args {
+    const int32_t* tok;
+    const float *old_logp, *behavior, *ref_logp, *adv, *weight;  // behavior and ref_logp may be NULL
+    float clip_low, clip_high, kl_coef, entropy_coef, log_is_low, log_is_high;
+    float *logp, *entropy;         // entropy may be NULL
+    float* terms;                  // [rows][POLICY_TERMS], the launcher's
+};
+size_t logits_work_floats(int rows, int V);
+void launch_token_logprobs(logits_args a, const logp_args& p, int rows, bool f32, float* work, hipStream_t s);
+void launch_token_logprobs_grad(logits_args a, const logp_grad_args& p, int rows, bool f32, hipStream_t s);
+void launch_policy_loss(logits_args a, policy_args p, int rows, bool f32, float* work, float* stats, hipStream_t s);

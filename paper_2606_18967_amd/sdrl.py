@@ -37,6 +37,7 @@ API_SYMBOLS = (
     "sd_alpha_from_tau", "sd_timing", "sd_timing_read", "sd_dense_gemm_bf16", "sd_accept_noalloc",
     "sd_rope_table", "sd_set_rope", "sd_kv4_page_bytes", "sd_kv4_append", "sd_kv4_read", "sd_kv4_workspace_bytes",
     "sd_kv4_attention", "sd_bind_kv4",
+    "sd_logits_workspace_bytes", "sd_token_logprobs", "sd_token_logprobs_grad", "sd_policy_loss",
 )
 
 # kernel classes of sd_timing_read
@@ -83,6 +84,11 @@ class RopeCfg(C.Structure):
 
 class RopeArgs(C.Structure):
     _fields_ = [("table", C.c_void_p), ("len", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class PolicyCfg(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("temperature", "clip_low", "clip_high", "kl_coef", "entropy_coef", "is_low", "is_high")] + \
+        [("reserved", C.c_int32)]
 
 
 class KV4Struct(C.Structure):
@@ -143,6 +149,10 @@ def lib():
             "sd_kv4_workspace_bytes": (_sz, [_P, _i32, _i32, _i32]),
             "sd_kv4_attention": (_i32, [_P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _f, _P, _i64, _P, _sz, _P]),
             "sd_bind_kv4": (_i32, [_P, _P]),
+            "sd_logits_workspace_bytes": (_sz, [_i32, _i32]),
+            "sd_token_logprobs": (_i32, [_i32, _i32, _i32, _P, _i64, _P, _f, _P, _P, _P, _P, _sz, _P]),
+            "sd_token_logprobs_grad": (_i32, [_i32, _i32, _i32, _P, _i64, _P, _f, _P, _P, _P, _P, _P, _i64, _P]),
+            "sd_policy_loss": (_i32, [_P, _i32, _i32, _i32, _P, _i64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _i64, _P, _sz, _P]),
             "sd_tau_from_alpha": (_d, [_d, _i32]),
             "sd_alpha_from_tau": (_d, [_d, _i32]),
         }
@@ -662,6 +672,125 @@ def kv4_workspace_bytes(cache: KV4Cache, B: int, n: int, n_q: int) -> int:
             raise SDError(SD_E_INVAL, lib().sd_last_error().decode(errors="replace"))
         cache._ws_bytes[B, n, n_q] = nb
     return nb
+
+
+# ------------------------------------------------- logits rows: log-probabilities, policy loss
+def logits_workspace_bytes(rows: int, vocab: int) -> int:
+    """Bytes of the workspace of token_logprobs and policy_loss."""
+    nb = int(lib().sd_logits_workspace_bytes(rows, vocab))
+    if not nb:
+        raise SDError(SD_E_UNSUPPORTED, f"rows={rows}, vocab={vocab}: need 0 to 2^21 rows and a vocabulary")
+    return nb
+
+
+def _logit_rows(t, name: str, shape=None, dtype=None, dev=None):
+    """Logits [..., V]: the pointer, the rows' stride in elements, and the sd_dtype."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: expected a device tensor")
+    if t.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name}: expected {dtype or 'float32 or bfloat16'}, got {t.dtype}")
+    if t.dim() < 1 or t.shape[-1] < 1 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape) if shape is not None else '[..., V]'}, got {tuple(t.shape)}")
+    if dev is not None and t.device != dev:
+        raise ValueError(f"{name}: on {t.device}, expected {dev}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    V, st, ld = t.shape[-1], t.stride(), None
+    rows = 1
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(st[:-1])):
+        if size == 1:
+            continue
+        if ld is None:
+            ld = stride
+        elif stride != rows * ld:
+            raise ValueError(f"{name}: rows must lie at one stride, got strides {st}")
+        rows *= size
+    ld = V if ld is None or not rows else ld
+    if (V > 1 and st[-1] != 1) or ld < V:
+        raise ValueError(f"{name}: rows must be contiguous and not overlap, got strides {st}")
+    return t.data_ptr(), ld, SD_DTYPE_BF16 if t.dtype == torch.bfloat16 else SD_DTYPE_F32
+
+
+def _rows_workspace(workspace, rows, V, dev):
+    if workspace is None:
+        workspace = torch.empty(logits_workspace_bytes(rows, V), dtype=torch.uint8, device=dev)
+    return workspace, _ptr(workspace, "workspace", torch.uint8, None, dev), workspace.numel()
+
+
+def token_logprobs(logits, tokens, T: float = 1.0, workspace=None):
+    """Log-probabilities of tokens under softmax(logits / T), the rows' entropies, and their norms (largest logit,
+    ln sum e^((logit - largest)/T)): logits [..., V] (fp32 or bf16, rows at one stride), tokens int32 [...];
+    returns fp32 logp [...], entropy [...] and norm [..., 2].  A token outside [0, V), as the -1 that accept
+    writes past n_emit, has no row: zeros.  workspace: a uint8 tensor of logits_workspace_bytes, for callers that
+    keep one."""
+    xp, ld, dt = _logit_rows(logits, "logits")
+    dev, V, shape, rows = logits.device, logits.shape[-1], logits.shape[:-1], tokens.numel()
+    tp = _ptr(tokens, "tokens", torch.int32, shape, dev)
+    workspace, wp, nb = _rows_workspace(workspace, rows, V, dev)     # (held until the call is enqueued)
+    logp, entropy, norm = (torch.empty(s, dtype=torch.float32, device=dev) for s in (shape, shape, (*shape, 2)))
+    _check(lib().sd_token_logprobs(dt, rows, V, xp, ld, tp, T, logp.data_ptr(), entropy.data_ptr(), norm.data_ptr(), wp, nb,
+                                   _stream()))
+    return logp, entropy, norm
+
+
+def token_logprobs_grad(logits, tokens, norm, dlogp, T: float = 1.0, entropy=None, dentropy=None, out=None):
+    """The gradient of sum(dlogp * logp) + sum(dentropy * entropy) by the logits, in their type, from token_logprobs'
+    norm (and entropy, which goes with dentropy); out may be logits itself."""
+    xp, ld, dt = _logit_rows(logits, "logits")
+    dev, shape = logits.device, logits.shape[:-1]
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    op, o_ld, _ = _logit_rows(out, "out", logits.shape, logits.dtype, dev)
+    if (entropy is None) != (dentropy is None):
+        raise ValueError("entropy and dentropy go together")
+    f32 = lambda t, name, s=shape: None if t is None else _ptr(t, name, torch.float32, s, dev)
+    _check(lib().sd_token_logprobs_grad(dt, tokens.numel(), logits.shape[-1], xp, ld, _ptr(tokens, "tokens", torch.int32, shape, dev), T,
+                                        f32(norm, "norm", (*shape, 2)), f32(dlogp, "dlogp"), f32(entropy, "entropy"),
+                                        f32(dentropy, "dentropy"), op, o_ld, _stream()))
+    return out
+
+
+class PolicyLoss:
+    """Coefficients of the clipped policy loss (sd_policy_cfg): the ratio is clipped to [1 - clip_low, 1 + clip_high],
+    tokens whose importance ratio old/behavior is outside [is_low, is_high] are dropped."""
+
+    def __init__(self, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
+                 is_low: float = 0.5, is_high: float = 2.0, temperature: float = 1.0):
+        self.c = PolicyCfg(temperature, clip_low, clip_high, kl_coef, entropy_coef, is_low, is_high, 0)
+
+
+class PolicyOut:
+    """policy_loss's results.  stats: fp32 [6], the loss and the weighted sums named in STATS."""
+    STATS = ("loss", "policy", "kl", "entropy", "clipped", "dropped")
+
+    def __init__(self, stats, logp, entropy, dlogits):
+        self.stats, self.logp, self.entropy, self.dlogits = stats, logp, entropy, dlogits
+
+    @property
+    def loss(self):
+        return self.stats[0]
+
+
+def policy_loss(cfg: PolicyLoss, logits, tokens, old_logp, advantage, weight, ref_logp=None, behavior_logp=None, dlogits=None,
+                grad: bool = True, workspace=None) -> PolicyOut:
+    """The clipped policy loss sum(weight * l) of response tokens, with a KL term to ref_logp, an entropy term and the
+    filter by behavior_logp (what the tokens were drawn with), and its gradient by the logits: logits and tokens as
+    token_logprobs, the others fp32 of tokens' shape.  dlogits: where the gradient goes (may be logits itself); None
+    makes a tensor, unless grad is False.  A trainer passes it on with logits.backward(out.dlogits)."""
+    xp, ld, dt = _logit_rows(logits, "logits")
+    dev, V, shape, rows = logits.device, logits.shape[-1], logits.shape[:-1], tokens.numel()
+    tp = _ptr(tokens, "tokens", torch.int32, shape, dev)
+    if dlogits is None and grad:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    op, o_ld = (None, 0) if dlogits is None else _logit_rows(dlogits, "dlogits", logits.shape, logits.dtype, dev)[:2]
+    f32 = lambda t, name: None if t is None else _ptr(t, name, torch.float32, shape, dev)
+    workspace, wp, nb = _rows_workspace(workspace, rows, V, dev)     # (held until the call is enqueued)
+    stats = torch.empty(6, dtype=torch.float32, device=dev)
+    logp, entropy = (torch.empty(shape, dtype=torch.float32, device=dev) for _ in range(2))
+    _check(lib().sd_policy_loss(C.byref(cfg.c), dt, rows, V, xp, ld, tp, f32(old_logp, "old_logp"), f32(behavior_logp, "behavior_logp"),
+                                f32(ref_logp, "ref_logp"), f32(advantage, "advantage"), f32(weight, "weight"), stats.data_ptr(),
+                                logp.data_ptr(), entropy.data_ptr(), op, o_ld, wp, nb, _stream()))
+    return PolicyOut(stats, logp, entropy, dlogits)
 
 
 def dense_gemm_bf16(A: torch.Tensor, W: torch.Tensor, out: torch.Tensor):

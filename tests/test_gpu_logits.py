@@ -1,0 +1,311 @@
+"""Token log-probabilities, their gradient and the policy loss against the formulas in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import logits_ref as ref
+from paper_2606_18967_amd import sdrl
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def rows(R, V, dtype, seed, ld=None, offset=0, spread=3.0):
+    """Logits [R, V] of rows at stride ld that start `offset` elements past an aligned address, and their values."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((R, V), generator=g) * spread
+    x[:, : min(4, V)] += 8 * torch.rand((R, min(4, V)), generator=g)
+    ld = ld or V
+    buf = torch.full((R * ld + offset,), float("nan"), dtype=DT[dtype], device="cuda")
+    t = buf[offset:].as_strided((R, V), (ld, 1))
+    t.copy_(x)
+    return t, t.double().cpu().numpy()
+
+
+def tokens(R, V, seed, absent=True):
+    t = np.random.default_rng(seed).integers(0, V, R).astype(np.int32)
+    t[0], t[R // 2] = V - 1, 0
+    if absent and R > 3:
+        t[1], t[2], t[R - 1] = -1, V, np.iinfo(np.int32).max
+    return t, torch.from_numpy(t).cuda()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def y_max(x, T):
+    f = np.where(np.isfinite(x), x, np.nan)
+    return min(np.nanmax(np.nanmax(f, 1) - np.nanmin(f, 1)) / T, 110.0)      # further down nothing is added
+
+
+def check_stats(x, t, T, logp, entropy, norm=None):
+    lp, H, nm = ref.logprobs(x, t, T)
+    es = ref.sum_error(x.shape[1], y_max(x, T))
+    # ln s: the sum's relative error, and its logarithm's; (x - max)/T is two roundings
+    tol = es + ref.E24 * (4 * np.abs(nm[:, 1]) + 2 * np.abs(lp) + 2 * np.abs(nm[:, 1]) + 4)
+    assert (np.abs(host(logp) - lp) <= tol).all(), np.max(np.abs(host(logp) - lp) / tol)
+    # H = ln s - t/s: t is as exact as s, relative to sum e |y|
+    tol_h = es * (2 + 2 * np.abs(nm[:, 1]) + 2 * H) + ref.E24 * (8 * np.abs(nm[:, 1]) + 8 * H + 8)
+    assert (np.abs(host(entropy) - H) <= tol_h).all(), np.max(np.abs(host(entropy) - H) / tol_h)
+    if norm is not None:
+        assert np.array_equal(host(norm)[:, 0], nm[:, 0])
+        assert (np.abs(host(norm)[:, 1] - nm[:, 1]) <= tol).all()
+
+
+def check_gradient(x, t, T, g, h, out, dtype, more=0.0):
+    """more: what the rows' factors g and h are off by themselves, relative."""
+    d, scale = ref.gradient(x, t, T, g, h)
+    es = ref.sum_error(x.shape[1], y_max(x, T)) * 4 + ref.E24 * 64 + more
+    tol = es * scale + ref.HALF_STEP[dtype] * np.abs(d) + 1e-38
+    off = np.abs(host(out) - d)
+    assert (off <= tol).all(), np.max(off / tol)
+
+
+SHAPES = [(1, 1), (1, 2), (5, 3), (7, 64), (9, 511), (33, 512), (6, 1023), (4, 4099), (5, 33001), (3, 70003), (600, 130), (513, 2051),
+          (2, 152064)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,V", SHAPES)
+def test_logprobs_and_gradient(R, V, dtype):
+    T = 0.7 if V % 2 else 1.0
+    x, xh = rows(R, V, dtype, R + V)
+    t, tok = tokens(R, V, V)
+    logp, entropy, norm = sdrl.token_logprobs(x, tok, T)
+    check_stats(xh, t, T, logp, entropy, norm)
+    rng = np.random.default_rng(R)
+    g, h = (rng.normal(size=R).astype(np.float32) for _ in range(2))
+    gd, hd = torch.from_numpy(g).cuda(), torch.from_numpy(h).cuda()
+    check_gradient(xh, t, T, g, 0 * h, sdrl.token_logprobs_grad(x, tok, norm, gd, T), dtype)
+    out = sdrl.token_logprobs_grad(x, tok, norm, gd, T, entropy=entropy, dentropy=hd)
+    check_gradient(xh, t, T, g, h, out, dtype)
+    same = sdrl.token_logprobs_grad(x, tok, norm, gd, T, entropy=entropy, dentropy=hd, out=x)
+    assert same is x and torch.equal(x.float(), out.float())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,ld,offset", [(1000, 1001, 1), (1000, 1024, 3), (515, 517, 5), (40001, 40003, 7)])
+def test_strides_and_alignments(V, ld, offset, dtype):
+    R, T = 6, 1.0
+    x, xh = rows(R, V, dtype, V, ld, offset)
+    t, tok = tokens(R, V, 3, absent=False)
+    logp, entropy, norm = sdrl.token_logprobs(x, tok, T)
+    check_stats(xh, t, T, logp, entropy, norm)
+    buf = torch.full((R * (ld + 6) + 2,), 7.0, dtype=DT[dtype], device="cuda")
+    out = buf[2:].as_strided((R, V), (ld + 6, 1))
+    g = np.ones(R, np.float32)
+    sdrl.token_logprobs_grad(x, tok, norm, torch.ones(R, device="cuda"), T, out=out)
+    check_gradient(xh, t, T, g, 0 * g, out, dtype)
+    gap = buf[2:].as_strided((R, ld + 6), (ld + 6, 1))[:, V:]
+    assert (gap == 7).all() and (buf[:2] == 7).all()
+
+
+def test_leading_dimensions():
+    x, xh = rows(12, 300, "f32", 0)
+    t, tok = tokens(12, 300, 1)
+    a = sdrl.token_logprobs(x.view(3, 4, 300), tok.view(3, 4))
+    b = sdrl.token_logprobs(x, tok)
+    assert a[0].shape == (3, 4) and a[2].shape == (3, 4, 2)
+    assert all(torch.equal(p.reshape(q.shape), q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("V", [700, 40000])
+def test_masked_and_odd_logits(V):
+    R, T = 8, 1.0
+    x, _ = rows(R, V, "f32", 5)
+    x[0, ::2] = -float("inf")                                     # half the vocabulary masked
+    x[1] = -float("inf")
+    x[1, V // 3] = 2.5                                            # one token left
+    x[2] = -float("inf")                                          # nothing left
+    x[3, 17] = float("nan")
+    x[4, V - 1] = float("inf")
+    x[5] = 1e30                                                   # equal and huge
+    x[6, 5] = -3e38
+    t = np.array([1, V // 3, 3, 4, 5, 6, 7, 8], np.int32)
+    tok = torch.from_numpy(t).cuda()
+    logp, H, norm = sdrl.token_logprobs(x, tok, T)
+    fine = [0, 1, 5, 6, 7]
+    xh = host(x)
+    check_stats(xh[fine], t[fine], T, logp[fine], H[fine], norm[fine])
+    assert torch.isnan(logp[[2, 3, 4]]).all() and logp[1] == 0 and H[1] == 0
+    one = torch.ones(R, device="cuda")
+    d = sdrl.token_logprobs_grad(x, tok, norm, one, T, entropy=H, dentropy=one)
+    check_gradient(xh[fine], t[fine], T, np.ones(5), np.ones(5), d[fine], "f32")
+    assert (d[0, ::2] == 0).all() and torch.isnan(d[3]).all()
+
+
+def policy_inputs(xh, t, T, seed, pad=0.3):
+    R, rng = len(t), np.random.default_rng(seed)
+    lp = ref.logprobs(np.where(np.isfinite(xh), xh, 0), t, T)[0]
+    def step(width, *borders):
+        """Differences of log-probabilities, none within 1e-3 of a border, which a rounding of ln p does not cross."""
+        d = rng.normal(size=R) * width
+        for b in borders:
+            d = np.where(np.abs(d - b) < 1e-3, d + 3e-3, d)
+        return d
+    old = lp - step(0.4, np.log(0.8), np.log(1.28))
+    v = dict(old=old, adv=rng.normal(size=R), w=np.where(rng.random(R) < pad, 0, rng.random(R)), ref=lp + step(0.3),
+             beh=old - step(0.5, np.log(0.5), np.log(2)))
+    return {k: a.astype(np.float32) for k, a in v.items()}
+
+
+def run_policy(x, tok, v, kl, ent, T, **kw):
+    cfg = sdrl.PolicyLoss(0.2, 0.28, kl, ent, 0.5, 2.0, T)
+    d = {k: torch.from_numpy(a).cuda() for k, a in v.items()}
+    return sdrl.policy_loss(cfg, x, tok, d["old"], d["adv"], d["w"], ref_logp=d.get("ref"), behavior_logp=d.get("beh"), **kw)
+
+
+def check_policy(xh, t, v, kl, ent, T, out, dtype):
+    stats, lp, H, g, h = ref.policy(xh, t, T, v["old"], v["adv"], v["w"], v.get("ref"), v.get("beh"), 0.2, 0.28, kl, ent)
+    es = ref.sum_error(xh.shape[1], y_max(xh, T))
+    live = H != 0
+    e_lp = (es + ref.E24 * 8 * (np.abs(lp) + 30))                 # of ln p, as check_stats has it (ln s < 5 |ln p| + 30)
+    assert (np.abs(host(out.logp) - lp) <= e_lp).all()
+    assert (host(out.logp)[~live] == 0).all() and (host(out.entropy)[~live] == 0).all()
+    # the terms' sums: an error of ln p and H moves each term by its slope at most; e^x of |x| < 4 has 2^-22
+    slope = np.abs(v["w"]) * (np.exp(4) * (np.abs(v["adv"]) + 1) + 1)
+    tol = ((e_lp + ref.E24 * 16 + 4 * es * (1 + np.abs(H))) * np.where(live, slope, 0)).sum() + ref.E24 * np.abs(stats)
+    assert (np.abs(host(out.stats) - stats) <= tol).all(), (host(out.stats), stats, tol)
+    if out.dlogits is not None:
+        d, _ = ref.gradient(np.where(live[:, None], xh, 0), t, T, g, h)
+        # g moves by e^4 (|A| + kl) w at most for an error of ln p: relative to g itself unless terms cancel there
+        scale = ref.gradient(np.where(live[:, None], xh, 0), t, T, np.where(live, slope, 0), h)[1]
+        tol = (e_lp[:, None] + es * 4 + ref.E24 * 64) * scale + ref.HALF_STEP[dtype] * np.abs(d) + 1e-38
+        off = np.abs(host(out.dlogits) - d)
+        assert (off <= tol).all(), np.max(off / tol)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kl,ent", [(0.0, 0.0), (0.1, 0.0), (0.05, 0.02)])
+@pytest.mark.parametrize("R,V", [(1, 5), (40, 129), (96, 512), (515, 1030), (70, 20011), (3, 50257)])
+def test_policy_loss(R, V, kl, ent, dtype):
+    T = 1.3 if V % 2 else 1.0
+    x, xh = rows(R, V, dtype, R)
+    t, tok = tokens(R, V, R)
+    v = policy_inputs(xh, t, T, R)
+    v["w"][0] = 0.5
+    out = run_policy(x, tok, v, kl, ent, T)
+    check_policy(xh, t, v, kl, ent, T, out, dtype)
+    less = run_policy(x, tok, v, kl, ent, T, grad=False)
+    assert less.dlogits is None and torch.equal(less.stats, out.stats) and torch.equal(less.logp, out.logp)
+    same = run_policy(x, tok, v, kl, ent, T, dlogits=x)
+    assert torch.equal(same.dlogits.float(), out.dlogits.float()) and torch.equal(same.stats, out.stats)
+
+
+@pytest.mark.parametrize("V", [300, 30000])
+def test_policy_without_reference_and_filter(V):
+    x, xh = rows(20, V, "bf16", 1)
+    t, tok = tokens(20, V, 1)
+    v = policy_inputs(xh, t, 1.0, 1)
+    del v["ref"], v["beh"]
+    check_policy(xh, t, v, 0.0, 0.01, 1.0, run_policy(x, tok, v, 0.0, 0.01, 1.0), "bf16")
+
+
+@pytest.mark.parametrize("V", [300, 30000])
+def test_policy_absent_rows_are_not_read(V):
+    """NaN in the logits and values of absent rows reaches nothing; their gradient is zeros."""
+    R = 16
+    x, xh = rows(R, V, "f32", 2)
+    t, tok = tokens(R, V, 2)
+    v = policy_inputs(xh, t, 1.0, 2, pad=0.5)
+    v["w"][3] = 0
+    v["w"][4] = 1
+    v["beh"][4] = np.nan                                          # dropped by the filter
+    dead = (v["w"] == 0) | (t < 0) | (t >= V)
+    for k in ("old", "adv", "ref", "beh"):
+        v[k][dead] = np.nan
+    x[torch.from_numpy(dead).cuda()] = float("nan")
+    out = run_policy(x, tok, v, 0.1, 0.01, 1.0)
+    check_policy(np.where(dead[:, None], 0, xh), t, v, 0.1, 0.01, 1.0, out, "f32")
+    assert (out.dlogits[torch.from_numpy(dead).cuda()] == 0).all() and host(out.stats)[5] >= 1
+
+
+@pytest.mark.parametrize("V", [120, 20000])
+def test_policy_gradient_against_differences(V):
+    """The kernel's gradient against differences of the loss in 64 bits."""
+    R, T = 6, 1.0
+    x, xh = rows(R, V, "f32", 9)
+    t, tok = tokens(R, V, 9, absent=False)
+    v = policy_inputs(xh, t, T, 9, pad=0.0)
+    d = host(run_policy(x, tok, v, 0.1, 0.05, T).dlogits)
+    f = lambda x: ref.policy(x, t, T, v["old"], v["adv"], v["w"], v["ref"], v["beh"], 0.2, 0.28, 0.1, 0.05)[0][0]  # noqa: E731
+    for r in range(R):
+        for j in {int(t[r]), 0, 3, V - 1}:
+            e = np.zeros_like(xh)
+            e[r, j] = 1e-5
+            # 64 bits leave 1e-10 of the difference; the kernel 32 bits' 1e-4 of a slope below e^2
+            assert abs((f(xh + e) - f(xh - e)) / 2e-5 - d[r, j]) < 1e-4
+
+
+def test_empty_batch():
+    x, t, z = torch.zeros((0, 50), device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, device="cuda")
+    assert sdrl.token_logprobs(x, t)[0].shape == (0,)
+    assert sdrl.token_logprobs_grad(x, t, torch.zeros((0, 2), device="cuda"), z).shape == (0, 50)
+    out = sdrl.policy_loss(sdrl.PolicyLoss(), x, t, z, z, z)
+    assert (out.stats == 0).all() and out.dlogits.shape == (0, 50)
+
+
+def test_python_refusals():
+    x, t = torch.zeros((4, 64), device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    z = torch.zeros(4, device="cuda")
+    bad = [(x.half(), t), (x, t.long()), (x, t[:3]), (x.t(), t), (x[:1].expand(4, 64), t), (x[:, ::2], t)]
+    for a, b in bad:
+        with pytest.raises(ValueError):
+            sdrl.token_logprobs(a, b)
+        with pytest.raises(ValueError):
+            sdrl.policy_loss(sdrl.PolicyLoss(), a, b, z, z, z)
+    with pytest.raises(ValueError):
+        sdrl.token_logprobs(x, t, workspace=torch.empty(64, device="cuda"))
+    with pytest.raises(sdrl.SDError):
+        sdrl.token_logprobs(x, t, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(sdrl.SDError):
+        sdrl.policy_loss(sdrl.PolicyLoss(kl_coef=0.1), x, t, z, z, z)
+    big = torch.zeros(4 * 64 + 8, device="cuda")
+    with pytest.raises(sdrl.SDError, match="overlap"):
+        sdrl.policy_loss(sdrl.PolicyLoss(), big[:256].view(4, 64), t, z, z, z, dlogits=big[8:].view(4, 64))
+    with pytest.raises(ValueError):
+        sdrl.token_logprobs_grad(x, t, torch.zeros((4, 2), device="cuda"), z, entropy=z)
+
+
+@pytest.mark.parametrize("R,V", [(520, 700), (12, 40000)])
+def test_in_a_graph_and_on_a_stream(R, V):
+    """Replays with other inputs in the same buffers, eager work between them, on a stream of their own."""
+    T = 1.0
+    x, _ = rows(R, V, "bf16", 0)
+    t, tok = tokens(R, V, 0)
+    v = policy_inputs(host(x), t, T, 0)
+    d = {k: torch.from_numpy(a).cuda() for k, a in v.items()}
+    cfg = sdrl.PolicyLoss(0.2, 0.28, 0.1, 0.01)
+    ws = torch.empty(sdrl.logits_workspace_bytes(R, V), dtype=torch.uint8, device="cuda")
+    call = lambda w: sdrl.policy_loss(cfg, x, tok, d["old"], d["adv"], d["w"], ref_logp=d["ref"], behavior_logp=d["beh"], workspace=w)  # noqa: E731
+    call(ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with sdrl.no_collection(), torch.cuda.graph(graph, stream=side):
+        out = call(ws)
+    torch.cuda.current_stream().wait_stream(side)
+    for seed in range(1, 4):
+        y, yh = rows(R, V, "bf16", seed)
+        x.copy_(y)
+        d["adv"].copy_(torch.randn(R, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = call(None)
+        for a, b in ((out.stats, eager.stats), (out.logp, eager.logp), (out.entropy, eager.entropy), (out.dlogits, eager.dlogits)):
+            assert torch.equal(a, b)
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.current_stream())
+            other = call(None)
+        side.synchronize()
+        assert torch.equal(other.dlogits, eager.dlogits) and torch.equal(other.stats, eager.stats)
+
+
+@pytest.mark.parametrize("R,V", [(520, 700), (12, 40000)])
+def test_same_bits_again(R, V):
+    x, xh = rows(R, V, "bf16", 4)
+    t, tok = tokens(R, V, 4)
+    v = policy_inputs(xh, t, 1.0, 4)
+    a, b = run_policy(x, tok, v, 0.1, 0.01, 1.0), run_policy(x, tok, v, 0.1, 0.01, 1.0)
+    assert torch.equal(a.stats, b.stats) and torch.equal(a.dlogits, b.dlogits) and torch.equal(a.logp, b.logp)
