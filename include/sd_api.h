@@ -274,6 +274,57 @@ sd_status sd_kv4_attention(const sd_kv4_cache* c, int32_t layer, int32_t B, int3
  * fp32 model), SD_E_NOMEM. */
 sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c);
 
+/* ------------------------------------------- groups of rollouts of one prompt
+ * A paged bf16 cache for the calls without an engine: K and V pools as those of
+ * sd_bind_kv_paged, [n_pages][n_layers][n_kv][page_size][head_dim] each, tables,
+ * lengths and flags as sd_kv4_cache's. */
+typedef struct {
+    void* k_pages;              /* bf16, 16-byte aligned */
+    void* v_pages;
+    const int32_t* block_table; /* int32[max_slots][pages_per_seq] */
+    int32_t* kv_len;            /* int32[max_slots] */
+    uint32_t* flags;            /* uint32[5] or NULL */
+    int32_t n_pages, page_size, pages_per_seq;  /* page_size: a multiple of 32, pages_per_seq * page_size >= max_ctx */
+    int32_t n_layers, n_kv, head_dim;           /* head_dim 64 or 128 */
+    int32_t max_slots, max_ctx;                 /* max_ctx up to 2^24 */
+} sd_kv_cache;
+
+/* Which sequences share their first positions (the G responses that are sampled of
+ * each prompt): slot s belongs to group[s] (device int32[max_slots]; outside [0,
+ * n_groups): none), and the positions [0, len[g]) (device int32[n_groups]) of all
+ * slots of group g hold the same keys and values, as they do where their block
+ * tables name the same pages.  Sequences of a group that follow one another in a
+ * call's batch and have at least len[g] positions cached (fewer: as many as the
+ * shortest has) are attended together: what they share, in whole tiles of 64
+ * positions, is read once, through the table of the first of them.  A batch in
+ * another order is attended right too, and reads more. */
+typedef struct {
+    const int32_t* group;
+    const int32_t* len;
+    int32_t n_groups;           /* >= 1 */
+    int32_t reserved;           /* 0 */
+} sd_prefix_groups;
+
+/* sd_kv4_append's rows (same arguments) stored in bf16: k rotated in fp32 and
+ * rounded once, v rounded, at kv_len[slots[b]] + i of layer `layer`, q rotated into
+ * q_out.  Slots named in one call write pages of their own. */
+sd_status sd_kv_append(const sd_kv_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots, const int32_t* lens,
+                       int32_t dtype, const void* k, int64_t k_ld, const void* v, int64_t v_ld, const void* q, int64_t q_ld,
+                       int32_t n_q, void* q_out, const sd_rope_args* rope, void* stream);
+
+/* Bytes of the workspace of sd_prefix_attention (0 for arguments it refuses). */
+size_t sd_prefix_workspace_bytes(const sd_kv_cache* c, int32_t B, int32_t n, int32_t n_q);
+
+/* sd_kv4_attention's rows (same arguments) over the bf16 cache: row (b, i) sees the
+ * positions up to its own, appended before.  groups may be NULL: nothing is shared.
+ * B up to 1024.  Scores, the softmax's statistics and all sums are fp32, the
+ * probabilities enter the second product in bf16 (2^-8 of each).  The results do
+ * not depend on what a row does not see; a key or value that is not finite makes the
+ * rows that see it NaN.  A missing page's positions are as if masked. */
+sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_groups* groups, int32_t layer, int32_t B, int32_t n,
+                              const int32_t* slots, const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld, float scale,
+                              void* out, int64_t out_ld, void* workspace, size_t bytes, void* stream);
+
 /* --------------------------------------- logits rows: what a learner needs of them
  * The calls below need no engine and allocate nothing.  logits: rows x vocab of
  * sd_dtype `dtype` at row stride ld >= vocab (elements; any element alignment),

@@ -550,6 +550,28 @@ static rows_t kv4_rows(const sd_kv4_cache& c, int B, int n, const int32_t* slots
     return r;
 }
 
+// the rows of an append, and its rotation
+static sd_status check_append(int n_kv, int D, int dtype, const void* k, int64_t k_ld, const void* v, int64_t v_ld, const void* q,
+                              int64_t q_ld, int n_q, const void* q_out, const sd_rope_args* rope, kv4_rope* ro)
+{
+    if (dtype != SD_DTYPE_F32 && dtype != SD_DTYPE_BF16) return fail(SD_E_INVAL, "dtype must be F32 or BF16");
+    const int el = dtype == SD_DTYPE_F32 ? 4 : 2;
+    if (!rows_ok(k, k_ld, n_kv, D, el) || !rows_ok(v, v_ld, n_kv, D, el))
+        return fail(SD_E_INVAL, "k and v must be 16-byte aligned, with row strides of whole 16 bytes >= n_kv*head_dim");
+    if (!q != !q_out) return fail(SD_E_INVAL, "q and q_out go together");
+    if (q && (n_q < 1 || !rows_ok(q, q_ld, n_q, D, el) || ((uintptr_t)q_out & 15)))
+        return fail(SD_E_INVAL, "n_q >= 1, q and q_out 16-byte aligned, q's row stride whole 16 bytes >= n_q*head_dim");
+    *ro = kv4_rope{nullptr, 0, 0, 0};
+    if (rope && rope->rot_dim) {
+        if (rope->rot_dim < 0 || rope->rot_dim > D || rope->rot_dim % 16)
+            return fail(SD_E_INVAL, "rot_dim=%d must be a multiple of 16 in [0, head_dim]", rope->rot_dim);
+        if (!rope->table || ((uintptr_t)rope->table & 15) || rope->len < 1)
+            return fail(SD_E_INVAL, "the rotary table must be 16-byte aligned and hold at least one position");
+        *ro = kv4_rope{(const float2*)rope->table, rope->len, rope->rot_dim, rope->interleaved != 0};
+    }
+    return SD_OK;
+}
+
 extern "C" sd_status sd_kv4_append(const sd_kv4_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
                                    const int32_t* lens, int32_t dtype, const void* k, int64_t k_ld, const void* v,
                                    int64_t v_ld, const void* q, int64_t q_ld, int32_t n_q, void* q_out,
@@ -557,21 +579,9 @@ extern "C" sd_status sd_kv4_append(const sd_kv4_cache* c, int32_t layer, int32_t
 {
     sd_status st = check_kv4_call(c, layer, B, n, slots);
     if (st != SD_OK) return st;
-    if (dtype != SD_DTYPE_F32 && dtype != SD_DTYPE_BF16) return fail(SD_E_INVAL, "dtype must be F32 or BF16");
-    const int el = dtype == SD_DTYPE_F32 ? 4 : 2, D = c->head_dim;
-    if (!rows_ok(k, k_ld, c->n_kv, D, el) || !rows_ok(v, v_ld, c->n_kv, D, el))
-        return fail(SD_E_INVAL, "k and v must be 16-byte aligned, with row strides of whole 16 bytes >= n_kv*head_dim");
-    if (!q != !q_out) return fail(SD_E_INVAL, "q and q_out go together");
-    if (q && (n_q < 1 || !rows_ok(q, q_ld, n_q, D, el) || ((uintptr_t)q_out & 15)))
-        return fail(SD_E_INVAL, "n_q >= 1, q and q_out 16-byte aligned, q's row stride whole 16 bytes >= n_q*head_dim");
-    kv4_rope ro = {nullptr, 0, 0, 0};
-    if (rope && rope->rot_dim) {
-        if (rope->rot_dim < 0 || rope->rot_dim > D || rope->rot_dim % 16)
-            return fail(SD_E_INVAL, "rot_dim=%d must be a multiple of 16 in [0, head_dim]", rope->rot_dim);
-        if (!rope->table || ((uintptr_t)rope->table & 15) || rope->len < 1)
-            return fail(SD_E_INVAL, "the rotary table must be 16-byte aligned and hold at least one position");
-        ro = kv4_rope{(const float2*)rope->table, rope->len, rope->rot_dim, rope->interleaved != 0};
-    }
+    kv4_rope ro;
+    if ((st = check_append(c->n_kv, c->head_dim, dtype, k, k_ld, v, v_ld, q, q_ld, n_q, q_out, rope, &ro)) != SD_OK) return st;
+    const int D = c->head_dim;
     // a launch has fewer than 2^32 threads
     const double waves = (double)B * (n / 8 + 2) * 2 * c->n_kv + (q ? (double)B * n * (n_q / (2048 / D) + 1) : 0.0);
     if (waves > 6e7) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
@@ -677,6 +687,116 @@ extern "C" sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c)
     e->kv_len = c->kv_len;
     e->kv4 = true;
     return SD_OK;
+}
+
+// ------------------------------------------------------------------ groups that share a prompt
+static sd_status check_pages(const sd_kv_cache* c)
+{
+    if (!c) return fail(SD_E_INVAL, "cache is NULL");
+    if (!c->k_pages || !c->v_pages || !c->block_table || !c->kv_len) return fail(SD_E_INVAL, "k_pages, v_pages, block_table or kv_len is NULL");
+    if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages) & 15) return fail(SD_E_INVAL, "k_pages and v_pages must be 16-byte aligned");
+    if (c->n_layers < 1 || c->n_kv < 1 || (c->head_dim != 64 && c->head_dim != 128) || c->page_size < 32 || c->page_size % 32)
+        return fail(SD_E_INVAL, "need n_layers, n_kv >= 1, head_dim 64 or 128 and page_size a positive multiple of 32 (got %d, %d, %d, %d)",
+                    c->n_layers, c->n_kv, c->head_dim, c->page_size);
+    if (c->n_pages < 1 || c->max_slots < 1) return fail(SD_E_INVAL, "need n_pages and max_slots >= 1");
+    if (c->max_ctx < 1 || c->max_ctx > KV4_MAX_CTX) return fail(SD_E_INVAL, "max_ctx=%d outside [1, %d]", c->max_ctx, KV4_MAX_CTX);
+    if (c->pages_per_seq < 1 || (long long)c->pages_per_seq * c->page_size < c->max_ctx)
+        return fail(SD_E_INVAL, "pages_per_seq * page_size = %lld must cover max_ctx = %d",
+                    (long long)c->pages_per_seq * c->page_size, c->max_ctx);
+    return SD_OK;
+}
+
+static sd_status check_pages_call(const sd_kv_cache* c, int layer, int B, int n, const void* slots)
+{
+    sd_status st = check_pages(c);
+    if (st != SD_OK) return st;
+    if (!slots) return fail(SD_E_INVAL, "slots is NULL");
+    if (layer < 0 || layer >= c->n_layers) return fail(SD_E_INVAL, "layer=%d outside [0, %d)", layer, c->n_layers);
+    if (B < 1 || B > c->max_slots) return fail(SD_E_INVAL, "B=%d outside [1, %d]", B, c->max_slots);
+    if (n < 1 || n > c->max_ctx) return fail(SD_E_INVAL, "n=%d outside [1, max_ctx=%d]", n, c->max_ctx);
+    return SD_OK;
+}
+
+static sd_status check_groups(const sd_prefix_groups* g)
+{
+    if (!g) return SD_OK;
+    if (!g->group || !g->len || g->n_groups < 1) return fail(SD_E_INVAL, "group and len must not be NULL, n_groups >= 1");
+    if (g->reserved) return fail(SD_E_INVAL, "reserved must be 0");
+    return SD_OK;
+}
+
+static cache_t pages_of(const sd_kv_cache& c)
+{
+    const long long D = c.head_dim, H = c.n_kv, L = c.n_layers, P = c.page_size;
+    return cache_t{c.k_pages, c.v_pages, 0, c.n_kv, c.head_dim,
+                   kv_geom{c.page_size, L * H * P * D, H * P * D, P * D, c.block_table, c.pages_per_seq, c.n_pages}};
+}
+
+static rows_t page_rows(const sd_kv_cache& c, int B, int n, const int32_t* slots, const int32_t* lens)
+{
+    rows_t r = {B, n, 0, slots, c.kv_len, c.max_slots, c.max_ctx, c.flags};
+    r.lim = lens;
+    return r;
+}
+
+extern "C" sd_status sd_kv_append(const sd_kv_cache* c, int32_t layer, int32_t B, int32_t n, const int32_t* slots,
+                                  const int32_t* lens, int32_t dtype, const void* k, int64_t k_ld, const void* v, int64_t v_ld,
+                                  const void* q, int64_t q_ld, int32_t n_q, void* q_out, const sd_rope_args* rope, void* stream)
+{
+    sd_status st = check_pages_call(c, layer, B, n, slots);
+    if (st != SD_OK) return st;
+    kv4_rope ro;
+    if ((st = check_append(c->n_kv, c->head_dim, dtype, k, k_ld, v, v_ld, q, q_ld, n_q, q_out, rope, &ro)) != SD_OK) return st;
+    if ((double)B * n > 8e6) return fail(SD_E_UNSUPPORTED, "B*n=%lld rows are too many for one call", (long long)B * n);
+    const rows_t r = page_rows(*c, B, n, slots, lens);
+    const cache_t kv = pages_of(*c);
+    const hipStream_t s = (hipStream_t)stream;
+    if (dtype == SD_DTYPE_F32)
+        launch_kv_append(r, kv, layer, n_q, kv4_src<float>{(const float*)k, (size_t)k_ld}, kv4_src<float>{(const float*)v, (size_t)v_ld},
+                         kv4_src<float>{(const float*)q, (size_t)q_ld}, (uint16_t*)q_out, ro, s);
+    else
+        launch_kv_append(r, kv, layer, n_q, kv4_src<uint16_t>{(const uint16_t*)k, (size_t)k_ld}, kv4_src<uint16_t>{(const uint16_t*)v, (size_t)v_ld},
+                         kv4_src<uint16_t>{(const uint16_t*)q, (size_t)q_ld}, (uint16_t*)q_out, ro, s);
+    return launched("sd_kv_append");
+}
+
+static sd_status check_prefix_rows(int B, int n, int n_q, int n_kv)
+{
+    if (n_q < 1 || n_q % n_kv) return fail(SD_E_INVAL, "n_q=%d must be a positive multiple of n_kv=%d", n_q, n_kv);
+    if (B > PX_SEQS || (double)B * n * n_q > 1e8) return fail(SD_E_UNSUPPORTED, "B=%d, n=%d, n_q=%d are too many for one call", B, n, n_q);
+    return SD_OK;
+}
+
+extern "C" size_t sd_prefix_workspace_bytes(const sd_kv_cache* c, int32_t B, int32_t n, int32_t n_q)
+{
+    if (check_pages_call(c, 0, B, n, c) != SD_OK || check_prefix_rows(B, n, n_q, c->n_kv) != SD_OK) return 0;
+    return prefix_plan_bytes(prefix_plan(B, n, n_q, c->n_kv), B, c->n_kv, c->head_dim);
+}
+
+extern "C" sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_groups* groups, int32_t layer, int32_t B, int32_t n,
+                                         const int32_t* slots, const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld,
+                                         float scale, void* out, int64_t out_ld, void* workspace, size_t bytes, void* stream)
+{
+    sd_status st = check_pages_call(c, layer, B, n, slots);
+    if (st != SD_OK) return st;
+    if ((st = check_groups(groups)) != SD_OK) return st;
+    if ((st = check_prefix_rows(B, n, n_q, c->n_kv)) != SD_OK) return st;
+    if (!rows_ok(q, q_ld, n_q, c->head_dim, 2) || !rows_ok(out, out_ld, n_q, c->head_dim, 2))
+        return fail(SD_E_INVAL, "q and out must be 16-byte aligned, with row strides of whole 16 bytes >= n_q*head_dim");
+    if (!isfinite(scale)) return fail(SD_E_INVAL, "scale must be finite");
+    if (!workspace || ((uintptr_t)workspace & 255)) return fail(SD_E_INVAL, "workspace is NULL or not 256-byte aligned");
+    px_plan p = prefix_plan(B, n, n_q, c->n_kv);
+    const size_t need = prefix_plan_bytes(p, B, c->n_kv, c->head_dim);
+    if (bytes < need) return fail(SD_E_INVAL, "workspace holds %zu bytes, need %zu", bytes, need);
+    const rows_t r = page_rows(*c, B, n, slots, lens);
+    const cache_t kv = pages_of(*c);
+    const px_groups g = groups ? px_groups{groups->group, groups->len, groups->n_groups} : px_groups{};
+    const hipStream_t s = (hipStream_t)stream;
+    prefix_plan_bind(p, workspace, B, c->n_kv);
+    launch_prefix_plan(r, g, p, n_q, c->n_kv, s);
+    launch_prefix_attention(r, p, kv, layer, n_q, (const uint16_t*)q, q_ld, scale, out, ACT_BF16, out_ld, s);
+    launch_prefix_combine(r, p, n_q, c->n_kv, c->head_dim, out, ACT_BF16, out_ld, s);
+    return launched("sd_prefix_attention");
 }
 
 extern "C" sd_status sd_set_debug(sd_engine e, int32_t flags)

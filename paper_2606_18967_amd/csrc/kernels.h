@@ -276,6 +276,45 @@ void launch_accept(const rows_t& r, int gamma, int V, float T, rng_t rng, const 
 size_t accept_work_floats(int B, int gamma);
 size_t accept_part_floats(int B, int gamma, int V);
 
+// ---- groups that share a prompt, paged bf16 cache (kernels_prefix.hip).  In these
+// rows_t::err may be NULL, rows_t::row0 and live are not used.
+constexpr int PX_SEQS = 1024;            // sequences of a call
+constexpr int PX_TILE = 64;              // positions of a tile; what a group shares is whole tiles
+constexpr int PX_ROWS = 128;             // query rows of an item
+constexpr int PX_SHARED = 1 << 30;       // px_item::base of shared positions
+struct px_groups {
+    const int32_t* group;                // device [max_slots], or NULL: no sharing
+    const int32_t* len;                  // device [n_groups]
+    int n_groups;
+};
+// Rows [128 z, 128 z + 128) of the QR query rows a KV head that start at row row0 of
+// the call, over the positions [p0, p1) of `slot`; base: the first row's position (its
+// causal limit), or PX_SHARED.  part: the first row's partial row, -1 where the item
+// writes the output itself.  QR 0: no item.
+struct px_item { int row0, QR, slot, p0, p1, base, part, z; };
+// a sequence's partial rows: pfx_n chunks of its run at a stride of pfx_rows, then own_n of its own
+struct px_seq { int pfx_part, pfx_n, pfx_rows, own_part, own_n, pad; };
+struct px_plan {
+    px_seq* seq;                         // device [B]
+    px_item* item;                       // device [max_items]
+    float2* ml;                          // device [n_kv][part_rows]: (m, l) in base 2, and o [..][D]
+    float* o;
+    int target, min_chunk;               // items wanted, shortest chunk
+    long long max_items, part_rows;
+    int layer;                           // (the launcher's)
+};
+px_plan prefix_plan(int B, int n, int n_q, int n_kv);
+size_t prefix_plan_bytes(const px_plan& p, int B, int n_kv, int D);
+void prefix_plan_bind(px_plan& p, void* buf, int B, int n_kv);
+void launch_prefix_plan(const rows_t& r, const px_groups& g, const px_plan& p, int n_q, int n_kv, hipStream_t s);
+void launch_prefix_attention(const rows_t& r, px_plan p, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld, float scale,
+                             void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
+void launch_prefix_combine(const rows_t& r, const px_plan& p, int n_q, int n_kv, int D, void* out, act_t out_t, long long out_ld, hipStream_t s);
+// T as launch_kv4_append's; q_out NULL: K and V alone
+template <typename T>
+void launch_kv_append(const rows_t& r, const cache_t& c, int layer, int n_q, kv4_src<T> k, kv4_src<T> v, kv4_src<T> q, uint16_t* q_out,
+                      const kv4_rope& ro, hipStream_t s);
+
 // ---- logits rows (kernels_logits.hip): x fp32 or bf16, row stride ld; c = log2(e)/T;
 // out: the gradient's rows (type of x), may be x, or NULL.  chunk is the launcher's.
 struct logits_args {

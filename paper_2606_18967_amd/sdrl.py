@@ -37,6 +37,7 @@ API_SYMBOLS = (
     "sd_alpha_from_tau", "sd_timing", "sd_timing_read", "sd_dense_gemm_bf16", "sd_accept_noalloc",
     "sd_rope_table", "sd_set_rope", "sd_kv4_page_bytes", "sd_kv4_append", "sd_kv4_read", "sd_kv4_workspace_bytes",
     "sd_kv4_attention", "sd_bind_kv4",
+    "sd_kv_append", "sd_prefix_workspace_bytes", "sd_prefix_attention",
     "sd_logits_workspace_bytes", "sd_token_logprobs", "sd_token_logprobs_grad", "sd_policy_loss",
 )
 
@@ -84,6 +85,17 @@ class RopeCfg(C.Structure):
 
 class RopeArgs(C.Structure):
     _fields_ = [("table", C.c_void_p), ("len", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class KVStruct(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("block_table", C.c_void_p), ("kv_len", C.c_void_p),
+                ("flags", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("pages_per_seq", C.c_int32),
+                ("n_layers", C.c_int32), ("n_kv", C.c_int32), ("head_dim", C.c_int32), ("max_slots", C.c_int32),
+                ("max_ctx", C.c_int32)]
+
+
+class GroupsStruct(C.Structure):
+    _fields_ = [("group", C.c_void_p), ("len", C.c_void_p), ("n_groups", C.c_int32), ("reserved", C.c_int32)]
 
 
 class PolicyCfg(C.Structure):
@@ -149,6 +161,9 @@ def lib():
             "sd_kv4_workspace_bytes": (_sz, [_P, _i32, _i32, _i32]),
             "sd_kv4_attention": (_i32, [_P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _f, _P, _i64, _P, _sz, _P]),
             "sd_bind_kv4": (_i32, [_P, _P]),
+            "sd_kv_append": (_i32, [_P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _P, _i64, _P, _i64, _i32, _P, _P, _P]),
+            "sd_prefix_workspace_bytes": (_sz, [_P, _i32, _i32, _i32]),
+            "sd_prefix_attention": (_i32, [_P, _P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _f, _P, _i64, _P, _sz, _P]),
             "sd_logits_workspace_bytes": (_sz, [_i32, _i32]),
             "sd_token_logprobs": (_i32, [_i32, _i32, _i32, _P, _i64, _P, _f, _P, _P, _P, _P, _sz, _P]),
             "sd_token_logprobs_grad": (_i32, [_i32, _i32, _i32, _P, _i64, _P, _f, _P, _P, _P, _P, _P, _i64, _P]),
@@ -605,6 +620,10 @@ def kv4_append(cache: KV4Cache, layer: int, slots, k, v, q=None, q_out=None, rop
     positions kv_len + i of a layer, k rotated by the table `rope` (rope_table; None: not rotated) in pairs of
     "half" or "interleaved" layout, and rotates q [B][n][n_q][head_dim] into q_out (bf16).  lens [B]: rows of
     each sequence.  kv_len is not changed."""
+    _append(lib().sd_kv4_append, cache, layer, slots, k, v, q, q_out, rope, layout, lens)
+
+
+def _append(call, cache, layer, slots, k, v, q, q_out, rope, layout, lens):
     B, sp, lp = _kv4_args(cache, slots, lens)
     dev, D, n, dtype = cache.device, cache.head_dim, k.shape[1], k.dtype
     if dtype not in (torch.bfloat16, torch.float32):
@@ -624,8 +643,8 @@ def kv4_append(cache: KV4Cache, layer: int, slots, k, v, q=None, q_out=None, rop
     if rope is not None and rope.shape[1]:
         ra = C.byref(RopeArgs(_ptr(rope, "rope", torch.float32, (rope.shape[0], rope.shape[1], 2), dev), rope.shape[0],
                               2 * rope.shape[1], layout == "interleaved"))
-    _check(lib().sd_kv4_append(cache._ref, layer, B, n, sp, lp, SD_DTYPE_BF16 if dtype == torch.bfloat16 else SD_DTYPE_F32,
-                               kp, k_ld, vp, v_ld, qp, q_ld, n_q, op, ra, _stream()))
+    _check(call(cache._ref, layer, B, n, sp, lp, SD_DTYPE_BF16 if dtype == torch.bfloat16 else SD_DTYPE_F32,
+                kp, k_ld, vp, v_ld, qp, q_ld, n_q, op, ra, _stream()))
 
 
 def kv4_read(cache: KV4Cache, layer: int, slots, start, k_out, v_out, lens=None):
@@ -672,6 +691,88 @@ def kv4_workspace_bytes(cache: KV4Cache, B: int, n: int, n_q: int) -> int:
             raise SDError(SD_E_INVAL, lib().sd_last_error().decode(errors="replace"))
         cache._ws_bytes[B, n, n_q] = nb
     return nb
+
+
+# ------------------------------------------------- groups of rollouts of one prompt
+class KVPages:
+    """A paged bf16 KV cache for the calls without an engine (sd_kv_cache): pools k and v
+    [n_pages][n_layers][n_kv][page_size][head_dim] (Engine.alloc_kv_paged's), an int32 block table
+    [max_slots][pages_per_seq] and the int32 lengths kv_len [max_slots], all caller-owned.  check() reports what
+    calls found out of range on the device."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, max_ctx: int):
+        if k.dim() != 5 or block_table.dim() != 2 or kv_len.dim() != 1:
+            raise ValueError("expected pools [n_pages][layers][n_kv][page_size][head_dim], block_table [slots][pages], kv_len [slots]")
+        n_pages, n_layers, n_kv, page, head_dim = k.shape
+        slots = kv_len.shape[0]
+        if head_dim not in (64, 128) or page < 32 or page % 32:
+            raise ValueError(f"pools: head_dim {head_dim} and pages of {page}, expected 64 or 128 and a multiple of 32")
+        if block_table.shape[1] * page < max_ctx:
+            raise ValueError(f"block_table: {block_table.shape[1]} pages of {page} do not cover max_ctx={max_ctx}")
+        self.device = k.device
+        self.n_layers, self.n_kv, self.head_dim, self.page_size = n_layers, n_kv, head_dim, page
+        self.max_slots, self.max_ctx = slots, max_ctx
+        ptrs = (_dev(k, "k", torch.bfloat16), _dev(v, "v", torch.bfloat16, k.shape, self.device),
+                _dev(block_table, "block_table", torch.int32, (slots, block_table.shape[1]), self.device),
+                _dev(kv_len, "kv_len", torch.int32, None, self.device))
+        self.k, self.v, self.block_table, self.kv_len = k, v, block_table, kv_len
+        self.flags = torch.zeros(5, dtype=torch.int32, device=self.device)
+        self.c = KVStruct(*ptrs, C.c_void_p(self.flags.data_ptr()), n_pages, page, block_table.shape[1], n_layers, n_kv, head_dim,
+                          slots, max_ctx)
+        self._ref = C.byref(self.c)
+        self._ws_bytes = {}
+
+    check = KV4Cache.check
+
+
+class PrefixGroups:
+    """Which slots share their first positions (sd_prefix_groups): group int32 [max_slots] (outside [0, n_groups):
+    none) and length int32 [n_groups], device tensors that later calls read; the caller may change them between calls."""
+
+    def __init__(self, group: torch.Tensor, length: torch.Tensor):
+        if group.dim() != 1 or length.dim() != 1 or length.shape[0] < 1:
+            raise ValueError("expected group [max_slots] and length [n_groups]")
+        self.device = group.device
+        self.group, self.length = group, length
+        self.c = GroupsStruct(_dev(group, "group", torch.int32), _dev(length, "length", torch.int32, None, self.device), length.shape[0], 0)
+        self._ref = C.byref(self.c)
+
+
+def kv_append(cache: KVPages, layer: int, slots, k, v, q=None, q_out=None, rope=None, layout: str = "half", lens=None):
+    """kv4_append's rows stored in bf16."""
+    _append(lib().sd_kv_append, cache, layer, slots, k, v, q, q_out, rope, layout, lens)
+
+
+def prefix_workspace_bytes(cache: KVPages, B: int, n: int, n_q: int) -> int:
+    """Bytes of prefix_attention's workspace."""
+    nb = cache._ws_bytes.get((B, n, n_q))
+    if nb is None:
+        nb = int(lib().sd_prefix_workspace_bytes(cache._ref, B, n, n_q))
+        if not nb:
+            raise SDError(SD_E_INVAL, lib().sd_last_error().decode(errors="replace"))
+        cache._ws_bytes[B, n, n_q] = nb
+    return nb
+
+
+def prefix_attention(cache: KVPages, groups: PrefixGroups | None, layer: int, slots, q, out=None, scale: float | None = None, lens=None,
+                     workspace=None):
+    """kv4_attention's rows over the bf16 cache, the positions that sequences of a group share read once for all of
+    them (groups None: nothing is shared); the members of a group belong next to each other in slots."""
+    B, sp, lp = _kv4_args(cache, slots, lens)
+    dev, n, n_q = cache.device, q.shape[1], q.shape[2]
+    if groups is not None and (groups.device != dev or groups.group.shape[0] != cache.max_slots):
+        raise ValueError(f"groups: on {groups.device} for {groups.group.shape[0]} slots, the cache on {dev} has {cache.max_slots}")
+    shape = (B, n, n_q, cache.head_dim)
+    qp, q_ld = _rows(q, "q", torch.bfloat16, shape, dev)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    op, o_ld = _rows(out, "out", torch.bfloat16, shape, dev)
+    if workspace is None:
+        workspace = torch.empty(prefix_workspace_bytes(cache, B, n, n_q), dtype=torch.uint8, device=dev)
+    _check(lib().sd_prefix_attention(cache._ref, None if groups is None else groups._ref, layer, B, n, sp, lp, n_q, qp, q_ld,
+                                     cache.head_dim ** -0.5 if scale is None else scale, op, o_ld,
+                                     _ptr(workspace, "workspace", torch.uint8, None, dev), workspace.numel(), _stream()))
+    return out
 
 
 # ------------------------------------------------- logits rows: log-probabilities, policy loss
