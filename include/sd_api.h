@@ -325,6 +325,14 @@ sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_groups* grou
                               const int32_t* slots, const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld, float scale,
                               void* out, int64_t out_ld, void* workspace, size_t bytes, void* stream);
 
+/* Groups for the engine's own steps over the paged cache (sd_bind_kv_paged): draft,
+ * verify and AR step attend through sd_prefix_attention's kernels from here on,
+ * with the groups of each call's slots read on the device; prefill is as before.
+ * NULL ends it, and so does binding another cache.  Allocates buffers on first use.
+ * Errors: SD_E_INVAL, SD_E_STATE (no paged cache bound), SD_E_UNSUPPORTED (an fp32 model,
+ * more than 1024 slots), SD_E_NOMEM. */
+sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
+
 /* --------------------------------------- logits rows: what a learner needs of them
  * The calls below need no engine and allocate nothing.  logits: rows x vocab of
  * sd_dtype `dtype` at row stride ld >= vocab (elements; any element alignment),

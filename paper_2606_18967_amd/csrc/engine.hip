@@ -82,6 +82,8 @@ struct sd_engine_s {
     kv_geom geo = {};                  // dense or paged layout of k / v
     bool kv4 = false;                  // the cache is the 4-bit one of geo4 instead
     kv4_geom geo4 = {};
+    bool px = false;                   // steps share the prompts of groups (paged cache)
+    px_groups groups = {};
     std::vector<const uint32_t*> qw;   // [L*4] packed codes
     std::vector<const uint16_t*> qs;   // [L*4] scales
     std::vector<const uint8_t*> qz;    // [L*4] zero points (asymmetric format), else NULL
@@ -91,6 +93,7 @@ struct sd_engine_s {
     workspace ws;                // of a step's rows
     workspace pf;                // of a long prefill's rows, from the first one on
     void* plan = nullptr;        // the running forward's attention plan
+    void* px_buf = nullptr;      // the same of grouped sequences, and its partial results
     float* samp_part = nullptr;
     float* acc_work = nullptr;
     float2* rope = nullptr;
@@ -301,7 +304,7 @@ static void free_ws(sd_engine e)
         for (void* p : ps)
             if (p) (void)hipFree(p);
     }
-    void* ps[] = {e->plan, e->samp_part, e->acc_work, e->rope, e->err, e->pf_lim};
+    void* ps[] = {e->plan, e->px_buf, e->samp_part, e->acc_work, e->rope, e->err, e->pf_lim};
     for (void* p : ps)
         if (p) (void)hipFree(p);
 }
@@ -427,7 +430,7 @@ extern "C" sd_status sd_bind_kv(sd_engine e, void* k, void* v, int32_t* kv_len)
     e->v = v;
     e->kv_len = kv_len;
     const long long D = e->c.head_dim, H = e->c.n_kv, C = e->max_ctx;
-    e->kv4 = false;
+    e->kv4 = e->px = false;
     e->geo = kv_geom{e->max_ctx, H * C * D, (long long)e->max_slots * H * C * D, C * D, nullptr, 1, e->max_slots};
     return SD_OK;
 }
@@ -455,7 +458,7 @@ extern "C" sd_status sd_bind_kv_paged(sd_engine e, void* k_pages, void* v_pages,
     e->v = v_pages;
     e->kv_len = kv_len;
     const long long D = e->c.head_dim, H = e->c.n_kv, L = e->c.n_layers, P = page_size;
-    e->kv4 = false;
+    e->kv4 = e->px = false;
     e->geo = kv_geom{page_size, L * H * P * D, H * P * D, P * D, block_table, pages_per_seq, n_pages};
     return SD_OK;
 }
@@ -686,6 +689,7 @@ extern "C" sd_status sd_bind_kv4(sd_engine e, const sd_kv4_cache* c)
     e->geo4 = kv4_geom_of(*c);
     e->kv_len = c->kv_len;
     e->kv4 = true;
+    e->px = false;
     return SD_OK;
 }
 
@@ -797,6 +801,36 @@ extern "C" sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_g
     launch_prefix_attention(r, p, kv, layer, n_q, (const uint16_t*)q, q_ld, scale, out, ACT_BF16, out_ld, s);
     launch_prefix_combine(r, p, n_q, c->n_kv, c->head_dim, out, ACT_BF16, out_ld, s);
     return launched("sd_prefix_attention");
+}
+
+extern "C" sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups)
+{
+    if (!e) return fail(SD_E_INVAL, "engine is NULL");
+    if (!groups) {
+        e->px = false;
+        return SD_OK;
+    }
+    sd_status st = check_groups(groups);
+    if (st != SD_OK) return st;
+    if (e->f32) return fail(SD_E_UNSUPPORTED, "groups need a bf16 model");
+    if (!e->k || e->kv4 || !e->geo.bt) return fail(SD_E_STATE, "no paged KV cache bound");
+    if (e->max_slots > PX_SEQS) return fail(SD_E_UNSUPPORTED, "max_slots=%d are more than %d", e->max_slots, PX_SEQS);
+    if (e->max_ctx > KV4_MAX_CTX) return fail(SD_E_UNSUPPORTED, "max_ctx=%d is more than %d", e->max_ctx, KV4_MAX_CTX);
+    const sd_model_cfg& m = e->c;
+    if ((double)e->max_slots * (e->max_gamma + 1) * m.n_q > 1e8)
+        return fail(SD_E_UNSUPPORTED, "max_slots=%d with drafts of %d are too many", e->max_slots, e->max_gamma);
+    // the largest call's: its bytes grow with the sequences and with their rows
+    const size_t need = prefix_plan_bytes(prefix_plan(e->max_slots, e->max_gamma + 1, m.n_q, m.n_kv), e->max_slots, m.n_kv, m.head_dim);
+    const size_t qb = (size_t)e->ws.rows * m.n_q * m.head_dim * 2;
+    for (auto [p, bytes] : {std::pair<void**, size_t>(&e->px_buf, need), {&e->ws.qrot, qb}}) {
+        if (*p || hipMalloc(p, bytes) == hipSuccess) continue;
+        (void)hipGetLastError();
+        *p = nullptr;
+        return fail(SD_E_NOMEM, "workspace allocation of %zu bytes failed", bytes);
+    }
+    e->groups = px_groups{groups->group, groups->len, groups->n_groups};
+    e->px = true;
+    return SD_OK;
 }
 
 extern "C" sd_status sd_set_debug(sd_engine e, int32_t flags)
@@ -921,6 +955,25 @@ static void attend_kv4(sd_engine e, const workspace& ws, const rows_t& r, const 
     }
 }
 
+// The same over the paged bf16 cache with the prompts of groups shared.
+static void attend_groups(sd_engine e, const workspace& ws, const rows_t& r, const px_plan& plan, const cache_t& kv, int l, int S, act_t at,
+                          hipStream_t s)
+{
+    const sd_model_cfg& c = e->c;
+    const int D = c.head_dim, qd = c.n_q * D, kd = c.n_kv * D, ld = qd + 2 * kd;
+    auto whole = [&](int col) { return kv4_src<float>{ws.qkv + col, (size_t)ld}; };
+    auto parts = [&](int col) { return kv4_src<f32_parts>{ws.gpart + col, (size_t)ld, S, (size_t)r.B * r.n * ld}; };
+    uint16_t* q = (uint16_t*)ws.qrot;
+    { tscope t(e, T_MISC, s);
+      const kv4_rope ro = {e->rope, e->max_ctx, D, 0};
+      if (S > 1) launch_kv_append(r, kv, l, c.n_q, parts(qd), parts(qd + kd), parts(0), q, ro, s);
+      else launch_kv_append(r, kv, l, c.n_q, whole(qd), whole(qd + kd), whole(0), q, ro, s); }
+    { kscope t(e, r.n == 1 ? T_ATTN_D : T_ATTN_V);
+      launch_prefix_attention(r, plan, kv, l, c.n_q, q, qd, 1.f / sqrtf((float)D), ws.att, at, qd, s, t.start, t.stop); }
+    tscope t(e, T_MISC, s);
+    launch_prefix_combine(r, plan, c.n_q, c.n_kv, D, ws.att, at, qd, s);
+}
+
 // One forward pass over B sequences x n tokens (row r = b*n + i at position
 // kv_len + off + i).  Token of row (b, i): i == 0 ? tokA[b*sA] :
 // tokB[b*sB + i - 1].  If logits != NULL, row r's logits go to logits + r*ldl;
@@ -945,6 +998,14 @@ static void forward(sd_engine e, const workspace& ws, bool draft, int B, const i
     const int pcls = draft ? T_Q4 : T_PROJ;
     att_plan plan = attention_plan(B, n, c.n_q, c.n_kv, e->max_ctx, e->f32, e->kv4);
     attention_plan_bind(plan, e->plan, e->max_slots);
+    const bool px = e->px && logits;                 // (a prefill attends as without groups)
+    px_plan shared = {};
+    if (px) {
+        tscope t(e, T_MISC, s);
+        shared = prefix_plan(B, n, c.n_q, c.n_kv);
+        prefix_plan_bind(shared, e->px_buf, B, c.n_kv);
+        launch_prefix_plan(r, e->groups, shared, c.n_q, c.n_kv, s);
+    }
     int S;
     { tscope t(e, T_MISC, s);
       launch_embed_rmsnorm(r, tokA, sA, tokB, sB, e->w[0], e->f32, c.hidden, c.vocab, ws.h, W(e, 0, 0), c.rms_eps, ws.a, at, plan, s); }
@@ -955,6 +1016,8 @@ static void forward(sd_engine e, const workspace& ws, bool draft, int B, const i
         if (e->kv4) {
             attend_kv4(e, ws, r, plan, l, S, kv_only, at, s);
             if (kv_only) break;
+        } else if (px) {
+            attend_groups(e, ws, r, shared, kv, l, S, at, s);
         } else if (kv_only) {
             tscope t(e, T_MISC, s);
             launch_rope_kv(r, ws.qkv, ws.gpart, S, e->rope, c.n_q, kv, l, nullptr, s);

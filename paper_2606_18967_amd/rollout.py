@@ -28,6 +28,16 @@ of `prompt` positions per sequence (or, with --prefill, `prompt` random
 tokens prefilled through the target), the same for every policy, so the
 makespan measured is that of the decode phase.
 
+With a group of G > 1 the responses come in groups of G of one prompt (the
+paper samples 8 of each, Sec. 5.1): a group's block tables name the same pages
+for the prompt's whole pages, its prompt is prefilled once, and every step's
+attention reads it once for all of the group's live responses.  The toggle then
+prices the positions that a step reads, the shared ones once.
+
+With log-probabilities on, every response token's ln p under the policy that
+drew it is kept (speculative or not, tokens follow softmax(p / T) of the target),
+as the learner's importance ratios need it.
+
 With graphs on, the live batch of each iteration is padded up to a bucket (a
 multiple of BUCKET rows; the padding rows run on spare KV slots whose length
 is reset before every step) and each (bucket, draft length) SD step and each
@@ -49,6 +59,7 @@ import numpy as np
 from . import sdrl, synth
 
 POLICIES = ("ar", "sd", "toggle", "adaptive")
+PAGE = 64                          # positions of a page where groups share prompts
 BUCKET = 8                         # graph buckets: live batches padded to a multiple of this many rows
 
 
@@ -87,15 +98,31 @@ class RolloutResult:
     capture_s: float = 0.0              # their capture time (outside makespan_s)
 
 
+def grouped_tables(B: int, group: int, spare: int, prompt: int, max_ctx: int, page: int):
+    """Block table [B + spare][pages], group of each slot and number of pages of a paged cache whose slots
+    [g group, (g + 1) group) share the whole pages of one prompt; spare slots join the last group."""
+    if group < 1 or B % group:
+        raise ValueError(f"B={B} responses are not whole groups of {group}")
+    slots, per, shared = B + spare, -(-max_ctx // page), prompt // page
+    gid = np.minimum(np.arange(slots) // group, B // group - 1)
+    table = np.empty((slots, per), dtype=np.int32)
+    table[:, :shared] = gid[:, None] * shared + np.arange(shared)
+    first = (B // group) * shared
+    table[:, shared:] = first + np.arange(slots * (per - shared)).reshape(slots, per - shared)
+    return table, gid.astype(np.int32), first + slots * (per - shared)
+
+
 def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: float, cost, eps: float,
-           ar_fn, sd_fn, compact_fn, clock=time.perf_counter, keep_trace: bool = True) -> dict:
+           ar_fn, sd_fn, compact_fn, clock=time.perf_counter, keep_trace: bool = True, group: int = 1) -> dict:
     """The decode loop of one rollout (the while loop of Algorithm 1).
 
     ar_fn() and sd_fn(gamma) run one iteration on the current live rows and
     return the tokens each row emitted (host int array, in row order; SD
     counts n_emit before truncation at the response's end).  compact_fn(keep)
     drops the rows whose keep flag is False.  cost is an sdrl.CostModel for
-    the toggle.  Returns the loop's statistics."""
+    the toggle, which is given the mean positions that a step reads for a live
+    row: with groups of `group` rows a prompt counts once for its live ones.
+    Returns the loop's statistics."""
     if policy not in POLICIES:
         raise ValueError(f"unknown policy {policy!r}")
     B0 = len(lengths)
@@ -110,7 +137,8 @@ def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: 
     it = 0
     while live.size:
         Bl = int(live.size)
-        S_mean = prompt + float(np.minimum(gen[live], L[live]).mean())
+        prompts = np.unique(live // group).size if group > 1 else Bl
+        S_mean = prompt * prompts / Bl + float(np.minimum(gen[live], L[live]).mean())
         if policy in ("toggle", "adaptive") and not sd_on:
             sd_on = sdrl.toggle(cost, Bl, S_mean, tau_prev, gamma, eps, 0)
             if sd_on:
@@ -150,15 +178,18 @@ def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: 
 
 
 class Rollout:
-    """One model on the GPU with a dense KV cache (kv4: a paged one in 4 bits)
-    for B sequences of up to prompt + lmax positions, the drafter buffer, and flat device buffers
+    """One model on the GPU with a dense KV cache (kv4: a paged one in 4 bits; group > 1: a
+    paged one whose groups of so many share their prompt) for B sequences of up to prompt + lmax positions, the drafter buffer, and flat device buffers
     viewed at the live batch size and draft length of each iteration."""
 
     def __init__(self, cfg: dict, B: int, prompt: int, lmax: int, gmax: int = max(GAMMA_SET), seed: int = 3,
                  T: float = 1.0, fmt: str = "w4", graphs: bool = False, padded: bool | None = None,
-                 prefill: bool = False, kv4: bool = False):
+                 prefill: bool = False, kv4: bool = False, group: int = 1, logprobs: bool = False):
         import torch
         self.torch = torch
+        if group > 1 and kv4:
+            raise ValueError("groups share the pages of a cache of the model's type, not of the 4-bit one")
+        self.group, self.logprobs = group, logprobs
         self.cfg, self.B, self.prompt, self.gmax, self.seed, self.T, self.fmt = cfg, B, prompt, gmax, seed, T, fmt
         # padded: steps run at the bucket size (spare slots B .. B + BUCKET - 2 carry the padding rows);
         # graphs: the padded steps are captured and replayed
@@ -173,22 +204,45 @@ class Rollout:
             from . import calibrate
             self.cache = calibrate.bind_kv4_context(self.eng, 0 if prefill else prompt, seed + 100)
             self.kv_len = self.cache.kv_len
+        elif group > 1:
+            table, gid, n_pages = grouped_tables(B, group, self.spare, prompt, self.eng.max_ctx, PAGE)
+            self.k, self.v, self.kv_len = self.eng.alloc_kv_paged(n_pages, PAGE)
+            self.table = torch.from_numpy(table).to(self.dev)
+            self.eng.bind_kv_paged(self.k, self.v, self.table, self.kv_len)
+            self.groups = sdrl.PrefixGroups(torch.from_numpy(gid).to(self.dev),
+                                            torch.full((B // group,), prompt, dtype=torch.int32, device=self.dev))
+            self.eng.bind_prefix(self.groups)
         else:
             self.k, self.v, self.kv_len = self.eng.alloc_kv()
             self.eng.bind_kv(self.k, self.v, self.kv_len)
         self.prefill_s = None
         if prefill:
-            # real prompts: `prompt` random tokens per sequence through the target (every slot, spares too)
+            # real prompts: `prompt` random tokens per sequence through the target (every slot, spares too; of a
+            # group the first)
             nslots = B + self.spare
-            toks = synth.make_tokens(nslots, prompt, cfg["vocab"], seed + 5).to(self.dev).contiguous()
+            first = torch.arange(0, B if group > 1 else nslots, group, dtype=torch.int32, device=self.dev)
+            toks = synth.make_tokens(first.numel(), prompt, cfg["vocab"], seed + 5).to(self.dev).contiguous()
             torch.cuda.synchronize()
             t0 = time.perf_counter()
-            self.eng.prefill(torch.arange(nslots, dtype=torch.int32, device=self.dev), toks)
+            self.eng.prefill(first, toks)
             self.eng.sync()
             self.prefill_s = time.perf_counter() - t0
             del toks
+        elif group > 1:
+            # whole pages of random context for the prompts, and each group's first slot's page behind them
+            gen = torch.Generator(device=self.dev).manual_seed(seed + 100)
+            lead = self.table[:B:group, :-(-prompt // PAGE)].reshape(-1).long()
+            for t in (self.k, self.v):
+                for pg in lead.split(256):
+                    t[pg] = torch.randn((pg.numel(), *t.shape[1:]), generator=gen, device=self.dev).to(t.dtype)
         elif not kv4:
             synth.fill_kv_context(self.k, self.v, prompt, seed + 100)
+        if group > 1 and prompt % PAGE:
+            # the rest of the prompt, past its whole pages: every slot has its own copy, since its response follows there
+            own = self.table[:, prompt // PAGE].long()
+            src = own[torch.from_numpy(gid).to(self.dev).long() * group]
+            for t in (self.k, self.v):
+                t[own, :, :, :prompt % PAGE] = t[src, :, :, :prompt % PAGE]
         self.qbuf = self.eng.refresh_drafter(fmt=fmt)
         V, dev, i32, f32 = cfg["vocab"], self.dev, torch.int32, torch.float32
         B = B + self.spare
@@ -201,10 +255,26 @@ class Rollout:
                          next_tok=torch.zeros(B, dtype=i32, device=dev),
                          ar_out=torch.zeros(B, dtype=i32, device=dev),
                          ar_logits=torch.zeros(B * V, dtype=f32, device=dev))
+        # the responses and their tokens' ln p by slot and place; the last column takes what is not kept
+        self.width = self.eng.max_ctx - prompt + 1
+        if logprobs:
+            self.resp = torch.zeros((B, self.width), dtype=i32, device=dev)
+            self.logp = torch.zeros((B, self.width), dtype=f32, device=dev)
+            self.logp_ws = torch.empty(sdrl.logits_workspace_bytes(B * (gmax + 1), V), dtype=torch.uint8, device=dev)
 
     def _view(self, name, *shape):
         n = int(np.prod(shape))
         return self.flat[name][:n].view(*shape)
+
+    def _record(self, slots, tokens, logits, emitted):
+        """Keeps the tokens [rows, n] (-1: none) that an iteration emitted, `emitted` a row, and their log-probabilities."""
+        torch = self.torch
+        lp = sdrl.token_logprobs(logits, tokens, self.T, workspace=self.logp_ws)[0]
+        s = slots.long()
+        at = (self.kv_len[s] - self.prompt - emitted)[:, None] + torch.arange(tokens.shape[1], device=self.dev)
+        at = torch.where(tokens >= 0, at, self.width - 1).long()
+        self.resp[s[:, None], at] = tokens
+        self.logp[s[:, None], at] = lp
 
     def run(self, policy: str, gamma: int, tau_prev: float, cost, eps: float, lengths, step: int,
             keep_trace: bool = True) -> tuple[RolloutResult, dict]:
@@ -277,6 +347,8 @@ class Rollout:
                 torch.add(ent["out"], 0, out=ent["last"])      # a kernel node, not a copy node
             cap = run_padded(ent, eager, self.graphs)
             state["last"] = ent["last"][:Bl].clone()
+            if self.logprobs:
+                self._record(state["slots"], ent["out"][:Bl, None], ent["logits"][:Bl, None], 1)
             torch.cuda.synchronize()
             return np.ones(Bl, dtype=np.int64), cap
 
@@ -290,6 +362,8 @@ class Rollout:
                 torch.add(bufs.next_tok, 0, out=ent["last"])
             cap = run_padded(ent, eager, self.graphs)
             state["last"] = ent["last"][:Bl].clone()
+            if self.logprobs:
+                self._record(state["slots"], bufs.out_tok[:Bl], bufs.p_logits[:Bl], bufs.n_emit[:Bl])
             return bufs.n_emit[:Bl].cpu().numpy(), cap
 
         def ar_fn():
@@ -297,6 +371,8 @@ class Rollout:
             out, pl = self._view("ar_out", Bl), self._view("ar_logits", Bl, V)
             eng.ar_step(state["slots"], state["last"], T, seed, 2 * step, out, pl)
             state["last"] = out.clone()
+            if self.logprobs:
+                self._record(state["slots"], out[:, None], pl[:, None], 1)
             torch.cuda.synchronize()          # the host learns which sequences ended (one token each here)
             return np.ones(Bl, dtype=np.int64)
 
@@ -310,6 +386,8 @@ class Rollout:
             eng.accept(state["slots"], dt_, ql, qs, pl, g, T, seed, 2 * step + 1, ot, ne, nt)
             eng.rollback(state["slots"], ne)
             state["last"] = nt.clone()
+            if self.logprobs:
+                self._record(state["slots"], ot, pl, ne)
             return ne.cpu().numpy()           # the host needs n_emit every step
 
         def compact_fn(keep):
@@ -320,8 +398,10 @@ class Rollout:
         torch.cuda.synchronize()
         st = decode(lengths, self.prompt, policy, gamma, tau_prev, cost, eps,
                     ar_padded if self.padded else ar_fn, sd_padded if self.padded else sd_fn, compact_fn,
-                    keep_trace=keep_trace)
+                    keep_trace=keep_trace, group=self.group)
         eng.sync()
+        if self.logprobs:
+            st["tokens"], st["logp"] = self.resp[:self.B], self.logp[:self.B]   # [B][lmax and more], up to each length
         res = RolloutResult(policy=policy, step=step, gamma=gamma, tau_prev=tau_prev, tau=st["tau"],
                             makespan_s=st["makespan_s"], prep_ms=prep_ms, ar_iters=st["ar_iters"],
                             sd_iters=st["sd_iters"], tokens=int(np.asarray(lengths).sum()),
@@ -418,6 +498,8 @@ def main(argv=None):
                     help="pad live batches to buckets of BUCKET rows and replay one captured HIP graph per "
                          "(bucket, draft length) and per AR bucket")
     ap.add_argument("--kv4", action="store_true", help="hold the KV cache in 4 bits (paged)")
+    ap.add_argument("--group", type=int, default=1, help="responses of each prompt, which share its KV pages and their reads")
+    ap.add_argument("--logprobs", action="store_true", help="keep every response token's log-probability")
     ap.add_argument("--tau-carry", action="store_true",
                     help="carry the toggle's tau to a new draft length through the acceptance rate "
                          "(default: Algorithm 1 as written, the measured tau as it is)")
@@ -437,9 +519,10 @@ def main(argv=None):
         calib = dict(F_eff=calib["F_eff"], params=calib["params"], agreement=calib["agreement"], kv4=calib["kv4"])
     cost = calibrated_cost(cfg, calib, a.kv4)
     log("building the rollout engine ...")
-    ro = Rollout(cfg, a.B, a.prompt, a.lmax, seed=a.seed, fmt=a.drafter, graphs=a.graphs, prefill=a.prefill, kv4=a.kv4)
+    ro = Rollout(cfg, a.B, a.prompt, a.lmax, seed=a.seed, fmt=a.drafter, graphs=a.graphs, prefill=a.prefill, kv4=a.kv4,
+                 group=a.group, logprobs=a.logprobs)
     if ro.prefill_s is not None:
-        log(f"prefill of {a.B} x {a.prompt} tokens: {ro.prefill_s:.2f} s")
+        log(f"prefill of {a.B // a.group} x {a.prompt} tokens: {ro.prefill_s:.2f} s")
     lengths_fn = lambda t: response_lengths(a.B, a.median, a.sigma, a.lmin, a.lmax, a.seed * 1000 + t)
     # one untimed rollout to load every kernel
     ro.run("sd", GAMMA_SET[0], float(GAMMA_SET[0]), cost, EPS, np.minimum(lengths_fn(0), 64), 99, keep_trace=False)
@@ -458,7 +541,7 @@ def main(argv=None):
     ro.close()
     L0 = lengths_fn(0)
     summary = dict(model=cfg["name"], drafter=a.drafter, B=a.B, prompt=a.prompt, tau_carry=a.tau_carry,
-                   graphs=a.graphs, kv4=a.kv4, prefill_s=ro.prefill_s,
+                   graphs=a.graphs, kv4=a.kv4, group=a.group, prefill_s=ro.prefill_s,
                    lengths=dict(median=a.median, sigma=a.sigma, lo=a.lmin, hi=a.lmax, mean_step0=float(L0.mean()),
                                 max_step0=int(L0.max())),
                    calib=dict(F_eff=calib["F_eff"], params=calib["params"], kv4=a.kv4),

@@ -37,7 +37,7 @@ API_SYMBOLS = (
     "sd_alpha_from_tau", "sd_timing", "sd_timing_read", "sd_dense_gemm_bf16", "sd_accept_noalloc",
     "sd_rope_table", "sd_set_rope", "sd_kv4_page_bytes", "sd_kv4_append", "sd_kv4_read", "sd_kv4_workspace_bytes",
     "sd_kv4_attention", "sd_bind_kv4",
-    "sd_kv_append", "sd_prefix_workspace_bytes", "sd_prefix_attention",
+    "sd_kv_append", "sd_prefix_workspace_bytes", "sd_prefix_attention", "sd_bind_prefix",
     "sd_logits_workspace_bytes", "sd_token_logprobs", "sd_token_logprobs_grad", "sd_policy_loss",
 )
 
@@ -163,6 +163,7 @@ def lib():
             "sd_bind_kv4": (_i32, [_P, _P]),
             "sd_kv_append": (_i32, [_P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _P, _i64, _P, _i64, _i32, _P, _P, _P]),
             "sd_prefix_workspace_bytes": (_sz, [_P, _i32, _i32, _i32]),
+            "sd_bind_prefix": (_i32, [_P, _P]),
             "sd_prefix_attention": (_i32, [_P, _P, _i32, _i32, _i32, _P, _P, _i32, _P, _i64, _f, _P, _i64, _P, _sz, _P]),
             "sd_logits_workspace_bytes": (_sz, [_i32, _i32]),
             "sd_token_logprobs": (_i32, [_i32, _i32, _i32, _P, _i64, _P, _f, _P, _P, _P, _P, _sz, _P]),
@@ -322,6 +323,19 @@ class Engine:
         self._on_current_device()
         _check(lib().sd_bind_kv4(self.h, cache._ref))
         self._keep_kv = cache
+
+    def bind_prefix(self, groups: "PrefixGroups | None"):
+        """Draft, verify and AR step read what slots of a group share once (paged cache only); None ends it, and so
+        does binding another cache."""
+        if groups is None:
+            _check(lib().sd_bind_prefix(self.h, None))
+            self._keep_groups = None
+            return
+        if groups.device != self.device or groups.group.shape[0] != self.max_slots:
+            raise ValueError(f"groups: on {groups.device} for {groups.group.shape[0]} slots, the engine on {self.device} has {self.max_slots}")
+        self._on_current_device()
+        _check(lib().sd_bind_prefix(self.h, groups._ref))
+        self._keep_groups = groups
 
     def set_rope(self, rope: "RopeConfig"):
         """Replaces the engine's rotary table (on the current stream) for every later call."""
