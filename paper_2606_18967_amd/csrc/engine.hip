@@ -797,8 +797,9 @@ extern "C" sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_g
     const px_groups g = groups ? px_groups{groups->group, groups->len, groups->n_groups} : px_groups{};
     const hipStream_t s = (hipStream_t)stream;
     prefix_plan_bind(p, workspace, B, c->n_kv);
-    launch_prefix_plan(r, g, p, n_q, c->n_kv, s);
-    launch_prefix_attention(r, p, kv, layer, n_q, (const uint16_t*)q, q_ld, scale, out, ACT_BF16, out_ld, s);
+    if (prefix_plans_itself(p, B)) p.item = nullptr;
+    else launch_prefix_plan(r, g, p, n_q, c->n_kv, s);
+    launch_prefix_attention(r, p, g, kv, layer, n_q, (const uint16_t*)q, q_ld, scale, out, ACT_BF16, out_ld, s);
     launch_prefix_combine(r, p, n_q, c->n_kv, c->head_dim, out, ACT_BF16, out_ld, s);
     return launched("sd_prefix_attention");
 }
@@ -969,7 +970,7 @@ static void attend_groups(sd_engine e, const workspace& ws, const rows_t& r, con
       if (S > 1) launch_kv_append(r, kv, l, c.n_q, parts(qd), parts(qd + kd), parts(0), q, ro, s);
       else launch_kv_append(r, kv, l, c.n_q, whole(qd), whole(qd + kd), whole(0), q, ro, s); }
     { kscope t(e, r.n == 1 ? T_ATTN_D : T_ATTN_V);
-      launch_prefix_attention(r, plan, kv, l, c.n_q, q, qd, 1.f / sqrtf((float)D), ws.att, at, qd, s, t.start, t.stop); }
+      launch_prefix_attention(r, plan, e->groups, kv, l, c.n_q, q, qd, 1.f / sqrtf((float)D), ws.att, at, qd, s, t.start, t.stop); }
     tscope t(e, T_MISC, s);
     launch_prefix_combine(r, plan, c.n_q, c.n_kv, D, ws.att, at, qd, s);
 }

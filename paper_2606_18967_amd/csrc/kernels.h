@@ -279,36 +279,42 @@ size_t accept_part_floats(int B, int gamma, int V);
 // ---- groups that share a prompt, paged bf16 cache (kernels_prefix.hip).  In these
 // rows_t::err may be NULL, rows_t::row0 and live are not used.
 constexpr int PX_SEQS = 1024;            // sequences of a call
+constexpr int PX_WAVE = 64;              // up to so many the attention may plan itself
 constexpr int PX_TILE = 64;              // positions of a tile; what a group shares is whole tiles
 constexpr int PX_ROWS = 128;             // query rows of an item
-constexpr int PX_SHARED = 1 << 30;       // px_item::base of shared positions
 struct px_groups {
     const int32_t* group;                // device [max_slots], or NULL: no sharing
     const int32_t* len;                  // device [n_groups]
     int n_groups;
 };
-// Rows [128 z, 128 z + 128) of the QR query rows a KV head that start at row row0 of
-// the call, over the positions [p0, p1) of `slot`; base: the first row's position (its
-// causal limit), or PX_SHARED.  part: the first row's partial row, -1 where the item
-// writes the output itself.  QR 0: no item.
-struct px_item { int row0, QR, slot, p0, p1, base, part, z; };
-// a sequence's partial rows: pfx_n chunks of its run at a stride of pfx_rows, then own_n of its own
-struct px_seq { int pfx_part, pfx_n, pfx_rows, own_part, own_n, pad; };
+// Rows [r0, r0 + rows) of the query rows a KV head of the nseq sequences from f on, over the tiles [t0, t1) of their
+// stream: P shared tiles, read through slot `reader`, then each sequence's own.  part: the first row's partial row, -1
+// where the item writes the output itself.  rows 0: no item.
+struct px_item { int f, nseq, r0, rows, reader, P, t0, t1, part; };
+// a sequence: slot, its first row's position, the end of what its rows see (0: nothing), its rows
+struct px_info { int slot, base, ctx, nlive; };
+// and its partial rows: of nc chunks, at a stride
+struct px_seq { int part, nc, stride, pad; };
 struct px_plan {
-    px_seq* seq;                         // device [B]
+    px_seq* seq;                         // device [B], info [B]
+    px_info* info;
     px_item* item;                       // device [max_items]
     float2* ml;                          // device [n_kv][part_rows]: (m, l) in base 2, and o [..][D]
     float* o;
-    int target, min_chunk;               // items wanted, shortest chunk
+    int target;                          // items wanted
+    int sps, zs;                         // sequences of a slice, slices of a sequence (one of them is 1)
     long long max_items, part_rows;
     int layer;                           // (the launcher's)
 };
 px_plan prefix_plan(int B, int n, int n_q, int n_kv);
+bool prefix_plans_itself(const px_plan& p, int B);
 size_t prefix_plan_bytes(const px_plan& p, int B, int n_kv, int D);
 void prefix_plan_bind(px_plan& p, void* buf, int B, int n_kv);
 void launch_prefix_plan(const rows_t& r, const px_groups& g, const px_plan& p, int n_q, int n_kv, hipStream_t s);
-void launch_prefix_attention(const rows_t& r, px_plan p, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld, float scale,
-                             void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0 = nullptr, hipEvent_t ev1 = nullptr);
+// p.item NULL: the plan is made by the attention itself, of up to PX_WAVE sequences (p.seq is then written for the combine)
+void launch_prefix_attention(const rows_t& r, px_plan p, const px_groups& g, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld,
+                             float scale, void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0 = nullptr,
+                             hipEvent_t ev1 = nullptr);
 void launch_prefix_combine(const rows_t& r, const px_plan& p, int n_q, int n_kv, int D, void* out, act_t out_t, long long out_ld, hipStream_t s);
 // T as launch_kv4_append's; q_out NULL: K and V alone
 template <typename T>

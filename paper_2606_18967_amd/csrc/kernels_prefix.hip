@@ -84,6 +84,17 @@ __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t
 }
 
 // ------------------------------------------------------------------ plan
+// How a call is cut into work-groups.  Sequences of one group that follow one another
+// are a run; what a run shares, min(len, the shortest kv_len in it), is rounded
+// down to whole tiles of PX_TILE positions.  Sequences of a run whose rows fit PX_ROWS
+// make a slice (a longer sequence makes several, of PX_ROWS rows each), and a slice
+// walks one stream of tiles: the shared positions, for all of its rows, then each of
+// its sequences' own.  All streams are cut into chunks of about W / target tiles (W:
+// the tiles of all), so that the work-groups are alike and resident at once, however
+// the batch divides between shared and own positions: with items of their own for the
+// sequences' tails, 8 groups of 8 behind prompts of 2048 (responses of up to 512) took
+// 42 us instead of 35, for a tail's item was 4 us of tiles and 8 of start and end.
+
 // inclusive sum over the 1024 threads of a work-group; sh: 16 ints
 __device__ __forceinline__ int scan1024(int v, int* sh)
 {
@@ -100,142 +111,262 @@ __device__ __forceinline__ int scan1024(int v, int* sh)
     return v;
 }
 
+// inclusive sum over the lanes, by lane permutations in registers (within 16 lanes, then across)
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);    // from lane - 1, - 2, - 4, - 8 of a row of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);    // lane 15 of the row before to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);    // lane 31 to rows 2 and 3
+    return v;
+}
+// the sum over the lanes of counts (whole floats)
+__device__ __forceinline__ float wave_total(float v)
+{
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-// The items of a call (px_item): runs of sequences of one group that follow one
-// another share min(len, the shortest kv_len among them) positions, rounded down to
-// whole tiles; both these and the sequences' own positions are cut into chunks of
-// about W / target positions, W being what all items read in all (a slice of PX_ROWS
-// rows reads its chunk by itself).  Thread t is sequence t and run t.
-__global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px_plan pl, int G)
+// What a sequence brings: where its rows are and what it may see (ctx 0: nothing), and the group it is in.
+struct member { px_info info; int gid, len; };
+__device__ __forceinline__ member member_of(const rows_t& r, const px_groups& gr, int b, bool report)
 {
-    __shared__ int s_gid[PX_SEQS];
-    __shared__ int s_first[PX_SEQS + 1], s_P[PX_SEQS], s_reader[PX_SEQS], s_live[PX_SEQS], s_rchunk[PX_SEQS], s_rend[PX_SEQS], s_rpart[PX_SEQS];
-    __shared__ int s_run[PX_SEQS], s_ctx[PX_SEQS], s_ochunk[PX_SEQS], s_oend[PX_SEQS], s_opart[PX_SEQS];
-    __shared__ unsigned long long s_work;
-    __shared__ int sh[16], s_total[3];
-    const int t = threadIdx.x, RG = r.n * G, zs = cdiv(RG, PX_ROWS);
-    const bool mine = t < r.B;
-    int slot = -1, nlive = 0, base = 0, gid = -1;
-    bool ok = false;
-    if (mine) {
-        slot = r.slots[t];
-        const int nl = r.lim ? r.lim[t] : r.n;
-        nlive = min(max(nl, 0), r.n);
-        if (nl != nlive) raise(r.err, ERR_LEN);
-        if (slot >= 0 && slot < r.max_slots) {
-            base = kv4_base((long long)r.kv_len[slot] + r.off);
-            ok = base >= 0 && base < r.max_ctx;
-            if (nlive > 0 && (base < 0 || base > r.max_ctx - nlive)) raise(r.err, ERR_CTX);
-            if (ok && gr.group) {
-                gid = gr.group[slot];
-                if (gid < 0 || gid >= gr.n_groups) gid = -1;
-            }
-        } else if (nlive > 0) {
-            raise(r.err, ERR_SLOT);
+    member m = {{-1, 0, 0, 0}, -1, 0};
+    const int slot = r.slots[b], nl = r.lim ? r.lim[b] : r.n, nlive = min(max(nl, 0), r.n);
+    m.info.nlive = nlive;
+    if (report && nl != nlive) raise(r.err, ERR_LEN);
+    if (slot < 0 || slot >= r.max_slots) {
+        if (report && nlive > 0) raise(r.err, ERR_SLOT);
+        return m;
+    }
+    const int kv = r.kv_len[slot];
+    if (gr.group) m.gid = gr.group[slot];
+    if (m.gid < 0 || m.gid >= gr.n_groups) m.gid = -1;
+    if (m.gid >= 0) m.len = gr.len[m.gid];
+    const int base = kv4_base((long long)kv + r.off);
+    if (report && nlive > 0 && (base < 0 || base > r.max_ctx - nlive)) raise(r.err, ERR_CTX);
+    m.info.slot = slot;
+    m.info.base = base;
+    if (base < 0 || base >= r.max_ctx) m.gid = -1;
+    else if (nlive > 0) m.info.ctx = min(base + nlive, r.max_ctx);
+    return m;
+}
+// tiles of a sequence's own behind P shared tiles
+__device__ __forceinline__ int own_tiles(const px_info& i, int P) { return i.ctx ? cdiv(i.ctx - P * PX_TILE, PX_TILE) : 0; }
+
+// A slice's chunks: of `tiles` tiles in shares of `share` (rows without a tile: one chunk, which writes zeros).  Slices
+// of a run are cut at the same tiles, so that the shared ones, which they read at about the same time, come once
+// from memory.
+struct chunks { int n, len; };
+constexpr int PX_SHARE = 1 << 24;                                  // the longest share: the tiles of 64 sequences of 2^24 positions
+__device__ __forceinline__ chunks chunks_of(int tiles, int share, bool any)
+{
+    if (!any) return {0, 0};
+    if (tiles <= 0) return {1, 0};
+    return {cdiv(tiles, share), min(tiles, share)};
+}
+
+// The plan of up to 64 sequences by one wave, a lane each, without a barrier: every wave of the attention makes it
+// for itself where a plan kernel before it would cost more (its launch, and the way of the plan through memory).
+struct wave_plan {
+    px_info info;
+    int P, reader, sfirst, send, nc, len, tiles, part;  // of the lane's slice: its run's shared tiles and the slot they are read through, ..
+    int iend, total;                                    // items up to the lane's, and in all
+};
+__device__ wave_plan plan_of_wave(const rows_t& r, const px_groups& gr, const px_plan& pl, int RG, bool report)
+{
+    const int lane = threadIdx.x & 63;
+    const bool mine = lane < r.B;
+    member m = {{-1, 0, 0, 0}, -1, 0};
+    if (mine) m = member_of(r, gr, lane, report);
+    wave_plan p = {};
+    p.info = m.info;
+    const bool live = m.info.ctx > 0;
+    // runs
+    const int before = __shfl_up(m.gid, 1, WAVE);
+    const bool lead = lane == 0 || !mine || m.gid < 0 || m.gid != before;
+    const uint64_t heads = __builtin_amdgcn_ballot_w64(lead), upto = ~0ull >> (63 - lane), later = heads & ~upto;
+    const int first = 63 - __builtin_clzll(heads & upto), end = min(later ? __builtin_ctzll(later) : 64, r.B);
+    const uint64_t run = (~0ull >> (64 - max(end, 1))) & (~0ull << first), alive = __builtin_amdgcn_ballot_w64(live) & run;
+    int low = live ? m.info.base : INT_MAX;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int t = __shfl_down(low, o, WAVE);
+        if (lane + o < end) low = min(low, t);
+    }
+    low = __shfl(low, first, WAVE);
+    if (m.gid >= 0 && (alive & (alive - 1))) p.P = max(min(m.len, low), 0) / PX_TILE;
+    p.reader = __shfl(m.info.slot, alive ? __builtin_ctzll(alive) : 0, WAVE);
+    // slices
+    p.sfirst = first + (lane - first) / pl.sps * pl.sps;
+    p.send = min(p.sfirst + pl.sps, end);
+    const int own = own_tiles(m.info, p.P), upto_own = wave_scan(own);
+    const int own_end = __shfl(upto_own, p.send - 1, WAVE), own_start = __shfl(upto_own, max(p.sfirst - 1, 0), WAVE);
+    const uint64_t slice = (~0ull >> (64 - max(p.send, 1))) & (~0ull << p.sfirst);
+    const bool any = (__builtin_amdgcn_ballot_w64(m.info.nlive > 0) & slice) != 0, sees = (__builtin_amdgcn_ballot_w64(live) & slice) != 0;
+    p.tiles = sees ? p.P + own_end - (p.sfirst ? own_start : 0) : 0;
+    // the shortest share of a few that makes at most `target` items, which are then resident at once
+    const bool leads = mine && lane == p.sfirst;
+    const float w = wave_total(leads ? (float)p.tiles * pl.zs : 0.f);
+    const int even = (int)fminf(fmaxf(ceilf(w / (float)pl.target), 1.f), (float)PX_SHARE);
+    int share = even;
+    for (int k = 0; k < 8; ++k) {
+        const int s = cdiv(even * (k < 5 ? 8 + k : 4 * k - 4), 8);     // 1, 9/8, .. 3/2, 2, 5/2, 3
+        const float rs = 1.f / (float)s;
+        if (wave_total(leads && any ? fmaxf(ceilf((float)p.tiles * rs), 1.f) * pl.zs : 0.f) <= (float)pl.target) {
+            share = s;
+            break;
         }
     }
-    s_gid[t] = gid;
-    s_P[t] = s_reader[t] = INT_MAX;
-    s_live[t] = 0;
+    const chunks c = chunks_of(p.tiles, share, any);
+    p.nc = c.n;
+    p.len = c.len;
+    p.iend = wave_scan(leads ? c.n * pl.zs : 0);
+    p.total = last_lane(p.iend);
+    const int parts = leads && c.n > 1 ? c.n * (p.send - p.sfirst) * RG : 0, upto_parts = wave_scan(parts);
+    p.part = __shfl(upto_parts - parts, p.sfirst, WAVE);
+    return p;
+}
+__device__ __forceinline__ px_seq seq_of(const wave_plan& p, int RG)
+{
+    return px_seq{p.part + ((int)(threadIdx.x & 63) - p.sfirst) * RG, p.nc, (p.send - p.sfirst) * RG, 0};
+}
+// rows [128 zz, ..) of a slice's chunk c (zs 1: all of its rows)
+__device__ __forceinline__ px_item make_item(const px_plan& pl, int RG, int f, int nseq, int reader, int P, int tiles, chunks ch, int part, int j)
+{
+    const int c = pl.zs == 1 ? j : j / pl.zs, zz = pl.zs == 1 ? 0 : j - c * pl.zs, rows = pl.zs == 1 ? nseq * RG : min(PX_ROWS, RG - PX_ROWS * zz);
+    const int t0 = c * ch.len;
+    return px_item{f, nseq, PX_ROWS * zz, rows, reader, P, t0, min(t0 + ch.len, tiles), ch.n > 1 ? part + zz * ch.n * PX_ROWS + c * rows : -1};
+}
+// item k (the same in every lane)
+__device__ px_item item_of(const wave_plan& p, const px_plan& pl, int RG, int k)
+{
+    if (k >= p.total) return px_item{};
+    const int L = __builtin_ctzll(__builtin_amdgcn_ballot_w64(p.iend > k));
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, L); };
+    return make_item(pl, RG, L, of(p.send) - L, of(p.reader), of(p.P), of(p.tiles), chunks{of(p.nc), of(p.len)}, of(p.part),
+                     k - (L ? __builtin_amdgcn_readlane(p.iend, L - 1) : 0));
+}
+// (the first wave makes the plan, every thread an item)
+__global__ void __launch_bounds__(256) k_prefix_plan_wave(rows_t r, px_groups gr, px_plan pl, int RG)
+{
+    __shared__ int s_send[64], s_reader[64], s_P[64], s_tiles[64], s_nc[64], s_len[64], s_part[64], s_iend[64];
+    const int t = threadIdx.x;
+    if (t < 64) {
+        const wave_plan p = plan_of_wave(r, gr, pl, RG, true);
+        if (t < r.B) {
+            pl.seq[t] = seq_of(p, RG);
+            pl.info[t] = p.info;
+        }
+        s_send[t] = p.send;
+        s_reader[t] = p.reader;
+        s_P[t] = p.P;
+        s_tiles[t] = p.tiles;
+        s_nc[t] = p.nc;
+        s_len[t] = p.len;
+        s_part[t] = p.part;
+        s_iend[t] = p.iend;
+    }
+    __syncthreads();
+    for (int k = t; k < pl.max_items; k += 256) {
+        px_item it = {};
+        if (k < s_iend[63]) {
+            int L = 0;                                             // the first whose items end past it
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1)
+                if (s_iend[L + o - 1] <= k) L += o;
+            it = make_item(pl, RG, L, s_send[L] - L, s_reader[L], s_P[L], s_tiles[L], chunks{s_nc[L], s_len[L]}, s_part[L], k - (L ? s_iend[L - 1] : 0));
+        }
+        pl.item[k] = it;
+    }
+}
+
+// The same for up to PX_SEQS sequences, a thread each.
+__global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px_plan pl, int RG)
+{
+    __shared__ int s_gid[PX_SEQS], s_first[PX_SEQS + 1], s_low[PX_SEQS], s_reader[PX_SEQS], s_alive[PX_SEQS];   // of runs, but the first
+    __shared__ int s_own[PX_SEQS], s_any[PX_SEQS], s_send[PX_SEQS], s_iend[PX_SEQS], s_part[PX_SEQS], s_tiles[PX_SEQS], s_nc[PX_SEQS], s_len[PX_SEQS];
+    __shared__ unsigned long long s_work;
+    __shared__ int sh[16];
+    const int t = threadIdx.x;
+    const bool mine = t < r.B;
+    member m = {{-1, 0, 0, 0}, -1, 0};
+    if (mine) {
+        m = member_of(r, gr, t, true);
+        pl.info[t] = m.info;
+    }
+    const bool live = m.info.ctx > 0;
+    s_gid[t] = m.gid;
+    s_low[t] = s_reader[t] = INT_MAX;
+    s_alive[t] = 0;
     if (t == 0) s_work = 0;
     __syncthreads();
-    // runs
-    const bool lead = mine && (t == 0 || gid < 0 || gid != s_gid[t - 1]);
-    const int run = scan1024(lead ? 1 : 0, sh) - 1;
-    s_run[t] = run;
+    const bool lead = mine && (t == 0 || m.gid < 0 || m.gid != s_gid[t - 1]);
+    const int run = max(scan1024(lead ? 1 : 0, sh) - 1, 0);
     if (lead) s_first[run] = t;
-    if (t == r.B - 1) {
-        s_first[run + 1] = r.B;
-        s_total[0] = run + 1;
-    }
-    const bool live = ok && nlive > 0;
-    __syncthreads();
-    const int nruns = s_total[0];
+    if (t == r.B - 1) s_first[run + 1] = r.B;
     if (live) {
-        atomicMin(&s_P[run], base);
+        atomicMin(&s_low[run], m.info.base);
         atomicMin(&s_reader[run], t);
-        atomicAdd(&s_live[run], 1);
+        atomicAdd(&s_alive[run], 1);
     }
     __syncthreads();
-    int P = 0, rows = 0, slices = 0;
-    if (t < nruns) {
-        const int f = s_first[t], g = s_gid[f];
-        rows = (s_first[t + 1] - f) * RG;
-        if (g >= 0 && s_live[t] > 1) P = max(min(gr.len[g], s_P[t]), 0) / PX_TILE * PX_TILE;
-        if (P > 0) slices = cdiv(rows, PX_ROWS);
+    const int first = s_first[run], end = s_first[run + 1];
+    const int P = m.gid >= 0 && s_alive[run] > 1 ? max(min(m.len, s_low[run]), 0) / PX_TILE : 0;
+    const int sfirst = first + (t - first) / pl.sps * pl.sps, send = min(sfirst + pl.sps, end);
+    s_own[t] = scan1024(own_tiles(m.info, P), sh);
+    s_any[t] = scan1024((m.info.nlive > 0 ? 1 << 16 : 0) + (live ? 1 : 0), sh);
+    s_send[t] = send;
+    __syncthreads();
+    const bool leads = mine && t == sfirst;
+    int tiles = 0;
+    bool any = false;
+    if (leads) {
+        const int counts = s_any[send - 1] - (t ? s_any[t - 1] : 0);
+        any = counts >> 16;
+        tiles = counts & 0xffff ? P + s_own[send - 1] - (t ? s_own[t - 1] : 0) : 0;
+        atomicAdd(&s_work, (unsigned long long)tiles * pl.zs);
     }
     __syncthreads();
-    s_P[t] = P;
+    const int share = (int)min(max((s_work + pl.target - 1) / pl.target, 1ull), (unsigned long long)PX_SHARE);
+    const chunks c = leads ? chunks_of(tiles, share, any) : chunks{0, 0};
+    s_iend[t] = scan1024(c.n * pl.zs, sh);
+    const int parts = c.n > 1 ? c.n * (send - sfirst) * RG : 0;
+    s_part[t] = scan1024(parts, sh) - parts;
+    s_tiles[t] = tiles;
+    s_nc[t] = c.n;
+    s_len[t] = c.len;
     __syncthreads();
-    // chunks
-    const int ctx = live ? min(base + nlive, r.max_ctx) : 0, pre = live ? s_P[run] : 0, own = ctx - pre;
-    const unsigned long long w = (unsigned long long)P * slices + (unsigned long long)own * zs;
-    if (w) atomicAdd(&s_work, w);
+    if (mine) pl.seq[t] = px_seq{s_part[sfirst] + (t - sfirst) * RG, s_nc[sfirst], (send - sfirst) * RG, 0};
+    s_low[t] = P;                                                  // (of the runs before, from here on of the sequences)
+    if (mine) s_gid[t] = s_reader[run] < r.B ? r.slots[s_reader[run]] : -1;
     __syncthreads();
-    // (no context is longer than 2^24: past 2^25 nothing is cut either way)
-    const int share = (int)min(max((s_work + pl.target - 1) / pl.target, (unsigned long long)pl.min_chunk), 1ull << 25);
-    auto cut = [&](int x, int& chunk) {                            // chunks of x positions, as even as whole tiles allow
-        if (x <= 0) return chunk = 0;
-        chunk = cdiv(cdiv(x, cdiv(x, share)), PX_TILE) * PX_TILE;
-        return cdiv(x, chunk);
-    };
-    int pchunk, ochunk;
-    const int np = cut(P, pchunk), no = nlive > 0 ? max(cut(own, ochunk), 1) : 0;
-    if (own <= 0) ochunk = 0;
-    // a sequence that is one item writes the output itself; partial rows: the runs' first, then the sequences'
-    s_live[t] = np;
-    __syncthreads();
-    const bool direct = no == 1 && s_live[max(run, 0)] == 0;
-    const int rend = scan1024(np * slices, sh), rpart = scan1024(np * rows, sh);
-    const int oend = scan1024(no * zs, sh), opart = scan1024(direct ? 0 : no * RG, sh);
-    if (t == 1023) {
-        s_total[0] = rend;
-        s_total[1] = oend;
-        s_total[2] = rpart;
-    }
-    s_rchunk[t] = pchunk;
-    s_rend[t] = rend;
-    s_rpart[t] = rpart - np * rows;
-    s_ctx[t] = ctx;
-    s_ochunk[t] = ochunk;
-    s_oend[t] = oend;
-    __syncthreads();
-    s_opart[t] = direct ? -1 : s_total[2] + opart - no * RG;
-    __syncthreads();
-    if (mine) {
-        const int f = s_first[run];
-        pl.seq[t] = px_seq{s_rpart[run] + (t - f) * RG, s_live[run], (s_first[run + 1] - f) * RG, s_opart[t], direct ? 0 : no, 0};
-    }
-    const int n_shared = s_total[0], total = n_shared + s_total[1];
     for (int k = t; k < pl.max_items; k += 1024) {
-        px_item it = {0, 0, -1, 0, 0, 0, 0, 0};                    // QR 0: no item
-        if (k < total) {
-            const bool shared = k < n_shared;
-            const int want = shared ? k : k - n_shared;
-            const int* ends = shared ? s_rend : s_oend;
-            int lo = 0, hi = (shared ? nruns : r.B) - 1;           // the first whose items end past it
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (ends[mid] > want) hi = mid;
-                else lo = mid + 1;
-            }
-            const int j = want - (lo ? ends[lo - 1] : 0);
-            if (shared) {
-                const int f = s_first[lo], qr = (s_first[lo + 1] - f) * RG, sl = cdiv(qr, PX_ROWS), c = j / sl, p0 = c * s_rchunk[lo];
-                it = px_item{f * r.n, qr, r.slots[s_reader[lo]], p0, min(p0 + s_rchunk[lo], s_P[lo]), PX_SHARED, s_rpart[lo] + c * qr, j - c * sl};
-            } else {
-                const int c = j / zs, p0 = min((s_ctx[lo] ? s_P[s_run[lo]] : 0) + c * s_ochunk[lo], s_ctx[lo]);
-                it = px_item{lo * r.n, RG, r.slots[lo], p0, min(p0 + s_ochunk[lo], s_ctx[lo]), 0, 0, j - c * zs};
-                it.base = it.slot >= 0 && it.slot < r.max_slots ? kv4_base((long long)r.kv_len[it.slot] + r.off) : 0;
-                it.part = s_opart[lo] < 0 ? -1 : s_opart[lo] + c * RG;
-            }
+        px_item it = {};
+        if (k < s_iend[1023]) {
+            int L = 0;
+#pragma unroll
+            for (int o = 512; o > 0; o >>= 1)
+                if (s_iend[L + o - 1] <= k) L += o;
+            it = make_item(pl, RG, L, s_send[L] - L, s_gid[L], s_low[L], s_tiles[L], chunks{s_nc[L], s_len[L]}, s_part[L], k - (L ? s_iend[L - 1] : 0));
         }
         pl.item[k] = it;
     }
 }
 
 // ------------------------------------------------------------------ attention
+typedef __attribute__((address_space(3))) uint8_t* lds_t;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
 // 64 lanes x 16 bytes at base + off straight into LDS, in lane order from byte `lds` on.
 // The compiler's wait counts do not see them.
 __device__ __forceinline__ void row_dma16(const void* base, uint32_t off, uint32_t lds)
@@ -268,151 +399,222 @@ __device__ __forceinline__ uint32_t finite2(uint32_t x)
     const uint32_t lo = (x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu, hi = (x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u;
     return lo | hi;
 }
-__device__ __forceinline__ bool odd2(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
-// A work-group takes an item's rows of one KV head: up to PX_ROWS query rows (a
-// sequence's heads of the group side by side, position after position, sequence
-// after sequence) over the positions [p0, p1).  Tiles of 64 positions go into LDS by
-// DMA, the next one while one is used; each of the four waves has 32 rows, or
-// with up to 64 rows two waves share 32 and take 32 positions of a tile each.
+template <int D>
+__device__ __forceinline__ constexpr int v_swizzle(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
+
+// A work-group takes a slice's rows of one KV head, up to PX_ROWS (a sequence's heads of
+// the group side by side, position after position, sequence after sequence), over the
+// tiles [t0, t1) of its stream.  Tiles of 64 positions go into LDS by DMA, the next
+// one while one is used; each of the four waves has 32 rows, or with up to 64 rows
+// two waves share 32 and take 32 positions of a tile each.
 //   S^T = K Q^T by v_mfma_f32_32x32x16_bf16: a lane has row l%32 and the
 //   positions 8 (i/4) + 4 (l/32) + i%4, i < 16, of 32, which in pairs of four are
 //   the operand P^T of O^T += V^T P^T; V^T is read from its rows transposed
 //   (ds_read_b64_tr_b16) at the same positions, so P never leaves its lane.
-// A row's pieces of 16 bytes lie in LDS at piece ^ position % pieces, which lets the
-// 32 lanes that read a column of pieces meet different banks.
+// A K row's pieces of 16 bytes lie in LDS at piece ^ position % pieces, which lets the
+// lanes that read a column of pieces meet different banks; a V row's at piece ^
+// v_swizzle, for 32 lanes that read four pieces of four rows.  (With V as K its
+// reads met 59% of their cycles in the same banks.)
 // The softmax is online in base 2; a row's reference moves when a score passes it by
 // more than 8.  Scores, sums and references are fp32; P is rounded to bf16 (2^-8
 // of each).  Positions that a row does not see may hold anything: there the scores
 // are replaced and values that are not finite taken as zeros; a row that sees such a
 // value is NaN.
-template <int D>
-__global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, const uint16_t* kc, const uint16_t* vc, int n_q, int n_kv,
-                                                        const uint16_t* q, long long q_ld, float cs, px_plan pl, void* out, int out_t,
-                                                        long long out_ld)
+// NBLK: the blocks of a tile that a wave takes, 2 with a row tile a wave
+template <int D, int NBLK>
+__device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32_t* s_odd, const px_item& it, const px_info& inf, const rows_t& r,
+                                            const kv_geom& g, const uint16_t* kc, const uint16_t* vc, int n_q, int n_kv, const uint16_t* q,
+                                            long long q_ld, float cs, const px_plan& pl, void* out, int out_t, long long out_ld)
 {
     constexpr int KS = D / 16, NB = D / 32, CPP = D / 8;           // k-steps of S, 32-dim blocks of O^T, 16-byte pieces of a row
-    constexpr int TILE = PX_TILE * D * 2;                          // bytes of a tile's K, and of its V
-    constexpr int NI = TILE / 4096;                                // a wave's DMA instructions for either
+    constexpr int TILE = PX_TILE * D * 2, BLOCK = TILE / 2;        // bytes of a tile's K, and of its V, and of half of it
+    constexpr int NI = TILE / 4096, PPI = 512 / D;                 // a wave's DMA instructions for either, and the positions of one
     constexpr int LDO = D + 4;                                     // LDS row stride of the merge
-    __shared__ __attribute__((aligned(1024))) uint8_t s_buf[4 * TILE > 64 * LDO * 4 ? 4 * TILE : 64 * LDO * 4];
-    __shared__ float2 s_ml[64];
-
-    const int kvh = blockIdx.x;
-    const px_item it = pl.item[blockIdx.y];
-    const int QR = __builtin_amdgcn_readfirstlane(it.QR), z = __builtin_amdgcn_readfirstlane(it.z);
-    const int q0 = z * PX_ROWS, nrows = min(QR - q0, PX_ROWS);
-    if (nrows <= 0) return;
-    const int row0 = __builtin_amdgcn_readfirstlane(it.row0), slot = __builtin_amdgcn_readfirstlane(it.slot);
-    const int p0 = __builtin_amdgcn_readfirstlane(it.p0), base = __builtin_amdgcn_readfirstlane(it.base);
-    const int part = __builtin_amdgcn_readfirstlane(it.part);
-    const int G = n_q / n_kv, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lr = lane & 31, h = lane >> 5;
-    const bool wide = nrows > 64;                                  // a row tile a wave
+    constexpr bool wide = NBLK == 2;
+    auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int kvh = blockIdx.x, f = uni(it.f), nseq = uni(it.nseq), r0 = uni(it.r0), nrows = uni(it.rows), P = uni(it.P);
+    const int t0 = uni(it.t0), nt = uni(it.t1) - t0, part = uni(it.part);
+    const int G = n_q / n_kv, RG = r.n * G, lane = threadIdx.x & 63, w = uni(threadIdx.x >> 6), lr = lane & 31, h = lane >> 5;
     const int rt = wide ? w : w & 1;                               // the wave's row tile
-    // what the slice's rows see ends with its last one; all of them see what the first one does
-    const int seen_all = base == PX_SHARED ? INT_MAX : base + q0 / G + 1;
-    const int p1 = base == PX_SHARED ? it.p1 : min(__builtin_amdgcn_readfirstlane(it.p1), base + (q0 + nrows - 1) / G + 1);
-    const int pe = __builtin_amdgcn_readfirstlane(p1);
 
-    // the lane's row: where it is, and the last position it sees (-1: it is not there)
-    const int tq = q0 + 32 * rt + lr, ridx = tq / G, head = kvh * G + tq - ridx * G;
-    const int ib = ridx % r.n, b = row0 / r.n + ridx / r.n;
-    int lim = -1;
-    bool exists = false;
-    if (tq < QR) {
-        exists = ib < (r.lim ? min(max(r.lim[b], 0), r.n) : r.n);
-        const int sl = r.slots[b];
-        if (exists && sl >= 0 && sl < r.max_slots) {
-            const int pos = kv4_base((long long)r.kv_len[sl] + r.off) + ib;
-            if (pos - ib >= 0 && pos < r.max_ctx) lim = pos;
+    // The stream: tiles [0, P) are shared, then come `own` of each sequence.  Lane l of a window holds block l % 2 of its tile
+    // l / 2: its page (-1: none, or past the end), its tile's first position, the end, and the sequence (-1: shared).
+    const int own = own_tiles(inf, P), upto = wave_scan(own);
+    int wpage = -1, wpos = 0, wend = 0, wseq = -1, kw = 0;
+    auto window = [&] {
+        const int t = t0 + kw + (lane >> 1), u = t - P;
+        int s = 0;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1)
+            if (__shfl(upto, s + o - 1, WAVE) <= u) s += o;
+        s = min(s, 63);
+        const int start = __shfl(upto - own, s, WAVE), slot = __shfl(inf.slot, s, WAVE), ctx = __shfl(inf.ctx, s, WAVE);
+        const bool shared = t < P;
+        wpos = shared ? t * PX_TILE : (P + u - start) * PX_TILE;
+        wend = shared ? P * PX_TILE : ctx;
+        wseq = shared ? -1 : s;
+        const int pos = wpos + 32 * (lane & 1);
+        wpage = -1;
+        if (t < t0 + nt && pos < wend) {
+            wpage = page_of(g, shared ? it.reader : slot, pos / g.P);
+            if (wpage < 0) raise(r.err, ERR_PAGE);
         }
-    }
+    };
+    window();
+
+    // the lane's row: its sequence in the slice, where it is, and the last position it sees (-1: it is not there)
+    const int tq = 32 * rt + lr, sr = pl.zs == 1 ? tq / RG : 0, tt = pl.zs == 1 ? tq - sr * RG : r0 + tq, ri = tt / G, head = kvh * G + tt - ri * G;
+    const int row = (f + sr) * r.n + ri, rbase = __shfl(inf.base, min(sr, 63), WAVE), rctx = __shfl(inf.ctx, min(sr, 63), WAVE);
+    const int rlive = __shfl(inf.nlive, min(sr, 63), WAVE);
+    const bool exists = tq < nrows && ri < rlive;
+    const int lim = exists && rctx > 0 && rbase + ri < r.max_ctx ? rbase + ri : -1;
+
+    struct tile_t { int pos, end, seq; uint32_t have; };           // have: bit k: block k has a page and positions
+    const int lp = lane / CPP, lc = lane % CPP;
+    const lds_t lds = (lds_t)s_buf;
+    const uint32_t ring = (uint32_t)(uintptr_t)lds;
+    const long long hb = (long long)pl.layer * g.LS + (long long)kvh * g.HS;
+    // tile i on its way into its place in LDS: a wave takes 16 positions, past the end the last one again
+    auto issue = [&](int i) {
+        if (i >= kw + 32) {
+            kw = i;
+            window();
+        }
+        const int j = 2 * (i - kw), pa = __builtin_amdgcn_readlane(wpage, j), pb = __builtin_amdgcn_readlane(wpage, j + 1);
+        const tile_t t = {__builtin_amdgcn_readlane(wpos, j), __builtin_amdgcn_readlane(wend, j), __builtin_amdgcn_readlane(wseq, j),
+                          (pa >= 0 ? 1u : 0u) | (pb >= 0 ? 2u : 0u)};
+        const int pg = w < 2 ? pa : pb;
+        if (pg < 0) return t;
+        const int bs = t.pos + 32 * (w >> 1), last = min(bs + 31, t.end - 1) - bs;
+        const long long at = (long long)pg * g.PS + hb + (long long)(bs % g.P) * D;
+        const uint32_t dst = ring + (i & 1) * (2 * TILE) + w * (NI * 1024);
+#pragma unroll
+        for (int k = 0; k < NI; ++k) {
+            const int rr = 16 * (w & 1) + PPI * k + lp;            // in its block
+            const uint32_t from = (uint32_t)(min(rr, last) * D * 2);
+            row_dma16(kc + at, from + ((lc ^ (rr & (CPP - 1))) << 4), dst + k * 1024);
+            row_dma16(vc + at, from + ((lc ^ v_swizzle<D>(rr)) << 4), dst + TILE + k * 1024);
+        }
+        return t;
+    };
+    tile_t next = {0, 0, -1, 0};
+    if (nt > 0) next = issue(0);                                   // under way while the queries are read
+
     bf16x8 qf[KS];
     const uint32_t flip = cs < 0.f ? 0x80008000u : 0u;             // a negative scale goes into the queries' signs
     const float acs = fmaxf(fabsf(cs), 0x1p-126f);                 // (a scale of 0 leaves masked scores at -inf)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         u32x4 v = {0, 0, 0, 0};
-        if (lim >= 0) v = *(const u32x4*)(q + (long long)(row0 + ridx) * q_ld + (long long)head * D + 16 * ks + 8 * h);
+        if (lim >= 0) v = *(const u32x4*)(q + (long long)row * q_ld + (long long)head * D + 16 * ks + 8 * h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] ^= flip;
         qf[ks] = __builtin_bit_cast(bf16x8, v);
     }
 
-    // The wave's part of a tile: 16 positions of its block w/2, NI instructions of 1024 / (2 D).
-    const int lp = lane / CPP, lc = lane % CPP;
-    constexpr int PPI = 512 / D;                                   // positions an instruction
-    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)s_buf;
-    const long long hb = (long long)pl.layer * g.LS + (long long)kvh * g.HS;
-    const int nt = max(pe - p0 + PX_TILE - 1, 0) / PX_TILE;
-    // pages of the 32-position blocks p0/32 + 128 win + ..: lane l holds l, l + 64 (-1: none, or past the end)
-    int pgw[2] = {-1, -1}, kw = -(1 << 20);
-    uint32_t there = 0;                                            // bit 2 (i % 2) + k: block k of tile i has a page
-    auto issue = [&](int i) {
-        const int blk0 = 2 * i;
-        if (blk0 < kw || blk0 + 1 >= kw + 128) {
-            kw = blk0;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int pos = p0 + 32 * (kw + 64 * k + lane);
-                pgw[k] = pos < pe ? page_of(g, slot, pos / g.P) : -1;
-                if (pos < pe && pgw[k] < 0) raise(r.err, ERR_PAGE);
-            }
-        }
-        auto page_at = [&](int blk) {
-            const int j = blk - kw, a = __builtin_amdgcn_readlane(pgw[0], j & 63), c = __builtin_amdgcn_readlane(pgw[1], j & 63);
-            return j < 64 ? a : c;
-        };
-        const int pa = page_at(blk0), pb = page_at(blk0 + 1);
-        there = (there & ~(3u << 2 * (i & 1))) | ((pa >= 0 ? 1u : 0u) | (pb >= 0 ? 2u : 0u)) << 2 * (i & 1);
-        const int pg = w < 2 ? pa : pb;
-        if (pg < 0) return;
-        const int bs = p0 + 32 * (blk0 + (w >> 1));
-        // (past the end: the last position again)
-        const int last = min(bs + 31, pe - 1) - bs;
-        const long long at = (long long)pg * g.PS + hb + (long long)(bs % g.P) * D;
-        const uint32_t dst = ring + (i & 1) * (2 * TILE) + w * (NI * 1024);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const int row = 16 * (w & 1) + PPI * j + lp;           // in its block
-            const uint32_t off = (uint32_t)(min(row, last) * D * 2 + ((lc ^ (row & (CPP - 1))) << 4));
-            row_dma16(kc + at, off, dst + j * 1024);
-            row_dma16(vc + at, off, dst + TILE + j * 1024);
-        }
-    };
-
-    float m = -INFINITY, l = 0.f;
+    float m = lim < 0 ? 0.f : -INFINITY, l = 0.f;                  // (a row that is not there never moves its reference)
     floatx16 o[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[nb][i] = 0.f;
 
-    // block k of the tile at `t`, positions from blk on
-    auto block = [&](const uint8_t* t, int k, int blk, auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        const uint8_t* kt = t + (32 * k + lr) * D * 2;
-        floatx16 s;
+    // LDS addresses from a block on: of the lane's K pieces (k-step ks at ^ 32 ks), and of its pieces of the transposing
+    // reads, positions 4 h + l%16/4, dims 16 (l/16%2) + 4 (l%4) of a 32-dim block nb (at ^ 64 nb)
+    const int tr = 4 * h + ((lane & 15) >> 2), tc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const uint32_t ka = lr * D * 2 + ((h ^ (lr & (CPP - 1))) << 4), va = tr * D * 2 + ((tc ^ v_swizzle<D>(tr)) << 4) + (lane & 1) * 8;
+
+    // The scores of the blocks whose K lies `tile` bytes into LDS.  (Left to itself the compiler reads each operand from LDS
+    // right before its product, and every product waits for its read.)
+    auto scores = [&](uint32_t tile, auto& s) {
+        constexpr int N = sizeof(s) / sizeof(floatx16);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const u32x4 kf = *(const u32x4*)(kt + (((2 * ks + h) ^ (lr & (CPP - 1))) << 4));
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[ks], s, 0, 0, 0);
+            for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+        auto fetch = [&](int k) { return *(const __attribute__((address_space(3))) u32x4*)(lds + ((ka + tile) ^ (k / N * 32)) + k % N * BLOCK); };
+        u32x4 kf[KS * N];
+        constexpr int AHEAD = KS;                                  // reads run so many products in front of theirs
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) kf[k] = fetch(k);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < KS * N; ++k) {
+            s[k % N] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[k]), qf[k / N], s[k % N], 0, 0, 0);
+            if (k + AHEAD < KS * N) kf[k + AHEAD] = fetch(k + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (MASKED) {
+    };
+    // the row's largest score, in base 2
+    auto top_of = [&](const auto& s) {
+        constexpr int N = sizeof(s) / sizeof(floatx16);
+        float bm = s[0][0];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (blk + 8 * (i >> 2) + 4 * h + (i & 3) > lim) s[i] = -INFINITY;
-        }
-        float bm = s[0];
+        for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int i = 1; i < 16; ++i) bm = fmaxf(bm, s[i]);
-        bm = other_half_max(bm) * acs;
+            for (int i = 0; i < 16; ++i) bm = fmaxf(bm, s[n][i]);
+        return other_half_max(bm) * acs;
+    };
+    // The probabilities above the reference `from`, into l, and their products with the values `tile` bytes into LDS,
+    // in an order of my own: a block's values are read while its powers are made, a second block's powers go between the first one's products.
+    // cap: +inf, or -inf for a row that sees none of them (whatever its scores are).
+    auto add = [&](uint32_t tile, const auto& s, float from, auto capped, float cap) {
+        constexpr int N = sizeof(s) / sizeof(floatx16), P = 2 * NB;    // products a block
+        uint32_t pk[N][8];
+        bf16x8 vf[N][P];
+        auto power2 = [&](int n, int i) {                          // two of a lane's 16 probabilities
+            float a = __builtin_fmaf(s[n][i], acs, -from), c = __builtin_fmaf(s[n][i + 1], acs, -from);
+            if (decltype(capped)::value) a = fminf(a, cap), c = fminf(c, cap);
+            a = __builtin_amdgcn_exp2f(a);
+            c = __builtin_amdgcn_exp2f(c);
+            l += a + c;
+            pk[n][i >> 1] = pack_bf16x2(a, c);
+        };
+        auto fetch = [&](int n, int k) {                           // the operand of product k: positions 16 (k / NB), dims 32 (k % NB)
+            auto piece = [&](uint32_t at) {
+                return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds + at));
+            };
+            const uint32_t at = ((va + tile) ^ (k % NB * 64)) + (32 * n + 16 * (k / NB)) * D * 2;
+            const v4s lo = piece(at), hi = piece(at + 8 * D * 2);
+            vf[n][k] = __builtin_bit_cast(bf16x8, (v8s){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        };
+        auto product = [&](int n, int k) {
+            const int st = k / NB;
+            const bf16x8 pf = __builtin_bit_cast(bf16x8, (u32x4){pk[n][4 * st], pk[n][4 * st + 1], pk[n][4 * st + 2], pk[n][4 * st + 3]});
+            o[k % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n][k], pf, o[k % NB], 0, 0, 0);
+        };
+#pragma unroll
+        for (int k = 0; k < P; ++k) fetch(0, k);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) power2(0, i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                product(n, k);
+                if (n + 1 < N) {
+                    fetch(n + 1, k);
+#pragma unroll
+                    for (int i = 0; i < 16 / P; i += 2) power2(n + 1, 16 / P * k + i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+    };
+    // A block that some row does not see (a row sees its positions from blk up to `to`), or whose scores move a reference.
+    auto slow_block = [&](uint32_t tile, int blk, int to, uint32_t odd) {
+        floatx16 s[1];
+        scores(tile, s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (blk + 8 * (i >> 2) + 4 * h + (i & 3) > to) s[0][i] = -INFINITY;
+        const float bm = top_of(s);
+        m = m == -INFINITY ? bm : m;                               // nothing seen so far: nothing to rescale
         const bool need = bm > m + 8.f;
         if (__builtin_amdgcn_ballot_w64(need)) {
-            const float mn = need ? bm : m, corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+            const float mn = need ? bm : m, corr = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             l *= corr;
 #pragma unroll
@@ -420,67 +622,99 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, con
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[nb][i] *= corr;
         }
-        const float mn = m == -INFINITY ? 0.f : m;
-        uint32_t pk[8];
+        // the rows that see a value that is not finite are NaN
+        if (odd)
+            for (int p = 0; p < 32; ++p)
+                if ((odd >> p & 1) && blk + p <= to) l = __builtin_nanf("");
+        add(tile + TILE, s, m == -INFINITY ? 0.f : m, std::false_type(), 0.f);
+    };
+    // Values that are not finite in the wave's own 16 positions of a tile become zeros, which 0 times nothing of them is left,
+    // and the positions' bits are noted for the rows that see them.  (Of a block without a page this is what lies there,
+    // for nobody.)
+    auto clean = [&](int i) {
+        constexpr int RPP = 1024 / D / 2;                          // rows a pass, D / 8 lanes of 16 bytes each
+        uint32_t odd = 0;
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], acs, -mn)), c = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], acs, -mn));
-            l += a + c;
-            pk[i >> 1] = pack_bf16x2(a, c);
-        }
-        const uint8_t* vt = t + TILE + 32 * k * D * 2;
-        if (MASKED) {
-            // positions with a value that is not finite: the rows that see one are NaN
-            const uint8_t* vr = vt + (lane >> 1) * D * 2 + (lane & 1) * D;
-            bool odd = false;
+        for (int t = 0; t < 16 / RPP; ++t) {
+            const lds_t p = lds + (i & 1) * (2 * TILE) + TILE + w * (NI * 1024) + t * 1024 + 16 * lane;
+            u32x4 x = *(const __attribute__((address_space(3))) u32x4*)p;
+            u16x2 most = {0, 0};
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                const u32x4 v = *(const u32x4*)(vr + 16 * c);
+            for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
+            const bool hit = most[0] >= 0x7f80 || most[1] >= 0x7f80;
+            const uint64_t b = __builtin_amdgcn_ballot_w64(hit);
+            if (!b) continue;
+            if (hit) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= odd2(v[e]);
+                for (int e = 0; e < 4; ++e) x[e] = finite2(x[e]);
+                *(__attribute__((address_space(3))) u32x4*)p = x;
             }
-            const uint64_t bad = __builtin_amdgcn_ballot_w64(odd);
-            if (bad)
-                for (int p = 0; p < 32; ++p)
-                    if ((bad >> 2 * p & 3) && blk + p <= lim) l = __builtin_nanf("");
+            for (int e = 0; e < RPP; ++e) odd |= (b >> CPP * e & (CPP == 8 ? 255 : 65535) ? 1u : 0u) << (RPP * t + e);
         }
-        // lane l's pieces of the transposing reads: positions 4 h + l%16/4 (+ 8, + 16 st), dims 16 (l/16%2) + 4 (l%4) of a 32-dim block
-        const int tr = 4 * h + ((lane & 15) >> 2), tc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), tb = (lane & 1) * 8;
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            const bf16x8 pf = __builtin_bit_cast(bf16x8, (u32x4){pk[4 * st], pk[4 * st + 1], pk[4 * st + 2], pk[4 * st + 3]});
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                auto piece = [&](int row) {
-                    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) v4s*)(vt + row * D * 2 + (((4 * nb + tc) ^ (row & (CPP - 1))) << 4) + tb));
-                };
-                const v4s lo = piece(16 * st + tr), hi = piece(16 * st + 8 + tr);
-                u32x4 vf = __builtin_bit_cast(u32x4, (v8s){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
-                if (MASKED) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) vf[e] = finite2(vf[e]);
-                }
-                o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[nb], 0, 0, 0);
-            }
-        }
+        if (lane == 0) ((uint16_t*)s_odd)[4 * (i & 1) + w] = (uint16_t)odd;
     };
 
-    if (nt > 0) issue(0);
+    // The walk.  Tiles are of three kinds: what every row sees as a whole, what the rows of one sequence see as a whole and the
+    // others not at all, and the rest.  The first two, as long as they move no reference, are loops of their own, which
+    // change no sum but by adding: with the references' rescaling inside them the compiler keeps a second copy of O and
+    // moves it every tile.
+    enum { ALL, ONE, PART };
     const bool works = 32 * rt < nrows;
-    for (int i = 0; i < nt; ++i) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        lds_barrier();                                             // everyone's pieces are in, and tile i - 1 is done with
-        const uint32_t have = there >> 2 * (i & 1);
-        if (i + 1 < nt) issue(i + 1);
-        if (!works) continue;
-        const uint8_t* t = s_buf + (i & 1) * (2 * TILE);
-        for (int k = wide ? 0 : w >> 1; k < 2; k += wide ? 1 : 2) {
-            const int blk = p0 + PX_TILE * i + 32 * k;
-            if (!(have >> k & 1)) continue;                        // no page, or past the end
-            if (blk + 32 <= min(pe, seen_all)) block(t, k, blk, std::false_type());
-            else block(t, k, blk, std::true_type());
+    const int from = wide ? 0 : w >> 1, first_row = r0 / G;        // the wave's first block, the slice's first row of its sequence
+    constexpr uint32_t mine = wide ? 3 : 1;
+    tile_t cur = next;
+    uint32_t have = 0;
+    int i = -1, kind = PART;
+    bool dirty = false;                                            // tile i was cleaned
+    // the next tile in which the wave has something to do; false: there is none
+    auto advance = [&] {
+        while (++i < nt) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            cur = next;
+            const bool whole = cur.seq < 0 || cur.pos + PX_TILE <= min(cur.end, __builtin_amdgcn_readlane(inf.base, cur.seq & 63) + first_row + 1);
+            const bool one = cur.seq >= 0 && nseq > 1;
+            dirty = one || !whole;
+            if (dirty) clean(i);
+            lds_barrier();                                         // everyone's pieces are in, and tile i - 1 is done with
+            if (i + 1 < nt) next = issue(i + 1);
+            have = cur.have >> from & mine;
+            kind = !whole || have != mine ? PART : one ? ONE : ALL;
+            if (works && have && (!dirty || __builtin_amdgcn_ballot_w64(sr == cur.seq && lim >= cur.pos))) return true;
         }
+        return false;
+    };
+    for (bool more = true; advance();) {
+        const auto walk = [&](auto which) {
+            constexpr int KIND = decltype(which)::value;
+            while (more && kind == KIND) {
+                const uint32_t tile = (i & 1) * (2 * TILE) + BLOCK * from;
+                floatx16 s[NBLK];
+                scores(tile, s);
+                float top = top_of(s), cap = INFINITY;
+                if (KIND == ONE) {
+                    if (sr != cur.seq) top = cap = -INFINITY;
+                    uint32_t odd = 0;
+                    for (int n = 0; n < NBLK; ++n) odd |= s_odd[2 * (i & 1) + from + n];
+                    if (odd && sr == cur.seq) l = __builtin_nanf("");
+                }
+                m = m == -INFINITY ? top : m;                      // nothing seen so far: nothing to rescale
+                if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
+                    kind = PART;
+                    return;
+                }
+                add(tile + TILE, s, m == -INFINITY ? 0.f : m, std::integral_constant<bool, KIND == ONE>(), cap);
+                more = advance();
+            }
+        };
+        walk(std::integral_constant<int, ALL>());
+        walk(std::integral_constant<int, ONE>());
+        if (!more) break;
+        // (of a shared tile, or of a slice's only sequence, rows may be compared with any position that they see)
+        const int to = cur.seq < 0 ? INT_MAX : sr == cur.seq ? lim : -1;
+#pragma clang loop unroll(disable)
+        for (int n = 0; n < NBLK; ++n)
+            if (have >> n & 1)
+                slow_block((i & 1) * (2 * TILE) + BLOCK * (from + n), cur.pos + 32 * (from + n), to, dirty ? s_odd[2 * (i & 1) + from + n] : 0);
     }
     l = other_half_sum(l);
     if (lim < 0) m = -INFINITY, l = 0.f;                           // a row that is not there sees nothing (its o is not used)
@@ -528,7 +762,7 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, con
         return;
     }
     const float rl = l == 0.f ? 0.f : 1.f / l;
-    const size_t oi = (size_t)(row0 + ridx) * out_ld + (size_t)head * D;
+    const size_t oi = (size_t)row * out_ld + (size_t)head * D;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -538,34 +772,69 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, con
                                : make_float4(o[nb][4 * j] * rl, o[nb][4 * j + 1] * rl, o[nb][4 * j + 2] * rl, o[nb][4 * j + 3] * rl));
 }
 
-// The parts of a row joined: D/4 lanes a (row, head), parts in order, eight under way
-// at once.
+// SELF: without a plan in memory, it is made here
+template <int D, bool SELF>
+__global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, const uint16_t* kc, const uint16_t* vc, int n_q, int n_kv,
+                                                        const uint16_t* q, long long q_ld, float cs, px_plan pl, px_groups gr, void* out,
+                                                        int out_t, long long out_ld)
+{
+    constexpr int RING = 4 * PX_TILE * D * 2, MERGE = 64 * (D + 4) * 4;
+    __shared__ __attribute__((aligned(1024))) uint8_t s_buf[RING > MERGE ? RING : MERGE];
+    __shared__ float2 s_ml[64];
+    __shared__ uint32_t s_odd[4];                                  // of the ring's two tiles, a bit a position
+    const int lane = threadIdx.x & 63;
+    px_item it;
+    px_info inf = {-1, 0, 0, 0};                                   // lane l: of the slice's sequence l
+    if constexpr (SELF) {
+        const bool teller = blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64;
+        const int RG = r.n * (n_q / n_kv);
+        const wave_plan p = plan_of_wave(r, gr, pl, RG, teller);
+        if (teller && lane < r.B) pl.seq[lane] = seq_of(p, RG);
+        it = item_of(p, pl, RG, blockIdx.y);
+        const int at = min(it.f + lane, 63);
+        const px_info x = {__shfl(p.info.slot, at, WAVE), __shfl(p.info.base, at, WAVE), __shfl(p.info.ctx, at, WAVE), __shfl(p.info.nlive, at, WAVE)};
+        if (lane < it.nseq) inf = x;
+    } else {
+        it = pl.item[blockIdx.y];
+        if (lane < it.nseq) inf = pl.info[it.f + lane];
+    }
+    const int rows = __builtin_amdgcn_readfirstlane(it.rows);
+    if (rows == 0) return;                                         // no item
+    if (rows > 64) attend_item<D, 2>(s_buf, s_ml, s_odd, it, inf, r, g, kc, vc, n_q, n_kv, q, q_ld, cs, pl, out, out_t, out_ld);
+    else attend_item<D, 1>(s_buf, s_ml, s_odd, it, inf, r, g, kc, vc, n_q, n_kv, q, q_ld, cs, pl, out, out_t, out_ld);
+}
+
+// The parts of a row joined: a wave a (row, head), D/4 lanes a part, eight parts of each under way at once; a
+// part that saw nothing of the row (l = 0) is not read.
 template <int D>
 __global__ void __launch_bounds__(256) k_prefix_combine(rows_t r, px_plan pl, int n_q, int n_kv, void* out, int out_t, long long out_ld)
 {
-    constexpr int LPR = D / 4, U = 8;
-    const long long unit = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    const int G = n_q / n_kv;
-    const int row = (int)(unit / n_q), head = (int)(unit - (long long)row * n_q), b = row / r.n, i = row - b * r.n, d = 4 * (threadIdx.x % LPR);
+    constexpr int LPP = D / 4, NP = WAVE / LPP, U = 4;             // lanes a part, parts side by side
+    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int G = n_q / n_kv, row = (int)(unit / n_q), head = (int)(unit - (long long)row * n_q), b = row / r.n, i = row - b * r.n;
     if (b >= r.B || (r.lim && i >= r.lim[b])) return;
     const px_seq q = pl.seq[b];
-    const int parts = q.pfx_n + q.own_n;
-    if (parts == 0) return;                                        // the attention wrote the output
-    const int kvh = head / G, t = i * G + head - kvh * G, RG = r.n * G;
-    const size_t at = (size_t)kvh * pl.part_rows;
+    if (q.nc <= 1) return;                                         // the attention wrote the output
+    const int lane = threadIdx.x & 63, d = 4 * (lane % LPP), side = lane / LPP;
+    const int kvh = head / G, t = i * G + head - kvh * G, RG = r.n * G, zz = pl.zs == 1 ? 0 : t / PX_ROWS;
+    const int stride = pl.zs == 1 ? q.stride : min(PX_ROWS, RG - PX_ROWS * zz);
+    const size_t at = (size_t)kvh * pl.part_rows + q.part + (size_t)zz * q.nc * PX_ROWS + (t - PX_ROWS * zz);
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < parts; c0 += U) {
+    for (int c0 = side; c0 < q.nc; c0 += U * NP) {
         float2 ml[U];
         float4 x[U];
         float bm = m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = min(c0 + u, parts - 1), own = c - q.pfx_n;
-            const size_t pr = at + (own < 0 ? q.pfx_part + c * q.pfx_rows : q.own_part + own * RG) + t;
-            ml[u] = pl.ml[pr];
-            x[u] = *(const float4*)(pl.o + pr * D + d);
+            ml[u] = make_float2(-INFINITY, 0.f);
+            if (c0 + u * NP < q.nc) ml[u] = pl.ml[at + (size_t)(c0 + u * NP) * stride];
             bm = fmaxf(bm, ml[u].x);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (ml[u].x != -INFINITY || ml[u].y != 0.f) x[u] = *(const float4*)(pl.o + (at + (size_t)(c0 + u * NP) * stride) * D + d);
         }
         const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - bm);
         m = bm;
@@ -573,13 +842,22 @@ __global__ void __launch_bounds__(256) k_prefix_combine(rows_t r, px_plan pl, in
         o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            // a part that saw nothing has l = 0 and any o
-            if (c0 + u >= parts || (ml[u].x == -INFINITY && ml[u].y == 0.f)) continue;
             const float e = ml[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - m);
             l += ml[u].y * e;
             o = make_float4(o.x + x[u].x * e, o.y + x[u].y * e, o.z + x[u].z * e, o.w + x[u].w * e);
         }
     }
+    // the sides joined, in all of them alike
+#pragma unroll
+    for (int k = LPP; k < WAVE; k <<= 1) {
+        const float om = __shfl_xor(m, k, WAVE), bm = fmaxf(m, om);
+        const float fa = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - bm), fb = om == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(om - bm);
+        m = bm;
+        l = l * fa + __shfl_xor(l, k, WAVE) * fb;
+        o = make_float4(o.x * fa + __shfl_xor(o.x, k, WAVE) * fb, o.y * fa + __shfl_xor(o.y, k, WAVE) * fb, o.z * fa + __shfl_xor(o.z, k, WAVE) * fb,
+                        o.w * fa + __shfl_xor(o.w, k, WAVE) * fb);
+    }
+    if (side) return;
     const float rl = l == 0.f ? 0.f : 1.f / l;
     px_store4(out, out_t, (size_t)row * out_ld + (size_t)head * D + d,
               l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * rl, o.y * rl, o.z * rl, o.w * rl));
@@ -604,17 +882,21 @@ template void launch_kv_append<f32_parts>(const rows_t&, const cache_t&, int, in
 template void launch_kv_append<uint16_t>(const rows_t&, const cache_t&, int, int, kv4_src<uint16_t>, kv4_src<uint16_t>, kv4_src<uint16_t>,
                                          uint16_t*, const kv4_rope&, hipStream_t);
 
-// Two work-groups a CU are resident.  Every run and sequence may have one chunk more
-// than its share of the target; a run's slices and a sequence's read their chunks each.
+// The plan in the attention itself: where its grid, the target's work-groups, holds every item (there are at most half as
+// many slices, and shares of up to three times the even one).
+bool prefix_plans_itself(const px_plan& p, int B) { return B <= PX_WAVE && 2ll * B * p.zs <= p.target; }
+
+// Two work-groups a CU are resident.  A slice may have one chunk more than its share of the target (and one more is what the
+// share, in floats, may be off).
 px_plan prefix_plan(int B, int n, int n_q, int n_kv)
 {
     px_plan p = {};
-    const long long RG = (long long)n * (n_q / n_kv);
+    const int RG = n * (n_q / n_kv);
+    p.zs = (RG + PX_ROWS - 1) / PX_ROWS;
+    p.sps = p.zs > 1 ? 1 : PX_ROWS / RG < 64 ? PX_ROWS / RG : 64;
     p.target = 512 / n_kv > 1 ? 512 / n_kv : 1;
-    p.min_chunk = 128;
-    const long long zs = (RG + PX_ROWS - 1) / PX_ROWS, run_slices = (B * RG + PX_ROWS - 1) / PX_ROWS + B / 2;
-    p.max_items = p.target + run_slices + B * zs;
-    p.part_rows = (long long)p.target * PX_ROWS + 2 * B * RG;
+    p.max_items = p.target + (long long)B * p.zs + 1;
+    p.part_rows = (long long)(p.target + 1) * PX_ROWS + (long long)B * RG;
     return p;
 }
 
@@ -622,51 +904,55 @@ static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t prefix_plan_bytes(const px_plan& p, int B, int n_kv, int D)
 {
-    return up256((size_t)B * sizeof(px_seq)) + up256((size_t)p.max_items * sizeof(px_item)) + up256((size_t)n_kv * p.part_rows * 8) +
-           up256((size_t)n_kv * p.part_rows * D * 4);
+    return up256((size_t)B * sizeof(px_seq)) + up256((size_t)B * sizeof(px_info)) + up256((size_t)p.max_items * sizeof(px_item)) +
+           up256((size_t)n_kv * p.part_rows * 8) + up256((size_t)n_kv * p.part_rows * D * 4);
 }
 
 void prefix_plan_bind(px_plan& p, void* buf, int B, int n_kv)
 {
     char* c = (char*)buf;
-    p.seq = (px_seq*)c;
-    c += up256((size_t)B * sizeof(px_seq));
-    p.item = (px_item*)c;
-    c += up256((size_t)p.max_items * sizeof(px_item));
-    p.ml = (float2*)c;
-    c += up256((size_t)n_kv * p.part_rows * 8);
+    auto take = [&](size_t bytes) {
+        char* at = c;
+        c += up256(bytes);
+        return at;
+    };
+    p.seq = (px_seq*)take((size_t)B * sizeof(px_seq));
+    p.info = (px_info*)take((size_t)B * sizeof(px_info));
+    p.item = (px_item*)take((size_t)p.max_items * sizeof(px_item));
+    p.ml = (float2*)take((size_t)n_kv * p.part_rows * 8);
     p.o = (float*)c;
 }
 
 void launch_prefix_plan(const rows_t& r, const px_groups& g, const px_plan& p, int n_q, int n_kv, hipStream_t s)
 {
-    k_prefix_plan<<<1, 1024, 0, s>>>(r, g, p, n_q / n_kv);
+    const int RG = r.n * (n_q / n_kv);
+    if (r.B <= PX_WAVE) k_prefix_plan_wave<<<1, 256, 0, s>>>(r, g, p, RG);
+    else k_prefix_plan<<<1, 1024, 0, s>>>(r, g, p, RG);
 }
 
 template <int D>
-static void prefix_attn_d(const rows_t& r, const px_plan& p, const cache_t& c, int n_q, const uint16_t* q, long long q_ld, float cs, void* out,
+static void prefix_attn_d(const rows_t& r, const px_plan& p, const px_groups& g, const cache_t& c, int n_q, const uint16_t* q, long long q_ld, float cs, void* out,
                           act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
 {
-    const dim3 grid(c.n_kv, p.max_items);
+    const dim3 grid(c.n_kv, p.item ? p.max_items : p.target);
+    const auto kern = p.item ? k_prefix_attn<D, false> : k_prefix_attn<D, true>;
     const uint16_t *kc = (const uint16_t*)c.k, *vc = (const uint16_t*)c.v;
-    if (ev0) hipExtLaunchKernelGGL(k_prefix_attn<D>, grid, dim3(256), 0, s, ev0, ev1, 0, r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, out, (int)out_t, out_ld);
-    else k_prefix_attn<D><<<grid, 256, 0, s>>>(r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, out, (int)out_t, out_ld);
+    if (ev0) hipExtLaunchKernelGGL(kern, grid, dim3(256), 0, s, ev0, ev1, 0, r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, g, out, (int)out_t, out_ld);
+    else kern<<<grid, 256, 0, s>>>(r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, g, out, (int)out_t, out_ld);
 }
 
-void launch_prefix_attention(const rows_t& r, px_plan p, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld, float scale,
+void launch_prefix_attention(const rows_t& r, px_plan p, const px_groups& g, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld, float scale,
                              void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
 {
     p.layer = layer;
     const float cs = scale * 1.4426950408889634f;
-    if (c.head_dim == 128) prefix_attn_d<128>(r, p, c, n_q, q, q_ld, cs, out, out_t, out_ld, s, ev0, ev1);
-    else prefix_attn_d<64>(r, p, c, n_q, q, q_ld, cs, out, out_t, out_ld, s, ev0, ev1);
+    if (c.head_dim == 128) prefix_attn_d<128>(r, p, g, c, n_q, q, q_ld, cs, out, out_t, out_ld, s, ev0, ev1);
+    else prefix_attn_d<64>(r, p, g, c, n_q, q, q_ld, cs, out, out_t, out_ld, s, ev0, ev1);
 }
 
 void launch_prefix_combine(const rows_t& r, const px_plan& p, int n_q, int n_kv, int D, void* out, act_t out_t, long long out_ld, hipStream_t s)
 {
-    const long long units = (long long)r.B * r.n * n_q;
-    const int per = 256 / (D / 4);
-    const unsigned blocks = (unsigned)((units + per - 1) / per);
+    const unsigned blocks = (unsigned)(((long long)r.B * r.n * n_q + 3) / 4);
     if (D == 128) k_prefix_combine<128><<<blocks, 256, 0, s>>>(r, p, n_q, n_kv, out, (int)out_t, out_ld);
     else k_prefix_combine<64><<<blocks, 256, 0, s>>>(r, p, n_q, n_kv, out, (int)out_t, out_ld);
 }
