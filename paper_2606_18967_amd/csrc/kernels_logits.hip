@@ -15,9 +15,13 @@
 // gradient is rounded once.  A logit of -inf has p = 0 and no gradient; where y
 // is a factor it is held above Y_MIN, so that 0 y is 0.
 //
-// What bounds them: the bytes of the logits, read once and, with a gradient,
-// written once.  A row is held in registers between its sums and its gradient as
-// far as it fits (k_policy_rows).
+// What bounds them: the bytes of the logits.  A gradient needs its row's sums first;
+// where one kernel makes both, the second reading is left to the caches, and all
+// others go past them: the loss of 8192 x 128256 bf16 rows (a fifth of them padding,
+// 3.8 GB of logits and gradients) takes 735 us, which is the rate of a large copy,
+// with both readings past the caches 958, with neither 746, with a work-group of 512
+// threads instead of 1024 767.  Alone, the log-probabilities of 2048 x 152064 take
+// 95 us (6.6 TB/s), their gradient 207 (6.0 TB/s; its stores past the caches 226).
 #include "common.h"
 #include "kernels.h"
 
@@ -58,15 +62,20 @@ template <> struct pack_t<float> {
     }
 };
 
-template <typename T>
+// KEEP: the logits are read again, and are to stay in the caches until then
+template <bool KEEP, typename T>
 __device__ __forceinline__ u32x4 load_vec(const T* p)
 {
-    return (u32x4)__builtin_nontemporal_load((const typename pack_t<T>::vec*)p);
+    const auto v = (const typename pack_t<T>::vec*)p;
+    return KEEP ? (u32x4)*v : (u32x4)__builtin_nontemporal_load(v);
 }
-template <typename T>
+// PASS: past the caches
+template <bool PASS, typename T>
 __device__ __forceinline__ void store_vec(T* p, u32x4 v)
 {
-    __builtin_nontemporal_store((typename pack_t<T>::vec)v, (typename pack_t<T>::vec*)p);
+    const auto to = (typename pack_t<T>::vec*)p;
+    if (PASS) __builtin_nontemporal_store((typename pack_t<T>::vec)v, to);
+    else *to = (typename pack_t<T>::vec)v;
 }
 
 // running sums of a part of a row: m the largest logit, s and t as above
@@ -121,7 +130,7 @@ __device__ __forceinline__ part_t join(part_t a, float c, float* sh)
 
 // A thread's pass over the logits [from, n) of a row part, vector by vector of the
 // work-group, U of them under way at once.
-template <typename T, int U>
+template <typename T, int U, bool KEEP>
 __device__ __forceinline__ void sum_part(part_t& a, const T* x, int first, int n, float c)
 {
     constexpr int N = pack_t<T>::N;
@@ -129,7 +138,7 @@ __device__ __forceinline__ void sum_part(part_t& a, const T* x, int first, int n
     for (int i0 = first + threadIdx.x * N; i0 + N <= n; i0 += U * step) {
         u32x4 v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = load_vec(x + min(i0 + u * step, n - N));
+        for (int u = 0; u < U; ++u) v[u] = load_vec<KEEP>(x + min(i0 + u * step, n - N));
         float m = a.m, y[U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -191,7 +200,7 @@ __device__ __forceinline__ void grad_vec(float (&x)[N], const grad_t& d, float c
 
 // A thread's pass that writes the gradient of the logits [first, n), and of the last
 // n % N where tail is set.  out may be x: a thread reads what it writes first.
-template <typename T, bool ENT, int U>
+template <typename T, bool ENT, int U, bool PASS>
 __device__ __forceinline__ void grad_part(const T* x, T* out, int first, int n, const grad_t& d, float c)
 {
     constexpr int N = pack_t<T>::N;
@@ -200,14 +209,14 @@ __device__ __forceinline__ void grad_part(const T* x, T* out, int first, int n, 
         u32x4 v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i0 + u * step + N <= n) v[u] = load_vec(x + i0 + u * step);
+            if (i0 + u * step + N <= n) v[u] = load_vec<false>(x + i0 + u * step);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (i0 + u * step + N > n) break;
             float y[N];
             pack_t<T>::get(v[u], y);
             grad_vec<ENT>(y, d, c);
-            store_vec(out + i0 + u * step, pack_t<T>::put(y));
+            store_vec<PASS>(out + i0 + u * step, pack_t<T>::put(y));
         }
     }
 }
@@ -221,7 +230,7 @@ template <typename T>
 __device__ __forceinline__ void zero_part(T* out, int n)
 {
     constexpr int N = pack_t<T>::N;
-    for (int i = threadIdx.x * N; i + N <= n; i += blockDim.x * N) store_vec(out + i, (u32x4){0, 0, 0, 0});
+    for (int i = threadIdx.x * N; i + N <= n; i += blockDim.x * N) store_vec<true>(out + i, (u32x4){0, 0, 0, 0});
     const int i = n / N * N + threadIdx.x;
     if (i < n) elem<T>::store(out, i, 0.f);
 }
@@ -298,7 +307,7 @@ __global__ void __launch_bounds__(1024) k_policy_rows(logits_args a, policy_args
     const int tok = p.tok[row];
     const float xt = elem<T>::load(x, tok);
     part_t s = {-INFINITY, 0.f, 0.f};
-    sum_part<T, 4>(s, x, 0, V, a.c);
+    sum_part<T, 4, GRAD>(s, x, 0, V, a.c);
     sum_tail(s, x, V, a.c);
     s = join(s, a.c, sh);
     const row_stat st = row_of(s, xt, a.T);
@@ -306,7 +315,7 @@ __global__ void __launch_bounds__(1024) k_policy_rows(logits_args a, policy_args
     if (threadIdx.x == 0) put_row(p, row, st, o);
     if (GRAD) {
         const grad_t d = grad_of(s.m, st.ln_s, 1.f / (s.s * a.T), st.entropy, o.g, o.h, a.T);
-        grad_part<T, ENT, 4>(x, out, 0, V, d, a.c);
+        grad_part<T, ENT, 4, true>(x, out, 0, V, d, a.c);
         grad_tail<T, ENT>(x, out, V, d, a.c);
         // the token's own, by the thread that wrote its place before
         constexpr int N = pack_t<T>::N;
@@ -317,7 +326,7 @@ __global__ void __launch_bounds__(1024) k_policy_rows(logits_args a, policy_args
 }
 
 // A row in several work-groups, where there are few rows: the sums of a part each.
-template <typename T>
+template <typename T, bool KEEP>
 __global__ void __launch_bounds__(256) k_row_parts(logits_args a, const int32_t* tok, part_t* parts)
 {
     __shared__ float sh[48];
@@ -325,7 +334,7 @@ __global__ void __launch_bounds__(256) k_row_parts(logits_args a, const int32_t*
     if (tok[row] < 0 || tok[row] >= a.V) return;
     const T* x = (const T*)a.x + (long long)row * a.ld + c0;
     part_t s = {-INFINITY, 0.f, 0.f};
-    sum_part<T, 4>(s, x, 0, n, a.c);
+    sum_part<T, 4, KEEP>(s, x, 0, n, a.c);
     sum_tail(s, x, n, a.c);
     s = join(s, a.c, sh);
     if (threadIdx.x == 0) parts[(size_t)row * gridDim.x + k] = s;
@@ -371,7 +380,7 @@ __global__ void __launch_bounds__(1024) k_logp_rows(logits_args a, logp_args p)
     float xt = 0.f;
     if (live) {
         xt = elem<T>::load(x, tok);
-        sum_part<T, 4>(s, x, 0, V, a.c);
+        sum_part<T, 4, false>(s, x, 0, V, a.c);
         sum_tail(s, x, V, a.c);
         s = join(s, a.c, sh);
     }
@@ -409,7 +418,7 @@ __global__ void __launch_bounds__(1024) k_logp_grad(logits_args a, logp_grad_arg
     const int at = tok - c0;
     if (at >= 0 && at < n) xt = elem<T>::load(x, at);
     constexpr int N = pack_t<T>::N;
-    grad_part<T, ENT, 4>(x, out, 0, n, d, a.c);
+    grad_part<T, ENT, 4, false>(x, out, 0, n, d, a.c);
     grad_tail<T, ENT>(x, out, n, d, a.c);
     const int body = n / N * N;
     if (at >= 0 && at < n && threadIdx.x == (at < body ? at / N % blockDim.x : at - body))
@@ -451,7 +460,7 @@ __global__ void __launch_bounds__(256) k_policy_grad(logits_args a, policy_args 
     const int at = p.tok[row] - c0;
     float xt = 0.f;
     if (at >= 0 && at < n) xt = elem<T>::load(x, at);
-    grad_part<T, ENT, 4>(x, out, 0, n, d, a.c);
+    grad_part<T, ENT, 4, true>(x, out, 0, n, d, a.c);
     grad_tail<T, ENT>(x, out, n, d, a.c);
     constexpr int N = pack_t<T>::N;
     const int body = n / N * N;
@@ -496,7 +505,7 @@ void logp_t(const logits_args& a, const logp_args& p, int rows, int S, float* wo
         k_logp_rows<T><<<rows, row_threads<T>(a.V, 1024), 0, s>>>(a, p);
         return;
     }
-    k_row_parts<T><<<dim3(S, rows), row_threads<T>(a.chunk, 256), 0, s>>>(a, p.tok, (part_t*)work);
+    k_row_parts<T, false><<<dim3(S, rows), row_threads<T>(a.chunk, 256), 0, s>>>(a, p.tok, (part_t*)work);
     k_logp_finish<T><<<rows, 64, 0, s>>>(a, p, (const part_t*)work, S);
 }
 template <typename T>
@@ -512,7 +521,8 @@ void policy_t(const logits_args& a, const policy_args& p, int rows, int S, float
         const int nt = row_threads<T>(a.chunk, 256);
         part_t* parts = (part_t*)work;
         grad_t* grads = (grad_t*)(work + (size_t)rows * S * 3);
-        k_row_parts<T><<<dim3(S, rows), nt, 0, s>>>(a, p.tok, parts);
+        if (a.out) k_row_parts<T, true><<<dim3(S, rows), nt, 0, s>>>(a, p.tok, parts);
+        else k_row_parts<T, false><<<dim3(S, rows), nt, 0, s>>>(a, p.tok, parts);
         k_policy_finish<T><<<rows, 64, 0, s>>>(a, p, parts, S, grads);
         if (a.out && ent) k_policy_grad<T, true><<<dim3(S, rows), nt, 0, s>>>(a, p, grads);
         else if (a.out) k_policy_grad<T, false><<<dim3(S, rows), nt, 0, s>>>(a, p, grads);

@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 import gc
 import os
 import threading
@@ -790,6 +791,7 @@ def prefix_attention(cache: KVPages, groups: PrefixGroups | None, layer: int, sl
 
 
 # ------------------------------------------------- logits rows: log-probabilities, policy loss
+@functools.lru_cache(maxsize=64)
 def logits_workspace_bytes(rows: int, vocab: int) -> int:
     """Bytes of the workspace of token_logprobs and policy_loss."""
     nb = int(lib().sd_logits_workspace_bytes(rows, vocab))
@@ -806,9 +808,10 @@ def _logit_rows(t, name: str, shape=None, dtype=None, dev=None):
         raise ValueError(f"{name}: expected {dtype or 'float32 or bfloat16'}, got {t.dtype}")
     if t.dim() < 1 or t.shape[-1] < 1 or (shape is not None and t.shape != shape):
         raise ValueError(f"{name}: expected shape {tuple(shape) if shape is not None else '[..., V]'}, got {tuple(t.shape)}")
-    if dev is not None and t.device != dev:
-        raise ValueError(f"{name}: on {t.device}, expected {dev}")
-    if t.device.index != torch.cuda.current_device():
+    if dev is not None:
+        if t.device != dev:
+            raise ValueError(f"{name}: on {t.device}, expected {dev}")
+    elif t.device.index != torch.cuda.current_device():
         raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     V, st, ld = t.shape[-1], t.stride(), None
     rows = 1
@@ -872,6 +875,7 @@ class PolicyLoss:
     def __init__(self, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0, entropy_coef: float = 0.0,
                  is_low: float = 0.5, is_high: float = 2.0, temperature: float = 1.0):
         self.c = PolicyCfg(temperature, clip_low, clip_high, kl_coef, entropy_coef, is_low, is_high, 0)
+        self._ref = C.byref(self.c)
 
 
 class PolicyOut:
@@ -900,10 +904,11 @@ def policy_loss(cfg: PolicyLoss, logits, tokens, old_logp, advantage, weight, re
     op, o_ld = (None, 0) if dlogits is None else _logit_rows(dlogits, "dlogits", logits.shape, logits.dtype, dev)[:2]
     f32 = lambda t, name: None if t is None else _ptr(t, name, torch.float32, shape, dev)
     workspace, wp, nb = _rows_workspace(workspace, rows, V, dev)     # (held until the call is enqueued)
+    olp, ap, wt = (_ptr(t, name, torch.float32, shape, dev) for t, name in ((old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight")))
     stats = torch.empty(6, dtype=torch.float32, device=dev)
-    logp, entropy = (torch.empty(shape, dtype=torch.float32, device=dev) for _ in range(2))
-    _check(lib().sd_policy_loss(C.byref(cfg.c), dt, rows, V, xp, ld, tp, f32(old_logp, "old_logp"), f32(behavior_logp, "behavior_logp"),
-                                f32(ref_logp, "ref_logp"), f32(advantage, "advantage"), f32(weight, "weight"), stats.data_ptr(),
+    logp, entropy = torch.empty_like(old_logp), torch.empty_like(old_logp)
+    _check(lib().sd_policy_loss(cfg._ref, dt, rows, V, xp, ld, tp, olp, f32(behavior_logp, "behavior_logp"),
+                                f32(ref_logp, "ref_logp"), ap, wt, stats.data_ptr(),
                                 logp.data_ptr(), entropy.data_ptr(), op, o_ld, wp, nb, _stream()))
     return PolicyOut(stats, logp, entropy, dlogits)
 
