@@ -31,35 +31,39 @@ __device__ __forceinline__ int page_of(const kv_geom& g, int slot, int lp)
 }
 
 // ------------------------------------------------------------------ append
-// A work-group a row, D/8 lanes a head, U of a thread's heads under way at once: the row's
-// position, page and table entries are looked up once.  Bound by the rows' bytes,
-// with few rows by the chain of loads slot, length, page.
-template <typename T, int D>
+// D/8 lanes a head.  Rows of many heads (WIDE) take a work-group each, U of a thread's heads under
+// way at once: the row's position, page and table entries are looked up once.  Rows of fewer heads
+// lie side by side in a work-group, a head a thread group.  Bound by the rows' bytes, short rows and few of them by
+// the chain of loads slot, length, page: 12216 fp32 rows of 12 heads of 64, 28 MB, take 12.2 us (with a
+// work-group each 19.0, with four rows of a thread under way 15.6), 8 rows of 48 heads of 128 4.5 us.
+template <typename T, int D, bool WIDE>
 __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t* kc, uint16_t* vc, int n_q, int n_kv, kv4_src<T> xk,
                                                    kv4_src<T> xv, kv4_src<T> xq, uint16_t* q_out, kv4_rope ro)
 {
-    constexpr int LPR = D / 8, HPP = 256 / LPR, U = 4;             // lanes a head, heads a pass
-    const int idx = blockIdx.x, b = idx / r.n, i = idx - b * r.n;
-    const int nl = r.lim ? r.lim[b] : r.n, nlive = min(max(nl, 0), r.n);
-    const int slot = r.slots[b];
-    const bool has_slot = slot >= 0 && slot < r.max_slots, first = i == 0 && threadIdx.x == 0;
-    if (first && nl != nlive) raise(r.err, ERR_LEN);
-    if (i >= nlive) return;
-    const int pos = has_slot ? kv4_base((long long)r.kv_len[slot] + r.off) + i : -1;
+    constexpr int LPR = D / 8, HPP = 256 / LPR, U = WIDE ? 4 : 1;  // lanes a head, heads a pass
+    const int nq = q_out ? n_q : 0, units = nq + 2 * n_kv, place = threadIdx.x / LPR, d0 = 8 * (threadIdx.x % LPR);
+    const int abreast = WIDE ? 1 : HPP / units, sub = WIDE ? 0 : place / units, idx = blockIdx.x * abreast + sub;
+    const bool in = WIDE || (sub < abreast && idx < r.B * r.n);
+    const int b = in ? idx / r.n : 0, i = in ? idx - b * r.n : 0;
+    const int nl = r.lim ? r.lim[b] : r.n, nlive = min(max(nl, 0), r.n), slot = r.slots[b];
+    const bool there = in && i < nlive, tells = in && d0 == 0 && place == sub * units, has_slot = slot >= 0 && slot < r.max_slots;
+    if (tells && i == 0 && nl != nlive) raise(r.err, ERR_LEN);
+    if (WIDE && !there) return;
+    const int pos = there && has_slot ? kv4_base((long long)r.kv_len[slot] + r.off) + i : -1;
     const int stop = ro.rot ? min(r.max_ctx, ro.len) : r.max_ctx;  // first position without a table row or a place
     const bool ok = pos >= 0 && pos < stop;
-    if (threadIdx.x == 0 && !ok) raise(r.err, has_slot ? ERR_CTX : ERR_SLOT);
+    if (tells && there && !ok) raise(r.err, has_slot ? ERR_CTX : ERR_SLOT);
     const int page = ok ? page_of(g, slot, pos / g.P) : -1;
-    if (threadIdx.x == 0 && ok && page < 0) raise(r.err, ERR_PAGE);
-    const int lw = threadIdx.x % LPR, d0 = 8 * lw, nq = q_out ? n_q : 0, units = nq + 2 * n_kv;
+    if (tells && ok && page < 0) raise(r.err, ERR_PAGE);
     float2 tr[8] = {};
     if (ok) turns(ro, pos, d0, tr);
     const long long at = (long long)max(page, 0) * g.PS + (long long)(max(pos, 0) % g.P) * D + d0;
-    for (int u0 = threadIdx.x / LPR; u0 - (int)(threadIdx.x / LPR) < units; u0 += U * HPP) {
+    const int own = WIDE ? place : place - sub * units;
+    for (int u0 = 0; u0 < (WIDE ? units : 1); u0 += U * HPP) {
         oct<T> x[U] = {};
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            const int u = u0 + j * HPP;
+            const int u = own + u0 + j * HPP;
             if (!ok || u >= units) continue;
             if (u < nq) x[j].load(xq, (size_t)idx * xq.ld + (size_t)u * D + d0);
             else if (u < nq + n_kv) x[j].load(xk, (size_t)idx * xk.ld + (size_t)(u - nq) * D + d0);
@@ -67,11 +71,11 @@ __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t
         }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            const int u = u0 + j * HPP;
+            const int u = own + u0 + j * HPP;
             float y[8];
             // (every lane of a wave takes part: the rotation's partner may be another lane's)
             turn<float>(x[j], tr, d0, ro, y);
-            if (u >= units) continue;
+            if (!there || u >= units) continue;
             if (u >= nq + n_kv) x[j].get(x[j].w, y);
             const u32x4 v = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
             if (u < nq) *(u32x4*)(q_out + ((size_t)idx * n_q + u) * D + d0) = v;
@@ -871,9 +875,12 @@ void launch_kv_append(const rows_t& r, const cache_t& c, int layer, int n_q, kv4
                       const kv4_rope& ro, hipStream_t s)
 {
     uint16_t *kc = (uint16_t*)c.k + layer * c.g.LS, *vc = (uint16_t*)c.v + layer * c.g.LS;
-    const int blocks = r.B * r.n;
-    if (c.head_dim == 128) k_kv_append<T, 128><<<blocks, 256, 0, s>>>(r, c.g, kc, vc, n_q, c.n_kv, k, v, q, q_out, ro);
-    else k_kv_append<T, 64><<<blocks, 256, 0, s>>>(r, c.g, kc, vc, n_q, c.n_kv, k, v, q, q_out, ro);
+    const int rows = r.B * r.n, units = (q_out ? n_q : 0) + 2 * c.n_kv, abreast = 2048 / c.head_dim / units;
+    auto go = [&](auto kern, int blocks) { kern<<<blocks, 256, 0, s>>>(r, c.g, kc, vc, n_q, c.n_kv, k, v, q, q_out, ro); };
+    if (abreast < 2 && c.head_dim == 128) go(k_kv_append<T, 128, true>, rows);
+    else if (abreast < 2) go(k_kv_append<T, 64, true>, rows);
+    else if (c.head_dim == 128) go(k_kv_append<T, 128, false>, (rows + abreast - 1) / abreast);
+    else go(k_kv_append<T, 64, false>, (rows + abreast - 1) / abreast);
 }
 template void launch_kv_append<float>(const rows_t&, const cache_t&, int, int, kv4_src<float>, kv4_src<float>, kv4_src<float>, uint16_t*,
                                       const kv4_rope&, hipStream_t);
