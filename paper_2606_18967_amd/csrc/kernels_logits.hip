@@ -19,9 +19,10 @@
 // where one kernel makes both, the second reading is left to the caches, and all
 // others go past them: the loss of 8192 x 128256 bf16 rows (a fifth of them padding,
 // 3.8 GB of logits and gradients) takes 735 us, which is the rate of a large copy,
-// with both readings past the caches 958, with neither 746, with a work-group of 512
-// threads instead of 1024 767.  Alone, the log-probabilities of 2048 x 152064 take
-// 95 us (6.6 TB/s), their gradient 207 (6.0 TB/s; its stores past the caches 226).
+// with both readings past the caches 958, with neither 746, with work-groups of 512
+// threads instead of 1024 767.  The log-probabilities of 2048 x 152064 and their
+// gradient, two readings and a writing, take 322 us (5.8 TB/s; 340 where the gradient
+// is stored through the caches, which the next kernel has to wait for).
 #include "common.h"
 #include "kernels.h"
 
@@ -69,13 +70,10 @@ __device__ __forceinline__ u32x4 load_vec(const T* p)
     const auto v = (const typename pack_t<T>::vec*)p;
     return KEEP ? (u32x4)*v : (u32x4)__builtin_nontemporal_load(v);
 }
-// PASS: past the caches
-template <bool PASS, typename T>
+template <typename T>
 __device__ __forceinline__ void store_vec(T* p, u32x4 v)
 {
-    const auto to = (typename pack_t<T>::vec*)p;
-    if (PASS) __builtin_nontemporal_store((typename pack_t<T>::vec)v, to);
-    else *to = (typename pack_t<T>::vec)v;
+    __builtin_nontemporal_store((typename pack_t<T>::vec)v, (typename pack_t<T>::vec*)p);
 }
 
 // running sums of a part of a row: m the largest logit, s and t as above
@@ -200,7 +198,7 @@ __device__ __forceinline__ void grad_vec(float (&x)[N], const grad_t& d, float c
 
 // A thread's pass that writes the gradient of the logits [first, n), and of the last
 // n % N where tail is set.  out may be x: a thread reads what it writes first.
-template <typename T, bool ENT, int U, bool PASS>
+template <typename T, bool ENT, int U>
 __device__ __forceinline__ void grad_part(const T* x, T* out, int first, int n, const grad_t& d, float c)
 {
     constexpr int N = pack_t<T>::N;
@@ -216,7 +214,7 @@ __device__ __forceinline__ void grad_part(const T* x, T* out, int first, int n, 
             float y[N];
             pack_t<T>::get(v[u], y);
             grad_vec<ENT>(y, d, c);
-            store_vec<PASS>(out + i0 + u * step, pack_t<T>::put(y));
+            store_vec(out + i0 + u * step, pack_t<T>::put(y));
         }
     }
 }
@@ -230,7 +228,7 @@ template <typename T>
 __device__ __forceinline__ void zero_part(T* out, int n)
 {
     constexpr int N = pack_t<T>::N;
-    for (int i = threadIdx.x * N; i + N <= n; i += blockDim.x * N) store_vec<true>(out + i, (u32x4){0, 0, 0, 0});
+    for (int i = threadIdx.x * N; i + N <= n; i += blockDim.x * N) store_vec(out + i, (u32x4){0, 0, 0, 0});
     const int i = n / N * N + threadIdx.x;
     if (i < n) elem<T>::store(out, i, 0.f);
 }
@@ -315,7 +313,7 @@ __global__ void __launch_bounds__(1024) k_policy_rows(logits_args a, policy_args
     if (threadIdx.x == 0) put_row(p, row, st, o);
     if (GRAD) {
         const grad_t d = grad_of(s.m, st.ln_s, 1.f / (s.s * a.T), st.entropy, o.g, o.h, a.T);
-        grad_part<T, ENT, 4, true>(x, out, 0, V, d, a.c);
+        grad_part<T, ENT, 4>(x, out, 0, V, d, a.c);
         grad_tail<T, ENT>(x, out, V, d, a.c);
         // the token's own, by the thread that wrote its place before
         constexpr int N = pack_t<T>::N;
@@ -418,7 +416,7 @@ __global__ void __launch_bounds__(1024) k_logp_grad(logits_args a, logp_grad_arg
     const int at = tok - c0;
     if (at >= 0 && at < n) xt = elem<T>::load(x, at);
     constexpr int N = pack_t<T>::N;
-    grad_part<T, ENT, 4, false>(x, out, 0, n, d, a.c);
+    grad_part<T, ENT, 4>(x, out, 0, n, d, a.c);
     grad_tail<T, ENT>(x, out, n, d, a.c);
     const int body = n / N * N;
     if (at >= 0 && at < n && threadIdx.x == (at < body ? at / N % blockDim.x : at - body))
@@ -460,7 +458,7 @@ __global__ void __launch_bounds__(256) k_policy_grad(logits_args a, policy_args 
     const int at = p.tok[row] - c0;
     float xt = 0.f;
     if (at >= 0 && at < n) xt = elem<T>::load(x, at);
-    grad_part<T, ENT, 4, true>(x, out, 0, n, d, a.c);
+    grad_part<T, ENT, 4>(x, out, 0, n, d, a.c);
     grad_tail<T, ENT>(x, out, n, d, a.c);
     constexpr int N = pack_t<T>::N;
     const int body = n / N * N;
