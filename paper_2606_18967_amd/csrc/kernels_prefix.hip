@@ -889,9 +889,10 @@ template void launch_kv_append<f32_parts>(const rows_t&, const cache_t&, int, in
 template void launch_kv_append<uint16_t>(const rows_t&, const cache_t&, int, int, kv4_src<uint16_t>, kv4_src<uint16_t>, kv4_src<uint16_t>,
                                          uint16_t*, const kv4_rope&, hipStream_t);
 
-// The plan in the attention itself: where its grid, the target's work-groups, holds every item (there are at most half as
-// many slices, and shares of up to three times the even one).
-bool prefix_plans_itself(const px_plan& p, int B) { return B <= PX_WAVE && 2ll * B * p.zs <= p.target; }
+// The plan in the attention itself: each wave's own takes about 2 us, a kernel before it 5 (8 groups of 8 behind prompts
+// of 2048: 34 us a call instead of 36; one group of 8 behind 512: 15 instead of 17), unless there are many more work-groups
+// than are resident at once.
+bool prefix_plans_itself(const px_plan& p, int B) { return B <= PX_WAVE && (long long)B * p.zs <= p.target; }
 
 // Two work-groups a CU are resident.  A slice may have one chunk more than its share of the target (and one more is what the
 // share, in floats, may be off).
@@ -941,7 +942,7 @@ template <int D>
 static void prefix_attn_d(const rows_t& r, const px_plan& p, const px_groups& g, const cache_t& c, int n_q, const uint16_t* q, long long q_ld, float cs, void* out,
                           act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
 {
-    const dim3 grid(c.n_kv, p.item ? p.max_items : p.target);
+    const dim3 grid(c.n_kv, p.max_items);
     const auto kern = p.item ? k_prefix_attn<D, false> : k_prefix_attn<D, true>;
     const uint16_t *kc = (const uint16_t*)c.k, *vc = (const uint16_t*)c.v;
     if (ev0) hipExtLaunchKernelGGL(kern, grid, dim3(256), 0, s, ev0, ev1, 0, r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, g, out, (int)out_t, out_ld);
