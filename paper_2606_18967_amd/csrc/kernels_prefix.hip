@@ -425,6 +425,12 @@ __device__ __forceinline__ constexpr int v_swizzle(int row) { return D == 128 ? 
 // of each).  Positions that a row does not see may hold anything: there the scores
 // are replaced and values that are not finite taken as zeros; a row that sees such a
 // value is NaN.
+// Few rows are bound by HBM: 8 groups of 8 behind prompts of 2048 (135 MB) take 35 us, 31
+// without the products.  Many are bound by the products, the softmax between them and
+// the tiles' way into LDS nearly alike: 64 sequences behind 32768 positions (202 MB, 35
+// GFLOP) take 65 us, 55 with all tiles from one page, 55 without the products; 8 x 8 verify
+// rows of 5 behind 8192 (32B shape) 125 us, 114 and 105, and 150 once the power limit has
+// lowered the clock.
 // NBLK: the blocks of a tile that a wave takes, 2 with a row tile a wave
 template <int D, int NBLK>
 __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32_t* s_odd, const px_item& it, const px_info& inf, const rows_t& r,
@@ -808,8 +814,9 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, con
     else attend_item<D, 1>(s_buf, s_ml, s_odd, it, inf, r, g, kc, vc, n_q, n_kv, q, q_ld, cs, pl, out, out_t, out_ld);
 }
 
-// The parts of a row joined: a wave a (row, head), D/4 lanes a part, eight parts of each under way at once; a
-// part that saw nothing of the row (l = 0) is not read.
+// The parts of a row joined: a wave a (row, head), D/4 lanes a part, U parts of each under way at once; a
+// part that saw nothing of the row is not read.  Bound by the parts' bytes and, with few, by its launch: 64 rows of 32
+// heads in 32 parts (34 MB) take 8 us, 8 rows of 32 heads in 8 parts 5.
 template <int D>
 __global__ void __launch_bounds__(256) k_prefix_combine(rows_t r, px_plan pl, int n_q, int n_kv, void* out, int out_t, long long out_ld)
 {
@@ -939,18 +946,19 @@ void launch_prefix_plan(const rows_t& r, const px_groups& g, const px_plan& p, i
 }
 
 template <int D>
-static void prefix_attn_d(const rows_t& r, const px_plan& p, const px_groups& g, const cache_t& c, int n_q, const uint16_t* q, long long q_ld, float cs, void* out,
-                          act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
+static void prefix_attn_d(const rows_t& r, const px_plan& p, const px_groups& g, const cache_t& c, int n_q, const uint16_t* q, long long q_ld,
+                          float cs, void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
 {
     const dim3 grid(c.n_kv, p.max_items);
     const auto kern = p.item ? k_prefix_attn<D, false> : k_prefix_attn<D, true>;
     const uint16_t *kc = (const uint16_t*)c.k, *vc = (const uint16_t*)c.v;
-    if (ev0) hipExtLaunchKernelGGL(kern, grid, dim3(256), 0, s, ev0, ev1, 0, r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, g, out, (int)out_t, out_ld);
+    if (ev0)
+        hipExtLaunchKernelGGL(kern, grid, dim3(256), 0, s, ev0, ev1, 0, r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, g, out, (int)out_t, out_ld);
     else kern<<<grid, 256, 0, s>>>(r, c.g, kc, vc, n_q, c.n_kv, q, q_ld, cs, p, g, out, (int)out_t, out_ld);
 }
 
-void launch_prefix_attention(const rows_t& r, px_plan p, const px_groups& g, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld, float scale,
-                             void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
+void launch_prefix_attention(const rows_t& r, px_plan p, const px_groups& g, const cache_t& c, int layer, int n_q, const uint16_t* q, long long q_ld,
+                             float scale, void* out, act_t out_t, long long out_ld, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1)
 {
     p.layer = layer;
     const float cs = scale * 1.4426950408889634f;

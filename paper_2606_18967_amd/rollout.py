@@ -178,9 +178,10 @@ def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: 
 
 
 class Rollout:
-    """One model on the GPU with a dense KV cache (kv4: a paged one in 4 bits; group > 1: a
-    paged one whose groups of so many share their prompt) for B sequences of up to prompt + lmax positions, the drafter buffer, and flat device buffers
-    viewed at the live batch size and draft length of each iteration."""
+    """One model on the GPU with a dense KV cache (kv4: a paged one in 4 bits; group > 1: a paged one whose groups of so
+    many share their prompt) for B sequences of up to prompt + lmax positions, the drafter buffer, and flat device buffers
+    viewed at the live batch size and draft length of each iteration.  logprobs: the responses and their tokens'
+    log-probabilities are kept by slot and place (resp, logp)."""
 
     def __init__(self, cfg: dict, B: int, prompt: int, lmax: int, gmax: int = max(GAMMA_SET), seed: int = 3,
                  T: float = 1.0, fmt: str = "w4", graphs: bool = False, padded: bool | None = None,
