@@ -319,8 +319,10 @@ size_t sd_prefix_workspace_bytes(const sd_kv_cache* c, int32_t B, int32_t n, int
  * positions up to its own, appended before.  groups may be NULL: nothing is shared.
  * B up to 1024.  Scores, the softmax's statistics and all sums are fp32, the
  * probabilities enter the second product in bf16 (2^-8 of each).  The results do
- * not depend on what a row does not see; a key or value that is not finite makes the
- * rows that see it NaN.  A missing page's positions are as if masked. */
+ * not depend on what a row does not see.  A key that is not finite makes the rows
+ * that see it NaN, but for scores of -inf, which are as if masked; a value that is not
+ * finite leaves the row not finite in its dimension, and may make all of it NaN.  A
+ * missing page's positions are as if masked.  At most 6e7 rows of heads (B n n_q). */
 sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_groups* groups, int32_t layer, int32_t B, int32_t n,
                               const int32_t* slots, const int32_t* lens, int32_t n_q, const void* q, int64_t q_ld, float scale,
                               void* out, int64_t out_ld, void* workspace, size_t bytes, void* stream);
@@ -328,7 +330,8 @@ sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_groups* grou
 /* Groups for the engine's own steps over the paged cache (sd_bind_kv_paged): draft,
  * verify and AR step attend through sd_prefix_attention's kernels from here on,
  * with the groups of each call's slots read on the device; prefill is as before.
- * NULL ends it, and so does binding another cache.  Allocates buffers on first use.
+ * NULL ends it, and so does binding another cache; a captured graph keeps the groups
+ * of its capture, whose tensors have to live as long.  Allocates buffers on first use.
  * Errors: SD_E_INVAL, SD_E_STATE (no paged cache bound), SD_E_UNSUPPORTED (an fp32 model,
  * more than 1024 slots), SD_E_NOMEM. */
 sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
@@ -344,7 +347,7 @@ sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
  * otherwise.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then only
  * the loss's stats are written.  workspace: 256-byte aligned, its contents need no
  * preparation, calls whose work may overlap need one each.  Errors: SD_E_INVAL,
- * SD_E_UNSUPPORTED (more than 2^21 rows). */
+ * SD_E_UNSUPPORTED (more than 2^21 rows, a vocabulary of more than 2^30). */
 size_t sd_logits_workspace_bytes(int32_t rows, int32_t vocab);
 
 /* logp[r] = ln p(tokens[r]), entropy[r] = -sum p ln p (may be NULL), norm[r] = (the

@@ -767,7 +767,9 @@ extern "C" sd_status sd_kv_append(const sd_kv_cache* c, int32_t layer, int32_t B
 static sd_status check_prefix_rows(int B, int n, int n_q, int n_kv)
 {
     if (n_q < 1 || n_q % n_kv) return fail(SD_E_INVAL, "n_q=%d must be a positive multiple of n_kv=%d", n_q, n_kv);
-    if (B > PX_SEQS || (double)B * n * n_q > 1e8) return fail(SD_E_UNSUPPORTED, "B=%d, n=%d, n_q=%d are too many for one call", B, n, n_q);
+    // (launches have fewer than 2^32 threads, and 2^16 work-groups along y)
+    if (B > PX_SEQS || (double)B * n * n_q > 6e7 || prefix_plan(B, n, n_q, n_kv).max_items > 65535)
+        return fail(SD_E_UNSUPPORTED, "B=%d, n=%d, n_q=%d are too many for one call", B, n, n_q);
     return SD_OK;
 }
 
@@ -818,8 +820,7 @@ extern "C" sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups)
     if (e->max_slots > PX_SEQS) return fail(SD_E_UNSUPPORTED, "max_slots=%d are more than %d", e->max_slots, PX_SEQS);
     if (e->max_ctx > KV4_MAX_CTX) return fail(SD_E_UNSUPPORTED, "max_ctx=%d is more than %d", e->max_ctx, KV4_MAX_CTX);
     const sd_model_cfg& m = e->c;
-    if ((double)e->max_slots * (e->max_gamma + 1) * m.n_q > 1e8)
-        return fail(SD_E_UNSUPPORTED, "max_slots=%d with drafts of %d are too many", e->max_slots, e->max_gamma);
+    if ((st = check_prefix_rows(e->max_slots, e->max_gamma + 1, m.n_q, m.n_kv)) != SD_OK) return st;
     // the largest call's: its bytes grow with the sequences and with their rows
     const size_t need = prefix_plan_bytes(prefix_plan(e->max_slots, e->max_gamma + 1, m.n_q, m.n_kv), e->max_slots, m.n_kv, m.head_dim);
     const size_t qb = (size_t)e->ws.rows * m.n_q * m.head_dim * 2;
@@ -1292,10 +1293,11 @@ extern "C" sd_status sd_dense_gemm_bf16(const void* A, const void* W, float* C, 
 
 // ------------------------------------------------------------------ logits rows
 constexpr int LOGITS_MAX_ROWS = 1 << 21;     // a launch has fewer than 2^32 threads
+constexpr int LOGITS_MAX_VOCAB = 1 << 30;    // a work-group's steps past a row's end stay below 2^31
 
 extern "C" size_t sd_logits_workspace_bytes(int32_t rows, int32_t vocab)
 {
-    if (rows < 0 || rows > LOGITS_MAX_ROWS || vocab < 1) return 0;
+    if (rows < 0 || rows > LOGITS_MAX_ROWS || vocab < 1 || vocab > LOGITS_MAX_VOCAB) return 0;
     return align256(logits_work_floats(rows, vocab) * 4 + 1);
 }
 
@@ -1305,7 +1307,8 @@ static sd_status check_logits(int dtype, int rows, int vocab, const void* x, int
 {
     if (dtype != SD_DTYPE_F32 && dtype != SD_DTYPE_BF16) return fail(SD_E_INVAL, "dtype must be F32 or BF16");
     if (rows < 0 || vocab < 1) return fail(SD_E_INVAL, "need rows >= 0 and vocab >= 1 (got %d, %d)", rows, vocab);
-    if (rows > LOGITS_MAX_ROWS) return fail(SD_E_UNSUPPORTED, "rows=%d are more than %d", rows, LOGITS_MAX_ROWS);
+    if (rows > LOGITS_MAX_ROWS || vocab > LOGITS_MAX_VOCAB)
+        return fail(SD_E_UNSUPPORTED, "rows=%d or vocab=%d are more than %d, %d", rows, vocab, LOGITS_MAX_ROWS, LOGITS_MAX_VOCAB);
     if (!(T > 0.f) || !isfinite(T) || !isfinite(1.4426950408889634f / T))
         return fail(SD_E_INVAL, "temperature must be finite and > 0, its inverse too");
     if (!rows) return SD_OK;

@@ -263,13 +263,15 @@ __device__ __forceinline__ policy_row policy_of(const policy_args& p, int row, c
         dkl = -em;
     }
     policy_row o;
-    o.term[0] = w * (pg + p.kl_coef * kl - p.entropy_coef * st.entropy);
+    // (e^x may be infinite for a term that the loss does not have)
+    const float klw = p.kl_coef != 0.f ? p.kl_coef * kl : 0.f, dklw = p.kl_coef != 0.f ? p.kl_coef * dkl : 0.f;
+    o.term[0] = w * (pg + klw - p.entropy_coef * st.entropy);
     o.term[1] = w * pg;
     o.term[2] = w * kl;
     o.term[3] = w * st.entropy;
     o.term[4] = clipped ? w : 0.f;
     o.term[5] = 0.f;
-    o.g = w * ((clipped ? 0.f : -free) + p.kl_coef * dkl);
+    o.g = w * ((clipped ? 0.f : -free) + dklw);
     o.h = -p.entropy_coef * w;
     return o;
 }

@@ -327,7 +327,7 @@ class Engine:
 
     def bind_prefix(self, groups: "PrefixGroups | None"):
         """Draft, verify and AR step read what slots of a group share once (paged cache only); None ends it, and so
-        does binding another cache."""
+        does binding another cache.  A captured graph keeps the groups of its capture: keep them as long."""
         if groups is None:
             _check(lib().sd_bind_prefix(self.h, None))
             self._keep_groups = None
@@ -796,7 +796,7 @@ def logits_workspace_bytes(rows: int, vocab: int) -> int:
     """Bytes of the workspace of token_logprobs and policy_loss."""
     nb = int(lib().sd_logits_workspace_bytes(rows, vocab))
     if not nb:
-        raise SDError(SD_E_UNSUPPORTED, f"rows={rows}, vocab={vocab}: need 0 to 2^21 rows and a vocabulary")
+        raise SDError(SD_E_UNSUPPORTED, f"rows={rows}, vocab={vocab}: need 0 to 2^21 rows and a vocabulary of 1 to 2^30")
     return nb
 
 

@@ -203,6 +203,20 @@ def test_policy_without_reference_and_filter(V):
 
 
 @pytest.mark.parametrize("V", [300, 30000])
+def test_a_kl_term_without_a_coefficient_is_not_in_the_loss(V):
+    """Where ref - logp is too large for e^x the KL's own sum is infinite or NaN, and a loss without it is as before."""
+    x, xh = rows(20, V, "f32", 3)
+    t, tok = tokens(20, V, 3, absent=False)
+    v = policy_inputs(xh, t, 1.0, 3, pad=0.0)
+    v["ref"][:] = 100
+    out = run_policy(x, tok, v, 0.0, 0.0, 1.0)
+    assert not np.isfinite(host(out.stats)[2])
+    plain = run_policy(x, tok, {k: a for k, a in v.items() if k != "ref"}, 0.0, 0.0, 1.0)
+    assert np.isfinite(host(plain.stats)).all() and (host(out.stats)[[0, 1, 3, 4, 5]] == host(plain.stats)[[0, 1, 3, 4, 5]]).all()
+    assert torch.equal(out.dlogits, plain.dlogits)
+
+
+@pytest.mark.parametrize("V", [300, 30000])
 def test_policy_absent_rows_are_not_read(V):
     """NaN in the logits and values of absent rows reaches nothing; their gradient is zeros."""
     R = 16

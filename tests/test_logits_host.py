@@ -19,8 +19,18 @@ def test_workspace_bytes():
     f = sdrl.lib().sd_logits_workspace_bytes
     assert f(0, 5) > 0 and f(8, 512) > 0 and f(64, 152064) % 256 == 0
     assert f(-1, 5) == 0 and f(4, 0) == 0 and f((1 << 21) + 1, 5) == 0
+    assert f(1, 1 << 30) > 0 and f(1, (1 << 30) + 1) == 0
     with pytest.raises(sdrl.SDError):
         sdrl.logits_workspace_bytes(-1, 5)
+
+
+def test_vocabularies_past_the_kernels_steps_are_refused():
+    V = (1 << 30) + 1                                  # a step past the end of a longer row could pass 2^31
+    L, c = sdrl.lib(), sdrl.PolicyCfg(1.0, 0.2, 0.2, 0.0, 0.0, 0.5, 2.0, 0)
+    assert L.sd_token_logprobs(0, 1, V, PTR, V, PTR, 1.0, PTR, None, None, PTR, 1 << 40, None) == UNSUPPORTED
+    assert L.sd_token_logprobs_grad(0, 1, V, PTR, V, PTR, 1.0, PTR, PTR, None, None, PTR, V, None) == UNSUPPORTED
+    assert L.sd_policy_loss(C.byref(c), 0, 1, V, PTR, V, PTR, PTR, None, None, PTR, PTR, PTR, PTR, None, None, 0, PTR, 1 << 40,
+                            None) == UNSUPPORTED
 
 
 COMMON = [dict(dtype=2), dict(rows=-1), dict(V=0), dict(x=None), dict(x=PTR + 2), dict(dtype=1, x=PTR + 1), dict(ld=99), dict(ld=1 << 31),

@@ -67,6 +67,16 @@ def test_attention_is_checked():
     assert L.sd_prefix_attention(C.byref(many), None, 0, 1025, 1, PTR, None, 4, PTR, 512, 1.0, PTR, 512, PTR, 1 << 40, None) == UNSUPPORTED
 
 
+def test_calls_past_a_launch_are_refused():
+    L, c = sdrl.lib(), cache(max_slots=64, max_ctx=1 << 21, pages_per_seq=1 << 15)
+    # 2^20 rows of 8 heads a KV head are 2^16 slices; 7 x 2^20 x 16 rows of heads more than a launch has waves for
+    for B, n, n_q in ((1, 1 << 20, 16), (7, 1 << 20, 16), (64, 1 << 19, 2)):
+        assert L.sd_prefix_workspace_bytes(C.byref(c), B, n, n_q) == 0
+        assert L.sd_prefix_attention(C.byref(c), None, 0, B, n, PTR, None, n_q, PTR, 128 * n_q, 1.0, PTR, 128 * n_q, PTR, 1 << 50,
+                                     None) == UNSUPPORTED
+    assert L.sd_prefix_workspace_bytes(C.byref(c), 1, 1 << 19, 16) > 0
+
+
 def test_python_objects_are_checked():
     k = torch.zeros((4, 1, 2, 32, 64), dtype=torch.bfloat16)
     t, n = torch.zeros((2, 2), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
