@@ -171,7 +171,9 @@ __device__ __forceinline__ int own_tiles(const px_info& i, int P) { return i.ctx
 // of a run are cut at the same tiles, so that the shared ones, which they read at about the same time, come once
 // from memory.
 struct chunks { int n, len; };
-constexpr int PX_SHARE = 1 << 24;                                  // the longest share: the tiles of 64 sequences of 2^24 positions
+// the shortest share (in tiles: one group of 8 behind 512 takes 14.2 us a call, with 1 15.1, with 3 15.1, with 4 16.4) and
+// the longest, the tiles of 64 sequences of 2^24 positions
+constexpr int PX_SHARE_MIN = 2, PX_SHARE_MAX = 1 << 24;
 __device__ __forceinline__ chunks chunks_of(int tiles, int share, bool any)
 {
     if (!any) return {0, 0};
@@ -221,7 +223,7 @@ __device__ wave_plan plan_of_wave(const rows_t& r, const px_groups& gr, const px
     // the shortest share of a few that makes at most `target` items, which are then resident at once
     const bool leads = mine && lane == p.sfirst;
     const float w = wave_total(leads ? (float)p.tiles * pl.zs : 0.f);
-    const int even = (int)fminf(fmaxf(ceilf(w / (float)pl.target), 1.f), (float)PX_SHARE);
+    const int even = (int)fminf(fmaxf(ceilf(w / (float)pl.target), (float)PX_SHARE_MIN), (float)PX_SHARE_MAX);
     int share = even;
     for (int k = 0; k < 8; ++k) {
         const int s = cdiv(even * (k < 5 ? 8 + k : 4 * k - 4), 8);     // 1, 9/8, .. 3/2, 2, 5/2, 3
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px
         atomicAdd(&s_work, (unsigned long long)tiles * pl.zs);
     }
     __syncthreads();
-    const int share = (int)min(max((s_work + pl.target - 1) / pl.target, 1ull), (unsigned long long)PX_SHARE);
+    const int share = (int)min(max((s_work + pl.target - 1) / pl.target, (unsigned long long)PX_SHARE_MIN), (unsigned long long)PX_SHARE_MAX);
     const chunks c = leads ? chunks_of(tiles, share, any) : chunks{0, 0};
     s_iend[t] = scan1024(c.n * pl.zs, sh);
     const int parts = c.n > 1 ? c.n * (send - sfirst) * RG : 0;
@@ -624,8 +626,8 @@ __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32
         m = m == -INFINITY ? bm : m;                               // nothing seen so far: nothing to rescale
         const bool need = bm > m + 8.f;
         if (__builtin_amdgcn_ballot_w64(need)) {
-            const float mn = need ? bm : m, corr = __builtin_amdgcn_exp2f(m - mn);
-            m = mn;
+            const float corr = need ? __builtin_amdgcn_exp2f(m - bm) : 1.f;   // (a row that saw nothing yet has m = -inf)
+            m = need ? bm : m;
             l *= corr;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)

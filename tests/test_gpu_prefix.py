@@ -126,6 +126,17 @@ def test_peaked_scores():
     x.check(x.run())
 
 
+@pytest.mark.parametrize("n_q,n_kv,D,sizes,n", [(64, 64, 64, [20], 1), (64, 32, 128, [40], 2), (256, 32, 64, [20], 1), (64, 64, 128, [1, 1, 7], 3),
+                                                (128, 128, 64, [70], 1)])
+@pytest.mark.parametrize("peak", [1, 8])
+def test_chunks_over_several_sequences(n_q, n_kv, D, sizes, n, peak):
+    """Many KV heads leave a head few work-groups: each walks the tiles of several sequences, whose rows have their first
+    position and their references' moves at different tiles."""
+    x = Batch(n_q, n_kv, D, sizes, [200] * len(sizes), own_lengths(sizes, 330, 5), n)
+    x.q *= peak
+    x.check(x.run(), seqs=range(0, sum(sizes), 3))
+
+
 def test_scores_that_rise():
     """Keys that grow with the position, so that the reference moves in every tile."""
     x = Batch(4, 2, 64, [3], [640], [10, 20, 30], 1)
