@@ -137,6 +137,48 @@ def test_chunks_over_several_sequences(n_q, n_kv, D, sizes, n, peak):
     x.check(x.run(), seqs=range(0, sum(sizes), 3))
 
 
+CHUNKS = [(64, 64, 64, 1), (256, 32, 128, 3), (64, 64, 128, 12)]     # few and many rows of a slice
+
+
+@pytest.mark.parametrize("n_q,n_kv,D,n", CHUNKS)
+@pytest.mark.parametrize("which,bad", [("k", float("nan")), ("k", float("inf")), ("v", float("nan")), ("v", -float("inf"))])
+@pytest.mark.parametrize("tail", [70, 150])
+def test_chunks_whose_values_are_not_finite(n_q, n_kv, D, n, which, bad, tail):
+    """A key or value of sequence 1 behind its prompt, in a tile that all of its rows see or some: the others' are as before."""
+    x = Batch(n_q, n_kv, D, [7], [200], [170, tail, 0, 300, 64, 5, 130], n)
+    x.q *= 4
+    p, pool, G = 200 + 65, x.k if which == "k" else x.v, n_q // n_kv
+    pool[int(x.table[int(x.slots_h[1]), p // x.page]), x.layer, 0, p % x.page, 5] = bad
+    out = x.run()
+    x.check(out, seqs=[0, 2, 3, 4, 5, 6])
+    o, tol = x.expected(1)
+    assert bool(((out[1].double() - o).abs() <= tol)[:, G:].all())
+    if which == "v":
+        assert not torch.isfinite(out[1, :, :G, 5]).any()
+    elif bad != bad:
+        assert torch.isnan(out[1, :, :G]).all()
+
+
+@pytest.mark.parametrize("n_q,n_kv,D,n", CHUNKS)
+def test_chunks_with_missing_pages(n_q, n_kv, D, n):
+    x = Batch(n_q, n_kv, D, [7], [200], [170, 150, 0, 300, 64, 5, 130], n)
+    x.q *= 4
+    for b, lp in ((0, 4), (3, 7), (6, 3)):
+        x.table[int(x.slots_h[b]), lp] = -1
+        keep = torch.ones(len(x.K[b]), dtype=torch.bool, device="cuda")
+        keep[64 * lp:64 * lp + 64] = False
+        x.base[b] -= int((~keep)[:x.base[b] + 1].sum())            # (sequence 3's is its last page, rows and all)
+        x.K[b], x.V[b] = x.K[b][keep], x.V[b][keep]
+    x.check(x.run())
+
+
+@pytest.mark.parametrize("n_q,n_kv,D,n", CHUNKS)
+def test_chunks_with_ragged_rows(n_q, n_kv, D, n):
+    x = Batch(n_q, n_kv, D, [5, 4], [200, 90], [170, 150, 0, 300, 64, 5, 130, 61, 63], n, lens=[n, 0, 1, n, 0, n, 0, 1, n - 1])
+    x.q *= 4
+    x.check(x.run())
+
+
 def test_scores_that_rise():
     """Keys that grow with the position, so that the reference moves in every tile."""
     x = Batch(4, 2, 64, [3], [640], [10, 20, 30], 1)
