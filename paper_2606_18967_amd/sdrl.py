@@ -813,8 +813,11 @@ def _logit_rows(t, name: str, shape=None, dtype=None, dev=None):
             raise ValueError(f"{name}: on {t.device}, expected {dev}")
     elif t.device.index != torch.cuda.current_device():
         raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    V, st, ld = t.shape[-1], t.stride(), None
-    rows = 1
+    dt = SD_DTYPE_BF16 if t.dtype == torch.bfloat16 else SD_DTYPE_F32
+    V = t.shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), V, dt
+    st, ld, rows = t.stride(), None, 1
     for size, stride in zip(reversed(t.shape[:-1]), reversed(st[:-1])):
         if size == 1:
             continue
@@ -826,7 +829,7 @@ def _logit_rows(t, name: str, shape=None, dtype=None, dev=None):
     ld = V if ld is None or not rows else ld
     if (V > 1 and st[-1] != 1) or ld < V:
         raise ValueError(f"{name}: rows must be contiguous and not overlap, got strides {st}")
-    return t.data_ptr(), ld, SD_DTYPE_BF16 if t.dtype == torch.bfloat16 else SD_DTYPE_F32
+    return t.data_ptr(), ld, dt
 
 
 def _rows_workspace(workspace, rows, V, dev):
@@ -845,7 +848,8 @@ def token_logprobs(logits, tokens, T: float = 1.0, workspace=None):
     dev, V, shape, rows = logits.device, logits.shape[-1], logits.shape[:-1], tokens.numel()
     tp = _ptr(tokens, "tokens", torch.int32, shape, dev)
     workspace, wp, nb = _rows_workspace(workspace, rows, V, dev)     # (held until the call is enqueued)
-    logp, entropy, norm = (torch.empty(s, dtype=torch.float32, device=dev) for s in (shape, shape, (*shape, 2)))
+    logp = torch.empty(shape, dtype=torch.float32, device=dev)
+    entropy, norm = torch.empty_like(logp), logp.new_empty((*shape, 2))
     _check(lib().sd_token_logprobs(dt, rows, V, xp, ld, tp, T, logp.data_ptr(), entropy.data_ptr(), norm.data_ptr(), wp, nb,
                                    _stream()))
     return logp, entropy, norm
@@ -905,7 +909,7 @@ def policy_loss(cfg: PolicyLoss, logits, tokens, old_logp, advantage, weight, re
     f32 = lambda t, name: None if t is None else _ptr(t, name, torch.float32, shape, dev)
     workspace, wp, nb = _rows_workspace(workspace, rows, V, dev)     # (held until the call is enqueued)
     olp, ap, wt = (_ptr(t, name, torch.float32, shape, dev) for t, name in ((old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight")))
-    stats = torch.empty(6, dtype=torch.float32, device=dev)
+    stats = old_logp.new_empty(6)
     logp, entropy = torch.empty_like(old_logp), torch.empty_like(old_logp)
     _check(lib().sd_policy_loss(cfg._ref, dt, rows, V, xp, ld, tp, olp, f32(behavior_logp, "behavior_logp"),
                                 f32(ref_logp, "ref_logp"), ap, wt, stats.data_ptr(),
