@@ -97,7 +97,10 @@ __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t
 // the tiles of all), so that the work-groups are alike and resident at once, however
 // the batch divides between shared and own positions: with items of their own for the
 // sequences' tails, 8 groups of 8 behind prompts of 2048 (responses of up to 512) took
-// 42 us instead of 35, for a tail's item was 4 us of tiles and 8 of start and end.
+// 42 us instead of 35, for a tail's item was 4 us of tiles and 8 of start and end.  All
+// tiles count alike: an own tile of a wide slice is a wave's work, but comes from memory
+// for this slice alone (counted as 2/3 of a shared one, 64 sequences behind 32768 took
+// 77 us a call instead of 68, as 5/4 72).
 
 // inclusive sum over the 1024 threads of a work-group; sh: 16 ints
 __device__ __forceinline__ int scan1024(int v, int* sh)

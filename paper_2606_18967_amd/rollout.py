@@ -188,6 +188,8 @@ class Rollout:
                  prefill: bool = False, kv4: bool = False, group: int = 1, logprobs: bool = False):
         import torch
         self.torch = torch
+        if group < 1 or B % group:
+            raise ValueError(f"B={B} responses are not whole groups of {group}")
         if group > 1 and kv4:
             raise ValueError("groups share the pages of a cache of the model's type, not of the 4-bit one")
         self.group, self.logprobs = group, logprobs

@@ -35,3 +35,9 @@ def test_decode_of_groups_prices_a_prompt_once():
     with mock.patch.object(rollout.sdrl, "toggle", fake_toggle):
         rollout.decode(np.array([1, 2, 3, 3]), 100, "toggle", 5, 5.0, None, 0.05, ar, None, compact, group=2)
     assert seen == [(4, 50.0), (3, 100 * 2 / 3 + 1.0), (2, 50.0 + 2.0)]
+
+
+@pytest.mark.parametrize("B,group", [(6, 0), (6, 4), (2, 3), (6, -1)])
+def test_batches_are_whole_groups(B, group):
+    with pytest.raises(ValueError, match="whole groups"):
+        rollout.Rollout({}, B, 100, 20, group=group)
