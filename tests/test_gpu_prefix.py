@@ -71,6 +71,17 @@ def test_batch_orders():
         x.check(x.run())
 
 
+def test_a_slot_twice():
+    """Two blocks of rows of one sequence, side by side and apart."""
+    for order in ([0, 1, 2, 3], [0, 2, 1, 3]):
+        x = Batch(8, 2, 128, [4], [300], [10, 70, 130, 30], 2, order=order)
+        a, b = order.index(0), order.index(1)
+        x.slots[b] = x.slots[a]
+        x.K[b], x.V[b], x.base[b] = x.K[a], x.V[a], x.base[a]
+        x.check(x.run())
+        x.cache.check()
+
+
 def test_lengths_that_groups_do_not_have():
     """len past the shortest cache, 0 and negative; groups out of range."""
     sizes = [3, 3]
