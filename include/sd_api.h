@@ -345,8 +345,9 @@ sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
  * or no finite logit gives NaN.  Gradients have logits' type, are rounded once,
  * and are written whole; dlogits may be logits itself (same stride), but not overlap it
  * otherwise.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then only
- * the loss's stats are written.  workspace: 256-byte aligned, its contents need no
- * preparation, calls whose work may overlap need one each.  Errors: SD_E_INVAL,
+ * the loss's stats are written.  workspace: 256-byte aligned, as large as for this
+ * many rows or more, its contents need no preparation, calls whose work may overlap
+ * need one each.  Errors: SD_E_INVAL,
  * SD_E_UNSUPPORTED (more than 2^21 rows, a vocabulary of more than 2^30). */
 size_t sd_logits_workspace_bytes(int32_t rows, int32_t vocab);
 

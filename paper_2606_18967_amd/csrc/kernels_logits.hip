@@ -544,11 +544,11 @@ static int row_splits(int rows, int V, int* chunk)
     return (V + *chunk - 1) / *chunk;
 }
 
+// for up to so many rows: r < 512 of them have at most 1024 + r - 1 parts
 size_t logits_work_floats(int rows, int V)
 {
-    int chunk;
-    const size_t S = row_splits(rows, V, &chunk);
-    return (size_t)rows * (POLICY_TERMS + (S > 1 ? 3 * S + 4 : 0));
+    const size_t split = V <= 16384 ? 0 : rows < 512 ? rows : 511;
+    return (size_t)rows * POLICY_TERMS + (split ? 3 * (1024 + split) + 4 * split : 0);
 }
 
 void launch_token_logprobs(logits_args a, const logp_args& p, int rows, bool f32, float* work, hipStream_t s)

@@ -793,7 +793,7 @@ def prefix_attention(cache: KVPages, groups: PrefixGroups | None, layer: int, sl
 # ------------------------------------------------- logits rows: log-probabilities, policy loss
 @functools.lru_cache(maxsize=64)
 def logits_workspace_bytes(rows: int, vocab: int) -> int:
-    """Bytes of the workspace of token_logprobs and policy_loss."""
+    """Bytes of the workspace of token_logprobs and policy_loss, for up to so many rows."""
     nb = int(lib().sd_logits_workspace_bytes(rows, vocab))
     if not nb:
         raise SDError(SD_E_UNSUPPORTED, f"rows={rows}, vocab={vocab}: need 0 to 2^21 rows and a vocabulary of 1 to 2^30")

@@ -216,6 +216,18 @@ def test_a_kl_term_without_a_coefficient_is_not_in_the_loss(V):
     assert torch.equal(out.dlogits, plain.dlogits)
 
 
+@pytest.mark.parametrize("R", [1, 2, 3, 31, 64, 300, 511, 512])
+def test_a_workspace_of_more_rows(R):
+    V = 128256 if R < 100 else 33000
+    x, xh = rows(R, V, "bf16", R)
+    t, tok = tokens(R, V, R)
+    v = policy_inputs(xh, t, 1.0, R)
+    ws = torch.full((sdrl.logits_workspace_bytes(600, V) + 256,), 0xff, dtype=torch.uint8, device="cuda")
+    check_stats(xh, t, 1.0, *sdrl.token_logprobs(x, tok, workspace=ws[:-256]))
+    check_policy(xh, t, v, 0.05, 0.01, 1.0, run_policy(x, tok, v, 0.05, 0.01, 1.0, workspace=ws[:-256]), "bf16")
+    assert (ws[-256:] == 0xff).all()
+
+
 @pytest.mark.parametrize("V", [300, 30000])
 def test_policy_absent_rows_are_not_read(V):
     """NaN in the logits and values of absent rows reaches nothing; their gradient is zeros."""

@@ -24,6 +24,13 @@ def test_workspace_bytes():
         sdrl.logits_workspace_bytes(-1, 5)
 
 
+@pytest.mark.parametrize("V", [1, 512, 16384, 16385, 50257, 128256, 1 << 30])
+def test_a_workspace_serves_fewer_rows_too(V):
+    f = sdrl.lib().sd_logits_workspace_bytes
+    b = [f(r, V) for r in range(1100)]
+    assert b == sorted(b)
+
+
 def test_vocabularies_past_the_kernels_steps_are_refused():
     V = (1 << 30) + 1                                  # a step past the end of a longer row could pass 2^31
     L, c = sdrl.lib(), sdrl.PolicyCfg(1.0, 0.2, 0.2, 0.0, 0.0, 0.5, 2.0, 0)
