@@ -335,3 +335,30 @@ def test_same_bits_again(R, V):
     v = policy_inputs(xh, t, 1.0, 4)
     a, b = run_policy(x, tok, v, 0.1, 0.01, 1.0), run_policy(x, tok, v, 0.1, 0.01, 1.0)
     assert torch.equal(a.stats, b.stats) and torch.equal(a.dlogits, b.dlogits) and torch.equal(a.logp, b.logp)
+
+
+def test_offsets_past_32_bits():
+    """Rows that end past 2^31 elements: the first, those around the border and the last, in place."""
+    R, V = 16800, 128256
+    assert R * V > 1 << 31
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("not enough memory")
+    x = torch.zeros((R, V), dtype=torch.bfloat16, device="cuda")
+    at = [0, (1 << 31) // V - 1, (1 << 31) // V, R - 1]
+    small, xh = rows(len(at), V, "bf16", 11)
+    t, tok4 = tokens(len(at), V, 11, absent=False)
+    x[at] = small
+    tok = torch.full((R,), -1, dtype=torch.int32, device="cuda")
+    tok[at] = tok4
+    logp, entropy, norm = sdrl.token_logprobs(x, tok)
+    check_stats(xh, t, 1.0, logp[at], entropy[at], norm[at])
+    v = policy_inputs(xh, t, 1.0, 11, pad=0.0)
+    full = {}
+    for k, a in v.items():
+        full[k] = np.zeros(R, np.float32)
+        full[k][at] = a
+    out = run_policy(x, tok, full, 0.05, 0.01, 1.0, dlogits=x)
+    wrote = (x != 0).any(1)
+    wrote[at] = False                                             # (of these the filter may have dropped one)
+    assert out.dlogits is x and not wrote.any()
+    check_policy(xh, t, v, 0.05, 0.01, 1.0, sdrl.PolicyOut(out.stats, out.logp[at], out.entropy[at], x[at]), "bf16")

@@ -86,3 +86,10 @@ def test_python_objects_are_checked():
     for g, ln in ((t, n), (n, t), (n, n[:0]), (n, n)):
         with pytest.raises(ValueError):
             sdrl.PrefixGroups(g, ln)
+
+
+def test_a_workspace_serves_smaller_calls_too():
+    L, c = sdrl.lib(), cache(max_slots=1024, max_ctx=4096, pages_per_seq=64, n_kv=8)
+    f = lambda B, n: L.sd_prefix_workspace_bytes(C.byref(c), B, n, 32)  # noqa: E731
+    for sizes in ([f(B, 5) for B in range(1, 1025)], [f(64, n) for n in range(1, 300)]):
+        assert sizes[0] > 0 and sizes == sorted(sizes)
