@@ -177,6 +177,11 @@ struct chunks { int n, len; };
 // the shortest share (in tiles: one group of 8 behind 512 takes 14.2 us a call, with 1 15.1, with 3 15.1, with 4 16.4) and
 // the longest, the tiles of 64 sequences of 2^24 positions
 constexpr int PX_SHARE_MIN = 2, PX_SHARE_MAX = 1 << 24;
+// The share is the shortest of a few that makes at most `target` items, which are then resident at once: the even one
+// times 1, 9/8, .. 3/2, 2, 5/2, 3.  (8 x 8 verify rows of 5 behind 8192, two slices of 178 and 158 tiles a group and KV
+// head: 135 us a call, with the even one 158; 16 x 8 behind 4096 177 and 209.)
+constexpr int PX_TRIES = 8;
+__device__ __forceinline__ int share_of(int even, int k) { return cdiv(even * (k < 5 ? 8 + k : 4 * k - 4), 8); }
 __device__ __forceinline__ chunks chunks_of(int tiles, int share, bool any)
 {
     if (!any) return {0, 0};
@@ -223,13 +228,12 @@ __device__ wave_plan plan_of_wave(const rows_t& r, const px_groups& gr, const px
     const uint64_t slice = (~0ull >> (64 - max(p.send, 1))) & (~0ull << p.sfirst);
     const bool any = (__builtin_amdgcn_ballot_w64(m.info.nlive > 0) & slice) != 0, sees = (__builtin_amdgcn_ballot_w64(live) & slice) != 0;
     p.tiles = sees ? p.P + own_end - (p.sfirst ? own_start : 0) : 0;
-    // the shortest share of a few that makes at most `target` items, which are then resident at once
     const bool leads = mine && lane == p.sfirst;
     const float w = wave_total(leads ? (float)p.tiles * pl.zs : 0.f);
     const int even = (int)fminf(fmaxf(ceilf(w / (float)pl.target), (float)PX_SHARE_MIN), (float)PX_SHARE_MAX);
     int share = even;
-    for (int k = 0; k < 8; ++k) {
-        const int s = cdiv(even * (k < 5 ? 8 + k : 4 * k - 4), 8);     // 1, 9/8, .. 3/2, 2, 5/2, 3
+    for (int k = 0; k < PX_TRIES; ++k) {
+        const int s = share_of(even, k);
         const float rs = 1.f / (float)s;
         if (wave_total(leads && any ? fmaxf(ceilf((float)p.tiles * rs), 1.f) * pl.zs : 0.f) <= (float)pl.target) {
             share = s;
@@ -305,6 +309,7 @@ __global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px
     __shared__ int s_gid[PX_SEQS], s_first[PX_SEQS + 1], s_low[PX_SEQS], s_reader[PX_SEQS], s_alive[PX_SEQS];   // of runs, but the first
     __shared__ int s_own[PX_SEQS], s_any[PX_SEQS], s_send[PX_SEQS], s_iend[PX_SEQS], s_part[PX_SEQS], s_tiles[PX_SEQS], s_nc[PX_SEQS], s_len[PX_SEQS];
     __shared__ unsigned long long s_work;
+    __shared__ int s_items[PX_TRIES];
     __shared__ int sh[16];
     const int t = threadIdx.x;
     const bool mine = t < r.B;
@@ -318,6 +323,7 @@ __global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px
     s_low[t] = s_reader[t] = INT_MAX;
     s_alive[t] = 0;
     if (t == 0) s_work = 0;
+    if (t < PX_TRIES) s_items[t] = 0;
     __syncthreads();
     const bool lead = mine && (t == 0 || m.gid < 0 || m.gid != s_gid[t - 1]);
     const int run = max(scan1024(lead ? 1 : 0, sh) - 1, 0);
@@ -346,7 +352,13 @@ __global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px
         atomicAdd(&s_work, (unsigned long long)tiles * pl.zs);
     }
     __syncthreads();
-    const int share = (int)min(max((s_work + pl.target - 1) / pl.target, (unsigned long long)PX_SHARE_MIN), (unsigned long long)PX_SHARE_MAX);
+    const int even = (int)min(max((s_work + pl.target - 1) / pl.target, (unsigned long long)PX_SHARE_MIN), (unsigned long long)PX_SHARE_MAX);
+    if (leads && any)
+        for (int k = 0; k < PX_TRIES; ++k) atomicAdd(&s_items[k], max(cdiv(tiles, share_of(even, k)), 1) * pl.zs);
+    __syncthreads();
+    int share = even;
+    for (int k = PX_TRIES - 1; k >= 0; --k)
+        if (s_items[k] <= pl.target) share = share_of(even, k);
     const chunks c = leads ? chunks_of(tiles, share, any) : chunks{0, 0};
     s_iend[t] = scan1024(c.n * pl.zs, sh);
     const int parts = c.n > 1 ? c.n * (send - sfirst) * RG : 0;
