@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t
 }
 
 // ------------------------------------------------------------------ plan
+constexpr int PX_JOIN = 1;
 // How a call is cut into work-groups.  Sequences of one group that follow one another
 // are a run; what a run shares, min(len, the shortest kv_len in it), is rounded
 // down to whole tiles of PX_TILE positions.  Sequences of a run whose rows fit PX_ROWS
@@ -170,6 +171,9 @@ __device__ __forceinline__ member member_of(const rows_t& r, const px_groups& gr
 // tiles of a sequence's own behind P shared tiles
 __device__ __forceinline__ int own_tiles(const px_info& i, int P) { return i.ctx ? cdiv(i.ctx - P * PX_TILE, PX_TILE) : 0; }
 
+// sequences of a slice: alone where they share too little
+__device__ __forceinline__ int slice_of(const px_plan& pl, int P) { return P >= PX_JOIN ? pl.sps : 1; }
+
 // A slice's chunks: of `tiles` tiles in shares of `share` (rows without a tile: one chunk, which writes zeros).  Slices
 // of a run are cut at the same tiles, so that the shared ones, which they read at about the same time, come once
 // from memory.
@@ -221,8 +225,9 @@ __device__ wave_plan plan_of_wave(const rows_t& r, const px_groups& gr, const px
     if (m.gid >= 0 && (alive & (alive - 1))) p.P = max(min(m.len, low), 0) / PX_TILE;
     p.reader = __shfl(m.info.slot, alive ? __builtin_ctzll(alive) : 0, WAVE);
     // slices
-    p.sfirst = first + (lane - first) / pl.sps * pl.sps;
-    p.send = min(p.sfirst + pl.sps, end);
+    const int per = slice_of(pl, p.P);
+    p.sfirst = first + (lane - first) / per * per;
+    p.send = min(p.sfirst + per, end);
     const int own = own_tiles(m.info, p.P), upto_own = wave_scan(own);
     const int own_end = __shfl(upto_own, p.send - 1, WAVE), own_start = __shfl(upto_own, max(p.sfirst - 1, 0), WAVE);
     const uint64_t slice = (~0ull >> (64 - max(p.send, 1))) & (~0ull << p.sfirst);
@@ -337,7 +342,7 @@ __global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px
     __syncthreads();
     const int first = s_first[run], end = s_first[run + 1];
     const int P = m.gid >= 0 && s_alive[run] > 1 ? max(min(m.len, s_low[run]), 0) / PX_TILE : 0;
-    const int sfirst = first + (t - first) / pl.sps * pl.sps, send = min(sfirst + pl.sps, end);
+    const int per = slice_of(pl, P), sfirst = first + (t - first) / per * per, send = min(sfirst + per, end);
     s_own[t] = scan1024(own_tiles(m.info, P), sh);
     s_any[t] = scan1024((m.info.nlive > 0 ? 1 << 16 : 0) + (live ? 1 : 0), sh);
     s_send[t] = send;
