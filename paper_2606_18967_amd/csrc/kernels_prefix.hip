@@ -88,7 +88,6 @@ __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t
 }
 
 // ------------------------------------------------------------------ plan
-constexpr int PX_JOIN = 1;
 // How a call is cut into work-groups.  Sequences of one group that follow one another
 // are a run; what a run shares, min(len, the shortest kv_len in it), is rounded
 // down to whole tiles of PX_TILE positions.  Sequences of a run whose rows fit PX_ROWS
@@ -171,8 +170,16 @@ __device__ __forceinline__ member member_of(const rows_t& r, const px_groups& gr
 // tiles of a sequence's own behind P shared tiles
 __device__ __forceinline__ int own_tiles(const px_info& i, int P) { return i.ctx ? cdiv(i.ctx - P * PX_TILE, PX_TILE) : 0; }
 
-// sequences of a slice: alone where they share too little
-__device__ __forceinline__ int slice_of(const px_plan& pl, int P) { return P >= PX_JOIN ? pl.sps : 1; }
+// Sequences of a slice of a run of so many: alone where they share little for their rows.  A tile of few rows takes a third
+// of the time of one of 128, and many slices fill the card better; what counts against them is that every slice reads
+// the shared tiles.  (8 x 8 behind 256, own up to 300, 5 rows of 5 heads: alone 23 us a call, joined 30; behind 1024 36 and 37,
+// behind 2048 53 and 46.  One row of 4 heads, own up to 30: behind 64 alone 15.5 and joined 15.3, behind 128 16.3 and 14.8.
+// 3 rows of 4 heads, own up to 40: behind 256 18.3 and 18.3, behind 512 22.6 and 20.5.)
+__device__ __forceinline__ int slice_of(const px_plan& pl, int RG, int P, int run)
+{
+    const int rows = min(pl.sps, run) * RG;
+    return P >= max(RG / 2, rows > PX_ROWS / 2 ? 6 : 2) ? pl.sps : 1;
+}
 
 // A slice's chunks: of `tiles` tiles in shares of `share` (rows without a tile: one chunk, which writes zeros).  Slices
 // of a run are cut at the same tiles, so that the shared ones, which they read at about the same time, come once
@@ -225,7 +232,7 @@ __device__ wave_plan plan_of_wave(const rows_t& r, const px_groups& gr, const px
     if (m.gid >= 0 && (alive & (alive - 1))) p.P = max(min(m.len, low), 0) / PX_TILE;
     p.reader = __shfl(m.info.slot, alive ? __builtin_ctzll(alive) : 0, WAVE);
     // slices
-    const int per = slice_of(pl, p.P);
+    const int per = slice_of(pl, RG, p.P, end - first);
     p.sfirst = first + (lane - first) / per * per;
     p.send = min(p.sfirst + per, end);
     const int own = own_tiles(m.info, p.P), upto_own = wave_scan(own);
@@ -342,7 +349,7 @@ __global__ void __launch_bounds__(1024) k_prefix_plan(rows_t r, px_groups gr, px
     __syncthreads();
     const int first = s_first[run], end = s_first[run + 1];
     const int P = m.gid >= 0 && s_alive[run] > 1 ? max(min(m.len, s_low[run]), 0) / PX_TILE : 0;
-    const int per = slice_of(pl, P), sfirst = first + (t - first) / per * per, send = min(sfirst + per, end);
+    const int per = slice_of(pl, RG, P, end - first), sfirst = first + (t - first) / per * per, send = min(sfirst + per, end);
     s_own[t] = scan1024(own_tiles(m.info, P), sh);
     s_any[t] = scan1024((m.info.nlive > 0 ? 1 << 16 : 0) + (live ? 1 : 0), sh);
     s_send[t] = send;

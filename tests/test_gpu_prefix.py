@@ -37,8 +37,9 @@ def test_prefix_lengths(prefix, page):
 @pytest.mark.parametrize("sizes", [[1], [2], [1, 1, 1], [33], [64], [17, 40], [2] * 30])
 @pytest.mark.parametrize("n", [1, 3])
 def test_group_sizes(sizes, n):
-    x = Batch(8, 2, 128, sizes, [300] * len(sizes), own_lengths(sizes, 90, 1), n, seed=len(sizes))
-    x.check(x.run())
+    for prefix in (300, 800):
+        x = Batch(8, 2, 128, sizes, [prefix] * len(sizes), own_lengths(sizes, 90, 1), n, seed=len(sizes))
+        x.check(x.run())
 
 
 @pytest.mark.parametrize("n_q,n_kv,D", [(32, 8, 128), (8, 2, 64)])
@@ -140,25 +141,28 @@ def test_peaked_scores():
 @pytest.mark.parametrize("n_q,n_kv,D,sizes,n", [(64, 64, 64, [20], 1), (64, 32, 128, [40], 2), (256, 32, 64, [20], 1), (64, 64, 128, [1, 1, 7], 3),
                                                 (128, 128, 64, [70], 1)])
 @pytest.mark.parametrize("peak", [1, 8])
-def test_chunks_over_several_sequences(n_q, n_kv, D, sizes, n, peak):
+@pytest.mark.parametrize("prefix", [200, 1000])
+def test_chunks_over_several_sequences(n_q, n_kv, D, sizes, n, peak, prefix):
     """Many KV heads leave a head few work-groups: each walks the tiles of several sequences, whose rows have their first
     position and their references' moves at different tiles."""
-    x = Batch(n_q, n_kv, D, sizes, [200] * len(sizes), own_lengths(sizes, 330, 5), n)
+    x = Batch(n_q, n_kv, D, sizes, [prefix] * len(sizes), own_lengths(sizes, 330, 5), n)
     x.q *= peak
     x.check(x.run(), seqs=range(0, sum(sizes), 3))
 
 
-CHUNKS = [(64, 64, 64, 1), (256, 32, 128, 3), (64, 64, 128, 12)]     # few and many rows of a slice
+# few and many rows of a slice; behind short prompts sequences of many rows go alone
+CHUNKS = [(64, 64, 64, 1, 0), (256, 32, 128, 3, 0), (256, 32, 128, 3, 12), (64, 64, 128, 12, 0), (64, 64, 128, 12, 12)]
 
 
-@pytest.mark.parametrize("n_q,n_kv,D,n", CHUNKS)
+@pytest.mark.parametrize("n_q,n_kv,D,n,more", CHUNKS)
 @pytest.mark.parametrize("which,bad", [("k", float("nan")), ("k", float("inf")), ("v", float("nan")), ("v", -float("inf"))])
 @pytest.mark.parametrize("tail", [70, 150])
-def test_chunks_whose_values_are_not_finite(n_q, n_kv, D, n, which, bad, tail):
+def test_chunks_whose_values_are_not_finite(n_q, n_kv, D, n, more, which, bad, tail):
     """A key or value of sequence 1 behind its prompt, in a tile that all of its rows see or some: the others' are as before."""
-    x = Batch(n_q, n_kv, D, [7], [200], [170, tail, 0, 300, 64, 5, 130], n)
+    prefix = 200 + 64 * more
+    x = Batch(n_q, n_kv, D, [7], [prefix], [170, tail, 0, 300, 64, 5, 130], n)
     x.q *= 4
-    p, pool, G = 200 + 65, x.k if which == "k" else x.v, n_q // n_kv
+    p, pool, G = prefix + 65, x.k if which == "k" else x.v, n_q // n_kv
     pool[int(x.table[int(x.slots_h[1]), p // x.page]), x.layer, 0, p % x.page, 5] = bad
     out = x.run()
     x.check(out, seqs=[0, 2, 3, 4, 5, 6])
@@ -170,11 +174,11 @@ def test_chunks_whose_values_are_not_finite(n_q, n_kv, D, n, which, bad, tail):
         assert torch.isnan(out[1, :, :G]).all()
 
 
-@pytest.mark.parametrize("n_q,n_kv,D,n", CHUNKS)
-def test_chunks_with_missing_pages(n_q, n_kv, D, n):
-    x = Batch(n_q, n_kv, D, [7], [200], [170, 150, 0, 300, 64, 5, 130], n)
+@pytest.mark.parametrize("n_q,n_kv,D,n,more", CHUNKS)
+def test_chunks_with_missing_pages(n_q, n_kv, D, n, more):
+    x = Batch(n_q, n_kv, D, [7], [200 + 64 * more], [170, 150, 0, 300, 64, 5, 130], n)
     x.q *= 4
-    for b, lp in ((0, 4), (3, 7), (6, 3)):
+    for b, lp in ((0, 4 + more), (3, 7 + more), (6, 3 + more)):
         x.table[int(x.slots_h[b]), lp] = -1
         keep = torch.ones(len(x.K[b]), dtype=torch.bool, device="cuda")
         keep[64 * lp:64 * lp + 64] = False
@@ -183,9 +187,9 @@ def test_chunks_with_missing_pages(n_q, n_kv, D, n):
     x.check(x.run())
 
 
-@pytest.mark.parametrize("n_q,n_kv,D,n", CHUNKS)
-def test_chunks_with_ragged_rows(n_q, n_kv, D, n):
-    x = Batch(n_q, n_kv, D, [5, 4], [200, 90], [170, 150, 0, 300, 64, 5, 130, 61, 63], n, lens=[n, 0, 1, n, 0, n, 0, 1, n - 1])
+@pytest.mark.parametrize("n_q,n_kv,D,n,more", CHUNKS)
+def test_chunks_with_ragged_rows(n_q, n_kv, D, n, more):
+    x = Batch(n_q, n_kv, D, [5, 4], [200 + 64 * more, 90], [170, 150, 0, 300, 64, 5, 130, 61, 63], n, lens=[n, 0, 1, n, 0, n, 0, 1, n - 1])
     x.q *= 4
     x.check(x.run())
 
