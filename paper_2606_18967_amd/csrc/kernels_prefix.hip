@@ -843,14 +843,26 @@ __global__ void __launch_bounds__(256, 2) k_prefix_attn(rows_t r, kv_geom g, con
     else attend_item<D, 1>(s_buf, s_ml, s_odd, it, inf, r, g, kc, vc, n_q, n_kv, q, q_ld, cs, pl, out, out_t, out_ld);
 }
 
-// The parts of a row joined: a wave a (row, head), D/4 lanes a part, U parts of each under way at once; a
+// Two sums of parts made one: the references, sums and four of the dims.
+struct px_sum { float m, l; float4 o; };
+__device__ __forceinline__ px_sum both(const px_sum& a, const px_sum& b)
+{
+    const float m = fmaxf(a.m, b.m);
+    const float fa = a.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(a.m - m), fb = b.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(b.m - m);
+    return {m, a.l * fa + b.l * fb,
+            make_float4(a.o.x * fa + b.o.x * fb, a.o.y * fa + b.o.y * fb, a.o.z * fa + b.o.z * fb, a.o.w * fa + b.o.w * fb)};
+}
+
+// The parts of a row joined: W waves a (row, head), D/4 lanes a part, U parts of each under way at once; a
 // part that saw nothing of the row is not read.  Bound by the parts' bytes and, with few, by its launch: 64 rows of 32
-// heads in 32 parts (34 MB) take 8 us, 8 rows of 32 heads in 8 parts 5.
-template <int D>
+// heads in 32 parts (34 MB) take 8 us, 8 rows of 32 heads in 20 parts 4.
+template <int D, int W>
 __global__ void __launch_bounds__(256) k_prefix_combine(rows_t r, px_plan pl, int n_q, int n_kv, void* out, int out_t, long long out_ld)
 {
     constexpr int LPP = D / 4, NP = WAVE / LPP, U = 4;             // lanes a part, parts side by side
-    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    __shared__ px_sum s_sum[W > 1 ? W : 1][LPP];
+    const int w = W > 1 ? threadIdx.x >> 6 : 0;
+    const long long unit = W > 1 ? blockIdx.x : (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int G = n_q / n_kv, row = (int)(unit / n_q), head = (int)(unit - (long long)row * n_q), b = row / r.n, i = row - b * r.n;
     if (b >= r.B || (r.lim && i >= r.lim[b])) return;
     const px_seq q = pl.seq[b];
@@ -859,48 +871,48 @@ __global__ void __launch_bounds__(256) k_prefix_combine(rows_t r, px_plan pl, in
     const int kvh = head / G, t = i * G + head - kvh * G, RG = r.n * G, zz = pl.zs == 1 ? 0 : t / PX_ROWS;
     const int stride = pl.zs == 1 ? q.stride : min(PX_ROWS, RG - PX_ROWS * zz);
     const size_t at = (size_t)kvh * pl.part_rows + q.part + (size_t)zz * q.nc * PX_ROWS + (t - PX_ROWS * zz);
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = side; c0 < q.nc; c0 += U * NP) {
+    px_sum s = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int c0 = w * NP + side; c0 < q.nc; c0 += U * W * NP) {
         float2 ml[U];
         float4 x[U];
-        float bm = m;
+        float bm = s.m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             ml[u] = make_float2(-INFINITY, 0.f);
-            if (c0 + u * NP < q.nc) ml[u] = pl.ml[at + (size_t)(c0 + u * NP) * stride];
+            if (c0 + u * W * NP < q.nc) ml[u] = pl.ml[at + (size_t)(c0 + u * W * NP) * stride];
             bm = fmaxf(bm, ml[u].x);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (ml[u].x != -INFINITY || ml[u].y != 0.f) x[u] = *(const float4*)(pl.o + (at + (size_t)(c0 + u * NP) * stride) * D + d);
+            if (ml[u].x != -INFINITY || ml[u].y != 0.f) x[u] = *(const float4*)(pl.o + (at + (size_t)(c0 + u * W * NP) * stride) * D + d);
         }
-        const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - bm);
-        m = bm;
-        l *= f;
-        o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        const float f = s.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(s.m - bm);
+        s = {bm, s.l * f, make_float4(s.o.x * f, s.o.y * f, s.o.z * f, s.o.w * f)};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float e = ml[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - m);
-            l += ml[u].y * e;
-            o = make_float4(o.x + x[u].x * e, o.y + x[u].y * e, o.z + x[u].z * e, o.w + x[u].w * e);
+            const float e = ml[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[u].x - bm);
+            s.l += ml[u].y * e;
+            s.o = make_float4(s.o.x + x[u].x * e, s.o.y + x[u].y * e, s.o.z + x[u].z * e, s.o.w + x[u].w * e);
         }
     }
-    // the sides joined, in all of them alike
+    // the sides joined, in all of them alike, then the waves
 #pragma unroll
-    for (int k = LPP; k < WAVE; k <<= 1) {
-        const float om = __shfl_xor(m, k, WAVE), bm = fmaxf(m, om);
-        const float fa = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - bm), fb = om == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(om - bm);
-        m = bm;
-        l = l * fa + __shfl_xor(l, k, WAVE) * fb;
-        o = make_float4(o.x * fa + __shfl_xor(o.x, k, WAVE) * fb, o.y * fa + __shfl_xor(o.y, k, WAVE) * fb, o.z * fa + __shfl_xor(o.z, k, WAVE) * fb,
-                        o.w * fa + __shfl_xor(o.w, k, WAVE) * fb);
+    for (int k = LPP; k < WAVE; k <<= 1)
+        s = both(s, px_sum{__shfl_xor(s.m, k, WAVE), __shfl_xor(s.l, k, WAVE),
+                           make_float4(__shfl_xor(s.o.x, k, WAVE), __shfl_xor(s.o.y, k, WAVE), __shfl_xor(s.o.z, k, WAVE), __shfl_xor(s.o.w, k, WAVE))});
+    if (W > 1) {
+        if (side == 0) s_sum[w][lane] = s;
+        __syncthreads();
+        if (w) return;
+        s = s_sum[0][lane % LPP];
+#pragma unroll
+        for (int k = 1; k < W; ++k) s = both(s, s_sum[k][lane % LPP]);
     }
     if (side) return;
-    const float rl = l == 0.f ? 0.f : 1.f / l;
+    const float rl = s.l == 0.f ? 0.f : 1.f / s.l;
     px_store4(out, out_t, (size_t)row * out_ld + (size_t)head * D + d,
-              l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * rl, o.y * rl, o.z * rl, o.w * rl));
+              s.l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.o.x * rl, s.o.y * rl, s.o.z * rl, s.o.w * rl));
 }
 
 }  // namespace
@@ -995,9 +1007,14 @@ void launch_prefix_attention(const rows_t& r, px_plan p, const px_groups& g, con
     else prefix_attn_d<64>(r, p, g, c, n_q, q, q_ld, cs, out, out_t, out_ld, s, ev0, ev1);
 }
 
+// Four waves a (row, head) up to so many of them: 4 rows of 16 heads behind 32768 in 256 parts take 25 us a call, with a wave
+// 45, 9 x 10 rows of 4 heads behind 8730 24 and 29.  With more of them the parts are fewer: 64 rows of 32 heads in 8 parts 35 us,
+// with a wave 33.5 (in 32 parts 72.6 and 75.1).
+constexpr int PX_FEW = 512;
 void launch_prefix_combine(const rows_t& r, const px_plan& p, int n_q, int n_kv, int D, void* out, act_t out_t, long long out_ld, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)(((long long)r.B * r.n * n_q + 3) / 4);
-    if (D == 128) k_prefix_combine<128><<<blocks, 256, 0, s>>>(r, p, n_q, n_kv, out, (int)out_t, out_ld);
-    else k_prefix_combine<64><<<blocks, 256, 0, s>>>(r, p, n_q, n_kv, out, (int)out_t, out_ld);
+    const long long units = (long long)r.B * r.n * n_q;
+    auto go = [&](auto kern, long long blocks) { kern<<<(unsigned)blocks, 256, 0, s>>>(r, p, n_q, n_kv, out, (int)out_t, out_ld); };
+    if (units <= PX_FEW) D == 128 ? go(k_prefix_combine<128, 4>, units) : go(k_prefix_combine<64, 4>, units);
+    else D == 128 ? go(k_prefix_combine<128, 1>, (units + 3) / 4) : go(k_prefix_combine<64, 1>, (units + 3) / 4);
 }
