@@ -325,9 +325,10 @@ __global__ void __launch_bounds__(1024) k_policy_rows(logits_args a, policy_args
     }
 }
 
-// A row in several work-groups, where there are few rows: the sums of a part each.
+// A row in several work-groups, where there are few rows: the sums of a part each, and the token's logit, over which a
+// gradient may be written before the last part has read it.
 template <typename T, bool KEEP>
-__global__ void __launch_bounds__(256) k_row_parts(logits_args a, const int32_t* tok, part_t* parts)
+__global__ void __launch_bounds__(256) k_row_parts(logits_args a, const int32_t* tok, part_t* parts, float* at_tok)
 {
     __shared__ float sh[48];
     const int row = blockIdx.y, k = blockIdx.x, c0 = k * a.chunk, n = min(a.chunk, a.V - c0);
@@ -337,7 +338,11 @@ __global__ void __launch_bounds__(256) k_row_parts(logits_args a, const int32_t*
     sum_part<T, 4, KEEP>(s, x, 0, n, a.c);
     sum_tail(s, x, n, a.c);
     s = join(s, a.c, sh);
-    if (threadIdx.x == 0) parts[(size_t)row * gridDim.x + k] = s;
+    if (threadIdx.x == 0) {
+        parts[(size_t)row * gridDim.x + k] = s;
+        const int at = tok[row] - c0;
+        if (at >= 0 && at < n) at_tok[row] = elem<T>::load(x, at);
+    }
 }
 // the parts of a row joined by one wave, in every lane
 __device__ __forceinline__ part_t join_parts(const part_t* parts, int row, int S, float c)
@@ -386,15 +391,14 @@ __global__ void __launch_bounds__(1024) k_logp_rows(logits_args a, logp_args p)
     }
     if (threadIdx.x == 0) put_logp(p, row, s, row_of(s, xt, a.T), live);
 }
-template <typename T>
-__global__ void __launch_bounds__(64) k_logp_finish(logits_args a, logp_args p, const part_t* parts, int S)
+__global__ void __launch_bounds__(64) k_logp_finish(logits_args a, logp_args p, const part_t* parts, int S, const float* at_tok)
 {
     const int row = blockIdx.x, tok = p.tok[row];
     const bool live = tok >= 0 && tok < a.V;
     part_t s = {-INFINITY, 0.f, 0.f};
     float xt = 0.f;
     if (live) {
-        xt = elem<T>::load((const T*)a.x + (long long)row * a.ld, tok);
+        xt = at_tok[row];
         s = join_parts(parts, row, S, a.c);
     }
     if (threadIdx.x == 0) put_logp(p, row, s, row_of(s, xt, a.T), live);
@@ -426,10 +430,8 @@ __global__ void __launch_bounds__(1024) k_logp_grad(logits_args a, logp_grad_arg
 }
 
 // ------------------------------------------------------------------ the loss of few rows
-// The rows' terms from their parts and, by the same work-group, the sums
-// (k_policy_sum's); the rows' gradient factors for k_policy_grad.
-template <typename T>
-__global__ void __launch_bounds__(64) k_policy_finish(logits_args a, policy_args p, const part_t* parts, int S, grad_t* grads)
+// The rows' terms from their parts.
+__global__ void __launch_bounds__(64) k_policy_finish(logits_args a, policy_args p, const part_t* parts, int S, const float* at_tok)
 {
     const int row = blockIdx.x;
     const live_t lv = policy_live(p, row, a.V);
@@ -437,33 +439,33 @@ __global__ void __launch_bounds__(64) k_policy_finish(logits_args a, policy_args
         if (threadIdx.x == 0) dead_row(p, row, lv.drop);
         return;
     }
-    const float xt = elem<T>::load((const T*)a.x + (long long)row * a.ld, p.tok[row]);
     const part_t s = join_parts(parts, row, S, a.c);
-    const row_stat st = row_of(s, xt, a.T);
-    const policy_row o = policy_of(p, row, st);
-    if (threadIdx.x == 0) {
-        put_row(p, row, st, o);
-        grads[row] = grad_of(s.m, st.ln_s, 1.f / (s.s * a.T), st.entropy, o.g, o.h, a.T);
-    }
+    const row_stat st = row_of(s, at_tok[row], a.T);
+    if (threadIdx.x == 0) put_row(p, row, st, policy_of(p, row, st));
 }
+// The same with the gradient of a part: every wave joins the row's parts for itself, which costs less than a launch for it.
 template <typename T, bool ENT>
-__global__ void __launch_bounds__(256) k_policy_grad(logits_args a, policy_args p, const grad_t* grads)
+__global__ void __launch_bounds__(256) k_policy_grad(logits_args a, policy_args p, const part_t* parts, int S, const float* at_tok)
 {
     const int row = blockIdx.y, k = blockIdx.x, c0 = k * a.chunk, n = min(a.chunk, a.V - c0);
     const T* x = (const T*)a.x + (long long)row * a.ld + c0;
     T* out = (T*)a.out + (long long)row * a.out_ld + c0;
-    if (!policy_live(p, row, a.V).live) {
+    const live_t lv = policy_live(p, row, a.V);
+    if (!lv.live) {
+        if (k == 0 && threadIdx.x == 0) dead_row(p, row, lv.drop);
         zero_part(out, n);
         return;
     }
-    const grad_t d = grads[row];
-    const int at = p.tok[row] - c0;
-    float xt = 0.f;
-    if (at >= 0 && at < n) xt = elem<T>::load(x, at);
+    const float xt = at_tok[row];
+    const part_t s = join_parts(parts, row, S, a.c);
+    const row_stat st = row_of(s, xt, a.T);
+    const policy_row o = policy_of(p, row, st);
+    if (k == 0 && threadIdx.x == 0) put_row(p, row, st, o);
+    const grad_t d = grad_of(s.m, st.ln_s, 1.f / (s.s * a.T), st.entropy, o.g, o.h, a.T);
     grad_part<T, ENT, 4>(x, out, 0, n, d, a.c);
     grad_tail<T, ENT>(x, out, n, d, a.c);
     constexpr int N = pack_t<T>::N;
-    const int body = n / N * N;
+    const int at = p.tok[row] - c0, body = n / N * N;
     if (at >= 0 && at < n && threadIdx.x == (at < body ? at / N % blockDim.x : at - body))
         elem<T>::store(out, at, grad_at<ENT>(xt, d, a.c) + d.D);
 }
@@ -505,8 +507,10 @@ void logp_t(const logits_args& a, const logp_args& p, int rows, int S, float* wo
         k_logp_rows<T><<<rows, row_threads<T>(a.V, 1024), 0, s>>>(a, p);
         return;
     }
-    k_row_parts<T, false><<<dim3(S, rows), row_threads<T>(a.chunk, 256), 0, s>>>(a, p.tok, (part_t*)work);
-    k_logp_finish<T><<<rows, 64, 0, s>>>(a, p, (const part_t*)work, S);
+    float* at_tok = work;
+    part_t* parts = (part_t*)(work + rows);
+    k_row_parts<T, false><<<dim3(S, rows), row_threads<T>(a.chunk, 256), 0, s>>>(a, p.tok, parts, at_tok);
+    k_logp_finish<<<rows, 64, 0, s>>>(a, p, parts, S, at_tok);
 }
 template <typename T>
 void policy_t(const logits_args& a, const policy_args& p, int rows, int S, float* work, float* stats, hipStream_t s)
@@ -519,36 +523,40 @@ void policy_t(const logits_args& a, const policy_args& p, int rows, int S, float
         else k_policy_rows<T, false, true><<<rows, nt, 0, s>>>(a, p);
     } else {
         const int nt = row_threads<T>(a.chunk, 256);
-        part_t* parts = (part_t*)work;
-        grad_t* grads = (grad_t*)(work + (size_t)rows * S * 3);
-        if (a.out) k_row_parts<T, true><<<dim3(S, rows), nt, 0, s>>>(a, p.tok, parts);
-        else k_row_parts<T, false><<<dim3(S, rows), nt, 0, s>>>(a, p.tok, parts);
-        k_policy_finish<T><<<rows, 64, 0, s>>>(a, p, parts, S, grads);
-        if (a.out && ent) k_policy_grad<T, true><<<dim3(S, rows), nt, 0, s>>>(a, p, grads);
-        else if (a.out) k_policy_grad<T, false><<<dim3(S, rows), nt, 0, s>>>(a, p, grads);
+        float* at_tok = work;
+        part_t* parts = (part_t*)(work + rows);
+        const dim3 grid(S, rows);
+        if (a.out) k_row_parts<T, true><<<grid, nt, 0, s>>>(a, p.tok, parts, at_tok);
+        else k_row_parts<T, false><<<grid, nt, 0, s>>>(a, p.tok, parts, at_tok);
+        if (!a.out) k_policy_finish<<<rows, 64, 0, s>>>(a, p, parts, S, at_tok);
+        else if (ent) k_policy_grad<T, true><<<grid, nt, 0, s>>>(a, p, parts, S, at_tok);
+        else k_policy_grad<T, false><<<grid, nt, 0, s>>>(a, p, parts, S, at_tok);
     }
     k_policy_sum<<<1, 1024, 0, s>>>(p.terms, rows, stats);
 }
 
 }  // namespace
 
-// Parts of a row: one work-group a row from 512 rows on or where a row is short,
-// else about 1024 work-groups of at least 4096 logits.
+// Parts of a row: few long rows take about 1024 work-groups of at least 4096 logits, others one each.  (The loss with its
+// gradient, in parts and whole, us a call: 14 x 50257 fp32 20.3 and 17.6, 40 x 100000 bf16 19.5 and 21.3, 14 x 128256
+// fp32 19.7 and 25.9, 130 x 128256 bf16 25.4 and 28.8, 200 x 128256 31.4 and 30.8, 416 x 128256 fp32 94.7 and 90.3, 511 x 152064 bf16
+// 75 and 68.)
+constexpr int PART_ROWS = 160, PART_V = 65536;
 static int row_splits(int rows, int V, int* chunk)
 {
     *chunk = V;
-    if (rows < 1 || rows >= 512 || V <= 16384) return 1;
+    if (rows < 1 || rows >= PART_ROWS || V <= PART_V) return 1;
     const int want = (1024 + rows - 1) / rows, most = V / 4096;
     const int S = want < most ? want : most;
     *chunk = ((V + S - 1) / S + 2047) / 2048 * 2048;
     return (V + *chunk - 1) / *chunk;
 }
 
-// for up to so many rows: r < 512 of them have at most 1024 + r - 1 parts
+// for up to so many rows: r < PART_ROWS of them have at most 1024 + r - 1 parts, and their tokens' logits
 size_t logits_work_floats(int rows, int V)
 {
-    const size_t split = V <= 16384 ? 0 : rows < 512 ? rows : 511;
-    return (size_t)rows * POLICY_TERMS + (split ? 3 * (1024 + split) + 4 * split : 0);
+    const size_t split = V <= PART_V ? 0 : rows < PART_ROWS ? rows : PART_ROWS - 1;
+    return (size_t)rows * POLICY_TERMS + (split ? 3 * (1024 + split) + split : 0);
 }
 
 void launch_token_logprobs(logits_args a, const logp_args& p, int rows, bool f32, float* work, hipStream_t s)
