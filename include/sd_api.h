@@ -344,7 +344,7 @@ sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
  * are zeros.  A logit of -inf has p = 0 and no gradient; a row with a NaN, a +inf
  * or no finite logit gives NaN.  Gradients have logits' type, are rounded once,
  * and are written whole; dlogits may be logits itself (same stride), but not overlap it
- * otherwise.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then only
+ * otherwise; the other outputs overlap no input.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then only
  * the loss's stats are written.  workspace: 256-byte aligned, as large as for this
  * many rows or more, its contents need no preparation, calls whose work may overlap
  * need one each.  Errors: SD_E_INVAL,

@@ -937,7 +937,7 @@ template void launch_kv_append<f32_parts>(const rows_t&, const cache_t&, int, in
 template void launch_kv_append<uint16_t>(const rows_t&, const cache_t&, int, int, kv4_src<uint16_t>, kv4_src<uint16_t>, kv4_src<uint16_t>,
                                          uint16_t*, const kv4_rope&, hipStream_t);
 
-// The plan in the attention itself: each wave's own takes about 2 us, a kernel before it 5 (8 groups of 8 behind prompts
+// The plan in the attention itself: each wave's own takes about 3 us, a kernel before it 5 and its launch (8 groups of 8 behind prompts
 // of 2048: 34 us a call instead of 36; one group of 8 behind 512: 15 instead of 17), unless there are many more work-groups
 // than are resident at once.
 bool prefix_plans_itself(const px_plan& p, int B) { return B <= PX_WAVE && (long long)B * p.zs <= p.target; }
