@@ -342,12 +342,13 @@ sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
  * x = logits/temperature, p = softmax(x).  A row whose token is outside [0,
  * vocab) (sd_accept's -1, padding) is absent: its logits are not read, its outputs
  * are zeros.  A logit of -inf has p = 0 and no gradient; a row with a NaN, a +inf
- * or no finite logit gives NaN.  Gradients have logits' type, are rounded once,
- * and are written whole; dlogits may be logits itself (same stride), but not overlap it
- * otherwise; the other outputs overlap no input.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then only
- * the loss's stats are written.  workspace: 256-byte aligned, as large as for this
- * many rows or more, its contents need no preparation, calls whose work may overlap
- * need one each.  Errors: SD_E_INVAL,
+ * or no finite logit gives NaN.  Powers e^(x - max x) below 2^-126 are zeros.
+ * Gradients have logits' type, are rounded once, and are written whole; dlogits may
+ * be logits itself (same stride), but not overlap it otherwise; the other outputs
+ * overlap no input.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then
+ * only the loss's stats are written.  workspace: 256-byte aligned, as large as for
+ * this many rows or more, its contents need no preparation, calls whose work may
+ * overlap need one each.  Errors: SD_E_INVAL,
  * SD_E_UNSUPPORTED (more than 2^21 rows, a vocabulary of more than 2^30). */
 size_t sd_logits_workspace_bytes(int32_t rows, int32_t vocab);
 

@@ -454,8 +454,8 @@ __device__ __forceinline__ constexpr int v_swizzle(int row) { return D == 128 ? 
 // of each).  Positions that a row does not see may hold anything: there the scores
 // are replaced and values that are not finite taken as zeros; a row that sees such a
 // value is NaN.
-// Few rows are bound by HBM: 8 groups of 8 behind prompts of 2048 (135 MB) take 35 us, 31
-// without the products.  Many are bound by the products, the softmax between them and
+// Few rows are bound by HBM: 8 groups of 8 behind prompts of 2048 (135 MB) take 37 us, 35
+// with a plan made before, 33 of them without the products.  Many are bound by the products, the softmax between them and
 // the tiles' way into LDS nearly alike: 64 sequences behind 32768 positions (202 MB, 35
 // GFLOP) take 65 us, 55 with all tiles from one page, 55 without the products; 8 x 8 verify
 // rows of 5 behind 8192 (32B shape) 125 us, 114 and 105, and 150 once the power limit has
