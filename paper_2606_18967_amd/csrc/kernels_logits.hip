@@ -263,9 +263,10 @@ __device__ __forceinline__ policy_row policy_of(const policy_args& p, int row, c
         dkl = -em;
     }
     policy_row o;
-    // (e^x may be infinite for a term that the loss does not have)
+    // (a term that the loss does not have may be infinite or NaN)
     const float klw = p.kl_coef != 0.f ? p.kl_coef * kl : 0.f, dklw = p.kl_coef != 0.f ? p.kl_coef * dkl : 0.f;
-    o.term[0] = w * (pg + klw - p.entropy_coef * st.entropy);
+    const float entw = p.entropy_coef != 0.f ? p.entropy_coef * st.entropy : 0.f;
+    o.term[0] = w * (pg + klw - entw);
     o.term[1] = w * pg;
     o.term[2] = w * kl;
     o.term[3] = w * st.entropy;
