@@ -92,11 +92,11 @@ __device__ __forceinline__ void take(part_t& a, const float (&x)[N], float m, fl
         a.t = __builtin_fmaf(p, fmaxf(y, Y_MIN), a.t);
     }
 }
-// the sums moved to the largest logit m
+// the sums moved to the largest logit m, which is not below their own (so d <= 0, -inf among it; where they met nothing but
+// -inf they are 0, or NaN and stay so)
 __device__ __forceinline__ void move_to(part_t& a, float m, float c)
 {
-    const float d = (origin(a.m) - m) * c, f = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(d);
-    // (NaN sums stay NaN: their m may be anything)
+    const float d = a.m == -INFINITY ? 0.f : (a.m - m) * c, f = __builtin_amdgcn_exp2f(d);
     a.t = (a.t + fmaxf(d, Y_MIN) * a.s) * f;
     a.s *= f;
     a.m = m;
