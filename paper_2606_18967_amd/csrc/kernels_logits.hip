@@ -252,8 +252,10 @@ __device__ __forceinline__ live_t policy_live(const policy_args& p, int row, int
 struct policy_row { float term[POLICY_TERMS], g, h; };
 __device__ __forceinline__ policy_row policy_of(const policy_args& p, int row, const row_stat& st)
 {
-    const float w = p.weight[row], A = p.adv[row], r = expf(st.logp - p.old_logp[row]);
-    const float free = r * A, cut = fminf(fmaxf(r, 1.f - p.clip_low), 1.f + p.clip_high) * A;
+    const float w = p.weight[row], A = p.adv[row], far = st.logp - p.old_logp[row], r = expf(far);
+    // (r may be past fp32's range, and 0 times it is 0 all the same)
+    const float free = A == 0.f && fabsf(far) < INFINITY ? 0.f : r * A;
+    const float cut = fminf(fmaxf(r, 1.f - p.clip_low), 1.f + p.clip_high) * A;
     const bool clipped = cut < free;
     const float pg = -(clipped ? cut : free);                   // a NaN ratio or advantage stays one
     float kl = 0.f, dkl = 0.f;

@@ -68,6 +68,8 @@ def check_masked_policy(xh, t, v, kl, ent, T, out, dtype):
     slope = np.where(live, np.abs(v["w"]) * (np.exp(4) * (np.abs(v["adv"]) + 1) + 1), 0)
     tol = ((e_lp + ref.E24 * 16 + 4 * es * (1 + np.abs(H))) * slope).sum() + ref.E24 * np.abs(stats)
     assert (np.abs(host(out.stats) - stats) <= tol).all(), (host(out.stats), stats, tol)
+    if out.dlogits is None:
+        return
     d, _ = ref.gradient(xh, t, T, g, h)
     scale = ref.gradient(xh, t, T, slope, h)[1]
     tol = (e_lp[:, None] + es * 4 + ref.E24 * 64) * scale + ref.HALF_STEP[dtype] * np.abs(d) + 1e-38
@@ -98,3 +100,20 @@ def test_many_rows_of_masked_logits():
     check_stats(xh, t, T, *sdrl.token_logprobs(x, tok, T))
     v = policy_inputs(xh, t, T, 2, pad=0.0)
     check_masked_policy(xh, t, v, 0.05, 0.02, T, run_policy(x, tok, v, 0.05, 0.02, T), "bf16")
+
+
+@pytest.mark.parametrize("V", [300, 30000, 70001])
+@pytest.mark.parametrize("grad", [False, True])
+def test_a_ratio_out_of_range_times_an_advantage_of_0_is_0(V, grad):
+    """e^(logp - old_logp) past fp32's range at rows whose group's rewards were all alike: their term is 0, as every other
+    ratio's, and so is their gradient."""
+    x, xh = rows(12, V, "f32", 3)
+    t = np.random.default_rng(V).integers(0, V, 12).astype(np.int32)
+    v = policy_inputs(xh, t, 1.0, 3, pad=0.0)
+    del v["ref"], v["beh"]
+    v["old"][::3] -= 300
+    v["adv"][::3] = 0
+    out = run_policy(x, torch.from_numpy(t).cuda(), v, 0.0, 0.01, 1.0, grad=grad)
+    check_masked_policy(xh, t, v, 0.0, 0.01, 1.0, out, "f32")
+    v["adv"][3] = np.nan                                          # what is no number stays none
+    assert np.isnan(host(run_policy(x, torch.from_numpy(t).cuda(), v, 0.0, 0.01, 1.0, grad=grad).stats)[:2]).all()
