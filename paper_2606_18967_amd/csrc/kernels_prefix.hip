@@ -433,6 +433,11 @@ __device__ __forceinline__ uint32_t finite2(uint32_t x)
     return lo | hi;
 }
 
+// Up to a reference of this size a score leaves it as one fused operation with the scale: that is exact but for the reference's own
+// rounding, which all of a row's weights have in common (2^0.5 at most).  Past it the scores are rounded as the reference was,
+// before they leave it: what rounding leaves between the two would be of any size (2^128 from scores of 2^31 on).
+constexpr float PX_FUSED = 0x1p24f;
+
 template <int D>
 __device__ __forceinline__ constexpr int v_swizzle(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
 
@@ -595,15 +600,15 @@ __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32
             for (int i = 0; i < 16; ++i) bm = fmaxf(bm, s[n][i]);
         return other_half_max(bm) * acs;
     };
-    // The probabilities above the reference `from`, into l, and their products with the values `tile` bytes into LDS,
+    // The probabilities 2^(s by - from) above the reference, into l, and their products with the values `tile` bytes into LDS,
     // in an order of my own: a block's values are read while its powers are made, a second block's powers go between the first one's products.
     // cap: +inf, or -inf for a row that sees none of them (whatever its scores are).
-    auto add = [&](uint32_t tile, const auto& s, float from, auto capped, float cap) {
+    auto add = [&](uint32_t tile, const auto& s, float by, float from, auto capped, float cap) {
         constexpr int N = sizeof(s) / sizeof(floatx16), P = 2 * NB;    // products a block
         uint32_t pk[N][8];
         bf16x8 vf[N][P];
         auto power2 = [&](int n, int i) {                          // two of a lane's 16 probabilities
-            float a = __builtin_fmaf(s[n][i], acs, -from), c = __builtin_fmaf(s[n][i + 1], acs, -from);
+            float a = __builtin_fmaf(s[n][i], by, -from), c = __builtin_fmaf(s[n][i + 1], by, -from);
             if (decltype(capped)::value) a = fminf(a, cap), c = fminf(c, cap);
             a = __builtin_amdgcn_exp2f(a);
             c = __builtin_amdgcn_exp2f(c);
@@ -642,7 +647,8 @@ __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32
                 }
             }
     };
-    // A block that some row does not see (a row sees its positions from blk up to `to`), or whose scores move a reference.
+    // A block that some row does not see (a row sees its positions from blk up to `to`), whose scores move a reference, or with
+    // a reference past PX_FUSED.
     auto slow_block = [&](uint32_t tile, int blk, int to, uint32_t odd) {
         floatx16 s[1];
         scores(tile, s);
@@ -665,7 +671,15 @@ __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32
         if (odd)
             for (int p = 0; p < 32; ++p)
                 if ((odd >> p & 1) && blk + p <= to) l = __builtin_nanf("");
-        add(tile + TILE, s, m == -INFINITY ? 0.f : m, std::false_type(), 0.f);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float by = acs;
+        if (fabsf(ref) > PX_FUSED) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] *= acs;
+            by = 1.f;
+        }
+        asm volatile("" : "+v"(by));                               // (a known 1 would let the compiler fuse the two again)
+        add(tile + TILE, s, by, ref, std::false_type(), 0.f);
     };
     // Values that are not finite in the wave's own 16 positions of a tile become zeros, which 0 times nothing of them is left,
     // and the positions' bits are noted for the rows that see them.  (Of a block without a page this is what lies there,
@@ -694,9 +708,9 @@ __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32
     };
 
     // The walk.  Tiles are of three kinds: what every row sees as a whole, what the rows of one sequence see as a whole and the
-    // others not at all, and the rest.  The first two, as long as they move no reference, are loops of their own, which
-    // change no sum but by adding: with the references' rescaling inside them the compiler keeps a second copy of O and
-    // moves it every tile.
+    // others not at all, and the rest.  The first two, as long as they move no reference and find none past PX_FUSED, are loops
+    // of their own, which change no sum but by adding: with the references' rescaling inside them the compiler keeps a second
+    // copy of O and moves it every tile.
     enum { ALL, ONE, PART };
     const bool works = 32 * rt < nrows;
     const int from = wide ? 0 : w >> 1, first_row = r0 / G;        // the wave's first block, the slice's first row of its sequence
@@ -737,11 +751,12 @@ __device__ __forceinline__ void attend_item(uint8_t* s_buf, float2* s_ml, uint32
                     if (odd && sr == cur.seq) l = __builtin_nanf("");
                 }
                 m = m == -INFINITY ? top : m;                      // nothing seen so far: nothing to rescale
-                if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
+                const float ref = m == -INFINITY ? 0.f : m;
+                if (__builtin_amdgcn_ballot_w64(top > m + 8.f || fabsf(ref) > PX_FUSED)) {
                     kind = PART;
                     return;
                 }
-                add(tile + TILE, s, m == -INFINITY ? 0.f : m, std::integral_constant<bool, KIND == ONE>(), cap);
+                add(tile + TILE, s, acs, ref, std::integral_constant<bool, KIND == ONE>(), cap);
                 more = advance();
             }
         };
