@@ -180,8 +180,8 @@ def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: 
 class Rollout:
     """One model on the GPU with a dense KV cache (kv4: a paged one in 4 bits; group > 1: a paged one whose groups of so
     many share their prompt) for B sequences of up to prompt + lmax positions, the drafter buffer, and flat device buffers
-    viewed at the live batch size and draft length of each iteration.  logprobs: the responses and their tokens'
-    log-probabilities are kept by slot and place (resp, logp)."""
+    viewed at the live batch size and draft length of each iteration.  logprobs: run() returns the responses and their
+    tokens' log-probabilities too."""
 
     def __init__(self, cfg: dict, B: int, prompt: int, lmax: int, gmax: int = max(GAMMA_SET), seed: int = 3,
                  T: float = 1.0, fmt: str = "w4", graphs: bool = False, padded: bool | None = None,
@@ -258,7 +258,7 @@ class Rollout:
                          next_tok=torch.zeros(B, dtype=i32, device=dev),
                          ar_out=torch.zeros(B, dtype=i32, device=dev),
                          ar_logits=torch.zeros(B * V, dtype=f32, device=dev))
-        # the responses and their tokens' ln p by slot and place; the last column takes what is not kept
+        # a run's responses and their tokens' ln p by slot and place; the last column takes what is not kept
         self.width = self.eng.max_ctx - prompt + 1
         if logprobs:
             self.resp = torch.zeros((B, self.width), dtype=i32, device=dev)
@@ -281,6 +281,9 @@ class Rollout:
 
     def run(self, policy: str, gamma: int, tau_prev: float, cost, eps: float, lengths, step: int,
             keep_trace: bool = True) -> tuple[RolloutResult, dict]:
+        """One rollout of training step `step`: its result and the decode loop's statistics.  With log-probabilities
+        the latter hold "tokens" (int32) and "logp" (fp32), [B][places], of this run alone: row b has gen[b] tokens, of
+        which the first lengths[b] are its response, then -1 and 0."""
         torch, eng, V = self.torch, self.eng, self.cfg["vocab"]
         if len(lengths) != self.B:
             raise ValueError("one length per sequence")
@@ -294,6 +297,9 @@ class Rollout:
         torch.cuda.synchronize()
         prep_ms = e0.elapsed_time(e1)
         self.kv_len.fill_(self.prompt)
+        if self.logprobs:
+            self.resp.fill_(-1)
+            self.logp.zero_()
         state = dict(slots=torch.arange(self.B, dtype=torch.int32, device=self.dev),
                      last=synth.make_tokens(self.B, 1, V, self.seed + 7 + step)[:, 0].to(self.dev).contiguous())
         T, seed = self.T, self.seed
@@ -404,7 +410,7 @@ class Rollout:
                     keep_trace=keep_trace, group=self.group)
         eng.sync()
         if self.logprobs:
-            st["tokens"], st["logp"] = self.resp[:self.B], self.logp[:self.B]   # [B][lmax and more], up to each length
+            st["tokens"], st["logp"] = (t[:self.B, :self.width - 1].clone() for t in (self.resp, self.logp))
         res = RolloutResult(policy=policy, step=step, gamma=gamma, tau_prev=tau_prev, tau=st["tau"],
                             makespan_s=st["makespan_s"], prep_ms=prep_ms, ar_iters=st["ar_iters"],
                             sd_iters=st["sd_iters"], tokens=int(np.asarray(lengths).sum()),
