@@ -50,6 +50,7 @@ from __future__ import annotations
 
 import argparse
 import json
+import os
 import sys
 import time
 from dataclasses import asdict, dataclass, field
@@ -96,6 +97,7 @@ class RolloutResult:
     trace: list = field(default_factory=list)   # (mode, B, S_mean, ms, emitted) per iteration
     graphs: int = 0                     # HIP graphs captured during the rollout
     capture_s: float = 0.0              # their capture time (outside makespan_s)
+    mean_logp: float | None = None      # of the response tokens (None: log-probabilities are not kept)
 
 
 def grouped_tables(B: int, group: int, spare: int, prompt: int, max_ctx: int, page: int):
@@ -409,14 +411,17 @@ class Rollout:
                     ar_padded if self.padded else ar_fn, sd_padded if self.padded else sd_fn, compact_fn,
                     keep_trace=keep_trace, group=self.group)
         eng.sync()
+        mean_logp = None
         if self.logprobs:
             st["tokens"], st["logp"] = (t[:self.B, :self.width - 1].clone() for t in (self.resp, self.logp))
+            lp = st["logp"].cpu().numpy()
+            mean_logp = sum(lp[b, :n].sum(dtype=np.float64) for b, n in enumerate(lengths)) / max(int(np.sum(lengths)), 1)
         res = RolloutResult(policy=policy, step=step, gamma=gamma, tau_prev=tau_prev, tau=st["tau"],
                             makespan_s=st["makespan_s"], prep_ms=prep_ms, ar_iters=st["ar_iters"],
                             sd_iters=st["sd_iters"], tokens=int(np.asarray(lengths).sum()),
                             switch_iter=st["switch_iter"], switch_B=st["switch_B"], trace=st["trace"],
                             graphs=sum(e["graph"] is not None for e in cache.values()),
-                            capture_s=st.get("capture_s", 0.0))
+                            capture_s=st.get("capture_s", 0.0), mean_logp=mean_logp)
         return res, st
 
     def close(self):
@@ -508,7 +513,10 @@ def main(argv=None):
                          "(bucket, draft length) and per AR bucket")
     ap.add_argument("--kv4", action="store_true", help="hold the KV cache in 4 bits (paged)")
     ap.add_argument("--group", type=int, default=1, help="responses of each prompt, which share its KV pages and their reads")
-    ap.add_argument("--logprobs", action="store_true", help="keep every response token's log-probability")
+    ap.add_argument("--logprobs", action="store_true",
+                    help="every response token's log-probability: their mean, and with --out FILE.json the tokens and their "
+                         "log-probabilities themselves, in FILE.logp.npz (by policy: <policy>_tokens and _logp [steps][B][places], "
+                         "_gen and _lengths [steps][B])")
     ap.add_argument("--tau-carry", action="store_true",
                     help="carry the toggle's tau to a new draft length through the acceptance rate "
                          "(default: Algorithm 1 as written, the measured tau as it is)")
@@ -535,13 +543,19 @@ def main(argv=None):
     lengths_fn = lambda t: response_lengths(a.B, a.median, a.sigma, a.lmin, a.lmax, a.seed * 1000 + t)
     # one untimed rollout to load every kernel
     ro.run("sd", GAMMA_SET[0], float(GAMMA_SET[0]), cost, EPS, np.minimum(lengths_fn(0), 64), 99, keep_trace=False)
+    kept = {}                              # array's name -> of each training step
     def run_and_report(p, g, tp, L, t):
-        r = ro.run(p, g, tp, cost, EPS, L, t)[0]
+        r, st = ro.run(p, g, tp, cost, EPS, L, t)
+        if a.logprobs and a.out:
+            for name, x in (("tokens", st["tokens"].cpu().numpy()), ("logp", st["logp"].cpu().numpy()),
+                            ("gen", np.array(st["gen"])), ("lengths", np.array(L))):
+                kept.setdefault(f"{p}_{name}", []).append(x)
         # one line per training step as soon as it ends (a policy's steps can take minutes in all)
         log(f"{p:9s} step {r.step}: gamma {r.gamma:2d}  tau_prev {r.tau_prev:5.2f}  tau "
             f"{'  -  ' if r.tau is None else f'{r.tau:5.2f}'}  makespan {r.makespan_s:7.3f} s  "
             f"AR iters {r.ar_iters:5d}  SD iters {r.sd_iters:5d}  SD on at B={r.switch_B}  prep {r.prep_ms:.1f} ms"
-            f"  graphs {r.graphs} ({r.capture_s:.2f} s to capture)")
+            f"  graphs {r.graphs} ({r.capture_s:.2f} s to capture)"
+            + (f"  mean ln p {r.mean_logp:.4f}" if a.logprobs else ""))
         return r
 
     results = {}
@@ -554,8 +568,13 @@ def main(argv=None):
                    lengths=dict(median=a.median, sigma=a.sigma, lo=a.lmin, hi=a.lmax, mean_step0=float(L0.mean()),
                                 max_step0=int(L0.max())),
                    calib=dict(F_eff=calib["F_eff"], params=calib["params"], kv4=a.kv4),
+                   logprobs=None, mean_logp={p: [r.mean_logp for r in rs] for p, rs in results.items()},
                    makespan_s={p: [r.makespan_s for r in rs] for p, rs in results.items()},
                    results={p: [asdict(r) for r in rs] for p, rs in results.items()})
+    if kept:
+        arrays = os.path.splitext(a.out)[0] + ".logp.npz"
+        np.savez(arrays, **{name: np.stack(x) for name, x in kept.items()})
+        summary["logprobs"] = os.path.basename(arrays)
     if a.out:
         with open(a.out, "w") as fh:
             json.dump(summary, fh)
@@ -563,7 +582,8 @@ def main(argv=None):
                           makespan_s=summary["makespan_s"],
                           tau={p: [r.tau for r in rs] for p, rs in results.items()},
                           gamma={p: [r.gamma for r in rs] for p, rs in results.items()},
-                          switch_B={p: [r.switch_B for r in rs] for p, rs in results.items()})))
+                          switch_B={p: [r.switch_B for r in rs] for p, rs in results.items()},
+                          logprobs=a.logprobs, mean_logp=summary["mean_logp"])))
 
 
 if __name__ == "__main__":

@@ -29,3 +29,38 @@ def test_results_outlive_the_next_run(group):
         assert (st["tokens"][past] == -1).all() and (st["logp"][past] == 0).all()
         assert (st["tokens"][~past] >= 0).all() and (st["logp"][~past] < 0).all()
     r.close()
+
+
+@pytest.mark.parametrize("out", [True, False])
+def test_the_command_keeps_log_probabilities(tmp_path, monkeypatch, capsys, out):
+    say("rollout --logprobs", out)
+    kept = {}
+    plain = rollout.Rollout.run
+
+    def spy(self, policy, gamma, tau_prev, cost, eps, lengths, step, keep_trace=True):
+        r = plain(self, policy, gamma, tau_prev, cost, eps, lengths, step, keep_trace)
+        kept[policy, step] = {k: v.cpu().numpy() if isinstance(v, torch.Tensor) else np.array(v) for k, v in r[1].items() if k in ("tokens", "logp", "gen")}
+        kept[policy, step]["lengths"] = np.array(lengths)
+        return r
+
+    monkeypatch.setattr(rollout.Rollout, "run", spy)
+    calib, to = tmp_path / "calib.json", tmp_path / "run.json"
+    calib.write_text(json.dumps(dict(F_eff=1e14, params={}, kv4=False)))
+    rollout.main(["--model", "TINY_BF16", "--B", "8", "--prompt", "64", "--lmin", "4", "--lmax", "24", "--median", "12", "--steps", "2",
+                  "--policies", "ar,sd", "--calib", str(calib), "--logprobs"] + (["--out", str(to)] if out else []))
+    line = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    mean = lambda p, t: np.mean([kept[p, t]["logp"][b, :n].mean(dtype=np.float64) * n for b, n in enumerate(kept[p, t]["lengths"])]) * 8 / kept[p, t]["lengths"].sum()  # noqa: E731
+    for p in ("ar", "sd"):
+        for t in range(2):
+            # sums of at most 192 fp32 values in fp64, however they are ordered
+            assert abs(line["mean_logp"][p][t] - mean(p, t)) <= 1e-12 * abs(mean(p, t))
+    assert line["logprobs"] is True
+    if not out:
+        return
+    summary = json.loads(to.read_text())
+    with np.load(tmp_path / summary["logprobs"], allow_pickle=False) as f:
+        for p in ("ar", "sd"):
+            for t in range(2):
+                for k in ("tokens", "logp", "gen", "lengths"):
+                    assert np.array_equal(f[f"{p}_{k}"][t], kept[p, t][k]), (p, t, k)
+    assert summary["mean_logp"] == line["mean_logp"]
