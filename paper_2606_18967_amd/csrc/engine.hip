@@ -789,7 +789,7 @@ extern "C" sd_status sd_prefix_attention(const sd_kv_cache* c, const sd_prefix_g
     if ((st = check_prefix_rows(B, n, n_q, c->n_kv)) != SD_OK) return st;
     if (!rows_ok(q, q_ld, n_q, c->head_dim, 2) || !rows_ok(out, out_ld, n_q, c->head_dim, 2))
         return fail(SD_E_INVAL, "q and out must be 16-byte aligned, with row strides of whole 16 bytes >= n_q*head_dim");
-    if (!isfinite(scale)) return fail(SD_E_INVAL, "scale must be finite");
+    if (!isfinite(scale * 1.4426950408889634f)) return fail(SD_E_INVAL, "scale, and scale log2 e, must be finite");
     if (!workspace || ((uintptr_t)workspace & 255)) return fail(SD_E_INVAL, "workspace is NULL or not 256-byte aligned");
     px_plan p = prefix_plan(B, n, n_q, c->n_kv);
     const size_t need = prefix_plan_bytes(p, B, c->n_kv, c->head_dim);
