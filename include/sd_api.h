@@ -295,9 +295,11 @@ typedef struct {
  * slots of group g hold the same keys and values, as they do where their block
  * tables name the same pages.  Sequences of a group that follow one another in a
  * call's batch and have at least len[g] positions cached (fewer: as many as the
- * shortest has) are attended together: what they share, in whole tiles of 64
- * positions, is read once, through the table of the first of them.  A batch in
- * another order is attended right too, and reads more. */
+ * shortest has) are attended together, in slices of up to 128 query rows a KV head
+ * (n n_q/n_kv of each): what they share, in whole tiles of 64 positions, is read once
+ * a slice, through the table of the run's first.  Where that is little beside their rows'
+ * work each is attended for itself.  A batch in another order is attended right too,
+ * and reads more. */
 typedef struct {
     const int32_t* group;
     const int32_t* len;
@@ -317,8 +319,8 @@ size_t sd_prefix_workspace_bytes(const sd_kv_cache* c, int32_t B, int32_t n, int
 
 /* sd_kv4_attention's rows (same arguments) over the bf16 cache: row (b, i) sees the
  * positions up to its own, appended before.  groups may be NULL: nothing is shared.
- * B up to 1024.  Scores, the softmax's statistics and all sums are fp32, the
- * probabilities enter the second product in bf16 (2^-8 of each).  The results do
+ * B up to 1024; scale and scale log2 e finite.  Scores, the softmax's statistics and all
+ * sums are fp32, the probabilities enter the second product in bf16 (2^-8 of each).  The results do
  * not depend on what a row does not see.  A key that is not finite makes the rows
  * that see it NaN, but for scores of -inf, which are as if masked; a value that is not
  * finite leaves the row not finite in its dimension, and may make all of it NaN.  A
@@ -341,8 +343,8 @@ sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
  * sd_dtype `dtype` at row stride ld >= vocab (elements; any element alignment),
  * x = logits/temperature, p = softmax(x).  A row whose token is outside [0,
  * vocab) (sd_accept's -1, padding) is absent: its logits are not read, its outputs
- * are zeros.  A logit of -inf has p = 0 and no gradient; a row with a NaN, a +inf
- * or no finite logit gives NaN.  Powers e^(x - max x) below 2^-126 are zeros.
+ * are zeros.  A logit of -inf has p = 0 and no gradient but, as a token's own, what
+ * its [j = token] gives; a row with a NaN, a +inf or no finite logit gives NaN.  Powers e^(x - max x) below 2^-126 are zeros.
  * Gradients have logits' type, are rounded once, and are written whole; dlogits may
  * be logits itself (same stride), but not overlap it otherwise; the other outputs
  * overlap no input.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then
@@ -380,7 +382,8 @@ sd_status sd_token_logprobs_grad(int32_t dtype, int32_t rows, int32_t vocab, con
  * term, of its KL term, of H, of the tokens whose gradient the clipping cuts, and of
  * the dropped rows' weights; logp and entropy (may be NULL) as above; dlogits (may be
  * NULL): the loss's gradient.  Where the ratio is at a border the unclipped side's
- * gradient is taken. */
+ * gradient is taken.  An advantage of 0 gives a clipped term of 0 for any finite old_logp;
+ * a term without a coefficient is not in the loss, whatever its own sum is. */
 typedef struct {
     float temperature;
     float clip_low, clip_high;      /* 0 <= clip_low <= 1, 0 <= clip_high */

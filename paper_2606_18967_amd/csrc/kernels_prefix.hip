@@ -97,10 +97,10 @@ __global__ void __launch_bounds__(256) k_kv_append(rows_t r, kv_geom g, uint16_t
 // the tiles of all), so that the work-groups are alike and resident at once, however
 // the batch divides between shared and own positions: with items of their own for the
 // sequences' tails, 8 groups of 8 behind prompts of 2048 (responses of up to 512) took
-// 42 us instead of 35, for a tail's item was 4 us of tiles and 8 of start and end.  All
+// a fifth longer, for a tail's item was 4 us of tiles and 8 of start and end.  All
 // tiles count alike: an own tile of a wide slice is a wave's work, but comes from memory
 // for this slice alone (counted as 2/3 of a shared one, 64 sequences behind 32768 took
-// 77 us a call instead of 68, as 5/4 72).
+// 13% longer, as 5/4 6%).
 
 // inclusive sum over the 1024 threads of a work-group; sh: 16 ints
 __device__ __forceinline__ int scan1024(int v, int* sh)
@@ -953,8 +953,8 @@ template void launch_kv_append<uint16_t>(const rows_t&, const cache_t&, int, int
                                          uint16_t*, const kv4_rope&, hipStream_t);
 
 // The plan in the attention itself: each wave's own takes about 3 us, a kernel before it 5 and its launch (8 groups of 8 behind prompts
-// of 2048: 34 us a call instead of 36; one group of 8 behind 512: 15 instead of 17), unless there are many more work-groups
-// than are resident at once.
+// of 2048: 40.2 us a call instead of 42.1; one group of 8 behind 512: 14.4 instead of 16.4), unless there are many more
+// work-groups than are resident at once.
 bool prefix_plans_itself(const px_plan& p, int B) { return B <= PX_WAVE && (long long)B * p.zs <= p.target; }
 
 // Two work-groups a CU are resident.  A slice may have one chunk more than its share of the target (and one more is what the

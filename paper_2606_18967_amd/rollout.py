@@ -31,8 +31,11 @@ makespan measured is that of the decode phase.
 With a group of G > 1 the responses come in groups of G of one prompt (the
 paper samples 8 of each, Sec. 5.1): a group's block tables name the same pages
 for the prompt's whole pages, its prompt is prefilled once, and every step's
-attention reads it once for all of the group's live responses.  The toggle then
-prices the positions that a step reads, the shared ones once.
+attention reads it once for each 128 query rows a KV head of the group's live
+responses.  The toggle then prices the positions that a step cannot but read, the
+shared ones once a group, with a cost model that is calibrated on the attention
+without groups: a verify whose rows fill several such slices reads more, and wide
+groups are bound by their products, so prices of grouped steps are estimates from below.
 
 With log-probabilities on, every response token's ln p under the policy that
 drew it is kept (speculative or not, tokens follow softmax(p / T) of the target),
@@ -123,7 +126,8 @@ def decode(lengths: np.ndarray, prompt: int, policy: str, gamma: int, tau_prev: 
     counts n_emit before truncation at the response's end).  compact_fn(keep)
     drops the rows whose keep flag is False.  cost is an sdrl.CostModel for
     the toggle, which is given the mean positions that a step reads for a live
-    row: with groups of `group` rows a prompt counts once for its live ones.
+    row: with groups of `group` rows a prompt counts once for its live ones (a
+    lower bound: the attention reads it once a slice of their query rows).
     Returns the loop's statistics."""
     if policy not in POLICIES:
         raise ValueError(f"unknown policy {policy!r}")

@@ -843,7 +843,8 @@ def token_logprobs(logits, tokens, T: float = 1.0, workspace=None):
     ln sum e^((logit - largest)/T)): logits [..., V] (fp32 or bf16, rows at one stride), tokens int32 [...];
     returns fp32 logp [...], entropy [...] and norm [..., 2].  A token outside [0, V), as the -1 that accept
     writes past n_emit, has no row: zeros (so a trainer gives a padded or shifted batch's logits whole, not a slice
-    [:, :-1], whose rows are not at one stride).  workspace: a uint8 tensor of logits_workspace_bytes, for callers that
+    [:, :-1], whose rows are not at one stride).  The results have no autograd graph: their gradient by the logits is
+    token_logprobs_grad's, which a trainer passes on with logits.backward(...).  workspace: a uint8 tensor of logits_workspace_bytes, for callers that
     keep one."""
     xp, ld, dt = _logit_rows(logits, "logits")
     dev, V, shape, rows = logits.device, logits.shape[-1], logits.shape[:-1], tokens.numel()
