@@ -346,8 +346,8 @@ sd_status sd_bind_prefix(sd_engine e, const sd_prefix_groups* groups);
  * are zeros.  A logit of -inf has p = 0 and no gradient but, as a token's own, what
  * its [j = token] gives; a row with a NaN, a +inf or no finite logit gives NaN.  Powers e^(x - max x) below 2^-126 are zeros.
  * Gradients have logits' type, are rounded once, and are written whole; dlogits may
- * be logits itself (same stride), but not overlap it otherwise; the other outputs
- * overlap no input.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then
+ * be logits itself (same stride) or its neighbour in rows of one buffer (same stride),
+ * but not overlap it otherwise; the other outputs overlap no input.  Sums are fp32 or wider, in a fixed order.  rows may be 0, then
  * only the loss's stats are written.  workspace: 256-byte aligned, as large as for
  * this many rows or more, its contents need no preparation, calls whose work may
  * overlap need one each.  Errors: SD_E_INVAL,

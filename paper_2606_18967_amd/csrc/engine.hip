@@ -1320,7 +1320,10 @@ static sd_status check_logits(int dtype, int rows, int vocab, const void* x, int
     if (out_ld < vocab || out_ld > INT_MAX) return fail(SD_E_INVAL, "dlogits_ld=%lld outside [vocab, 2^31)", (long long)out_ld);
     const uintptr_t a = (uintptr_t)x, b = (uintptr_t)out;
     const uintptr_t ae = a + ((uintptr_t)(rows - 1) * ld + vocab) * el, be = b + ((uintptr_t)(rows - 1) * out_ld + vocab) * el;
-    if (a < be && b < ae && !(a == b && (ld == out_ld || rows == 1)))
+    // (rows at one stride may lie side by side, as columns of one buffer)
+    const uintptr_t w = (uintptr_t)vocab * el, L = (uintptr_t)ld * el, d = b >= a ? (b - a) % L : (L - (a - b) % L) % L;
+    const bool apart = ld == out_ld && d >= w && d + w <= L;
+    if (a < be && b < ae && !apart && !(a == b && (ld == out_ld || rows == 1)))
         return fail(SD_E_INVAL, "dlogits must be logits itself, at the same stride, or not overlap it");
     return SD_OK;
 }
