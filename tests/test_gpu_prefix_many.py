@@ -2,7 +2,6 @@
 slices a sequence, every sequence compared; and rows with other sequences of their group beside them."""
 import numpy as np
 import pytest
-import torch
 
 from paper_2606_18967_amd import sdrl
 from prefix_ref import Batch
